@@ -254,7 +254,8 @@ def prepare(case, seed):
             n = lm.embed_bwd_workspace_bytes(T, c["V"], c["D"])
         else:
             op = {"logp": lm.TOKEN_LOSS_OP_LOGP, "policy": lm.TOKEN_LOSS_OP_POLICY, "preference": lm.TOKEN_LOSS_OP_PREFERENCE}[kind]
-            n = lm.token_loss_workspace_bytes(op, T, c["V"], c["V"] + c["pad"], c.get("pairs", 0), s["z"].dtype)
+            n = lm.token_loss_workspace_bytes(op, T, c["V"], c["V"] + c["pad"], c.get("pairs", 0),
+                                              lm.LORA_BF16 if c["dt"] == "bf16" else lm.LORA_F32)
         s["ws"] = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
     s["case"] = c
     return s
