@@ -306,6 +306,123 @@ lora_status_t lora_ckpt_backward(const lora_node_t *nodes, int n, int64_t T, con
                                  void *dx0, const void *host_stash, size_t host_bytes, void *ws,
                                  size_t ws_bytes, void *compute_stream, void *copy_stream);
 
+/* ---- Embedding --------------------------------------------------------------
+ * The ends of the chain of linears: token ids to the first node's input, and
+ * the gradient of a trained embedding table [V, D].
+ *   embed_fwd       out[t] = scale table[ids[t]]            [T, D], type dt
+ *   embed_bwd       dtable[v] = scale sum_{t: ids[t] = v} dout[t]
+ *                   [V, D] fp32, overwritten (rows of tokens that do not occur
+ *                   are 0), or with accumulate != 0 added to
+ *   embed_bwd_rows  the same without the rows of absent tokens: tokens[i], i <
+ *                   min(T, V), lists the distinct ids in ascending order and then
+ *                   -1, rows[i] [D] fp32 their gradients and then zeros.
+ * ids are int32 device values; one outside [0, V) gives a zero row of out and
+ * no gradient (a padding position, say).  table, out and dout have type dt; out is
+ * rounded once.  Sums are fp32, over ascending t in groups whose size depends on T
+ * alone.  D a multiple of 8 (LORA_EUNSUPPORTED).  T and V up to 2^30, matrices up
+ * to 2^40 elements. */
+lora_status_t embed_fwd(const void *table, const int32_t *ids, void *out, int64_t T, int64_t V,
+                        int64_t D, float scale, lora_dtype_t dt, void *hip_stream);
+size_t embed_bwd_workspace_bytes(int64_t T, int64_t V, int64_t D);
+lora_status_t embed_bwd(const int32_t *ids, const void *dout, float *dtable, int64_t T, int64_t V,
+                        int64_t D, float scale, int accumulate, lora_dtype_t dt, void *ws,
+                        size_t ws_bytes, void *hip_stream);
+lora_status_t embed_bwd_rows(const int32_t *ids, const void *dout, int32_t *tokens, float *rows,
+                             int64_t T, int64_t V, int64_t D, float scale, lora_dtype_t dt,
+                             void *ws, size_t ws_bytes, void *hip_stream);
+
+/* ---- Losses over the targets' log-probabilities --------------------------------
+ * From the head's logits z [T, ldz] (type dt, the first V columns; a forward with
+ * r = 0 gives them) to the gradient dlogits that frozen_linear_bwd_dx takes as its
+ * dy.  With targets y [T] int32 and weights w [T] fp32 (NULL: all 1):
+ *   logp[t] = z_t[y_t] - log sum_{j < V} exp(z_tj)   where w[t] != 0, else 0.
+ * Logits of positions of weight 0 (a prompt, padding) are not read, nor are
+ * the other values of such a position: its loss is 0 and its row of dlogits zeros.
+ *
+ * policy_loss: with advantages A, the log-probabilities old_logp of the policy that
+ * produced the tokens and ref_logp of the reference (NULL where kl_coef = 0),
+ *   rho_t = exp(logp_t - old_t),  d_t = ref_t - logp_t,
+ *   L_t   = - min(rho_t A_t, min(max(rho_t, 1 - clip_lo), 1 + clip_hi) A_t)
+ *           + kl_coef (exp(d_t) - d_t - 1),
+ *   loss  = sum_t w_t L_t   (w carries the mean: 1 / number of positions, say).
+ * preference_loss: sequences of the flattened positions in pairs, chosen
+ * [seq[2i], seq[2i+1]) and rejected [seq[2i+1], seq[2i+2]) for i < npairs (seq
+ * [2 npairs + 1] int32, ascending; a sequence may be empty, positions outside all
+ * of them have no gradient),
+ *   margin_i = beta (sum over chosen - sum over rejected of w_t (logp_t - ref_t))
+ *   loss     = mean over i of -(1 - eps) log sigma(margin_i) - eps log sigma(-margin_i)
+ * with eps = label_smoothing and ref_logp NULL for a reference of 0.
+ * Both:  dlogits_tj = dloss/dlogp_t ([j = y_t] - softmax(z_t)_j), [T, ldz] of type
+ * dt with zeros in columns V .. ldz, rounded once; NULL: the loss only.  dlogits may
+ * be logits itself.  Where the clipped and the free term of L_t are equal the free
+ * one's derivative is taken.
+ *
+ * A target outside [0, V) at a position of weight != 0 gives NaN (logp, the loss and
+ * that row); logits of -inf are forbidden tokens of probability 0.  Rows of logits
+ * must be whole 16-byte vectors (ldz a multiple of 8 bf16, 4 fp32;
+ * LORA_EUNSUPPORTED); V is any.  loss is one fp32, margins [npairs] and logp [T]
+ * fp32.  Statistics are fp32, the sums over positions 64-bit.  Workspace:
+ * token_loss_workspace_bytes ((size_t)-1 for rejected sizes; npairs counts for
+ * TOKEN_LOSS_OP_PREFERENCE only). */
+typedef enum {
+  TOKEN_LOSS_OP_LOGP = 0,
+  TOKEN_LOSS_OP_POLICY = 1,
+  TOKEN_LOSS_OP_PREFERENCE = 2
+} token_loss_op_t;
+size_t token_loss_workspace_bytes(token_loss_op_t op, int64_t T, int64_t V, int64_t ldz,
+                                  int64_t npairs, lora_dtype_t dt);
+lora_status_t token_logp(const void *logits, int64_t ldz, const int32_t *targets,
+                         const float *weights, float *logp, int64_t T, int64_t V, lora_dtype_t dt,
+                         void *ws, size_t ws_bytes, void *hip_stream);
+lora_status_t policy_loss(const void *logits, int64_t ldz, const int32_t *targets,
+                          const float *weights, const float *advantages, const float *old_logp,
+                          const float *ref_logp, float *loss, float *logp, void *dlogits,
+                          int64_t T, int64_t V, float clip_lo, float clip_hi, float kl_coef,
+                          lora_dtype_t dt, void *ws, size_t ws_bytes, void *hip_stream);
+lora_status_t preference_loss(const void *logits, int64_t ldz, const int32_t *targets,
+                              const float *weights, const float *ref_logp, const int32_t *seq,
+                              int64_t npairs, float *loss, float *margins, float *logp,
+                              void *dlogits, int64_t T, int64_t V, float beta,
+                              float label_smoothing, lora_dtype_t dt, void *ws, size_t ws_bytes,
+                              void *hip_stream);
+
+/* ---- Clipping by the global norm -------------------------------------------------
+ * All gradients of a step (every node's dA and dB, embedding rows) as one list:
+ *   norm = sqrt(sum of g^2 over all elements of all of them)
+ *   c    = 1 if norm <= max_norm, else max_norm / norm;   out = c g
+ * Squares are summed in 64 bits.  A norm that is not finite makes c 0 or NaN by this
+ * formula; norm tells.
+ * A list is laid out once, in device memory of the caller (grad_list_bytes), for
+ * buffers that a program keeps: grad_list_init writes it on hip_stream and fills the
+ * host struct.  The memory also holds the partial sums of the calls, so calls on one
+ * list are ordered on one stream.  The list refers to the gradients' buffers, not to
+ * their values.
+ *   g    n elements of type dt; n = 0 entries are skipped
+ *   out  n elements of type out_dt that grad_clip writes: g itself (same type), a
+ *        buffer of its own, or NULL in a list used for grad_norm alone
+ * Errors: LORA_EINVAL (NULL or misaligned pointers, negative n, an output that
+ * overlaps another range, a list not laid out, max_norm negative or NaN),
+ * LORA_EUNSUPPORTED (over 2^20 gradients or 2^40 elements), LORA_EWORKSPACE, LORA_EHIP. */
+typedef struct {
+  const void *g;
+  void *out;
+  int64_t n;
+  lora_dtype_t dt, out_dt;
+} lora_grad_t;
+typedef struct { /* filled by grad_list_init */
+  void *mem;
+  int64_t elems;
+  int32_t nchunk, chunk, has_out;
+} lora_grad_list_t;
+size_t grad_list_bytes(const lora_grad_t *grads, int64_t n);
+lora_status_t grad_list_init(lora_grad_list_t *list, const lora_grad_t *grads, int64_t n,
+                             void *mem, size_t mem_bytes, void *hip_stream);
+/* norm [1] fp32 */
+lora_status_t grad_norm(const lora_grad_list_t *list, float *norm, void *hip_stream);
+/* norm [2] fp32: the norm before clipping, and c */
+lora_status_t grad_clip(const lora_grad_list_t *list, float max_norm, float *norm,
+                        void *hip_stream);
+
 /* ---- Plan and hand-over diagnostics -----------------------------------------
  * Which kernel configuration lora_linear_fwd / lora_linear_bwd run for these
  * sizes (host logic only, no GPU work): the output tile of the forward GEMM

@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "../../include/lora_mi355x.h"
+#include "api_util.hpp"
 #include "launch.hpp"
 
 using namespace lora;
@@ -25,35 +26,14 @@ void lora::set_last_error(const char *msg) { std::snprintf(g_err, sizeof g_err, 
 
 namespace {
 
-lora_status_t fail(lora_status_t s, const char *msg) {
-  lora::set_last_error(msg);
-  return s;
-}
-
-// ----- kernel timing hook ----------------------------------------------------
-enum KernelId {
-  K_GEMM_FWD = 0,     // y  = x W^T + (s u) B^T
-  K_GEMM_BWD_DX,      // dx = dy W + du A, with the dA / dB token reductions alongside
-  K_GEMM_FROZEN_DX,   // dx = dy W (rank 0)
-  K_LORA_DOWN,        // u  = x A^T (+ LoRA-step operands)
-  K_LORA_DY_B,        // du = s dy B (+ LoRA-step operand)
-  K_GEMM_FWD_Q,       // gemm_fwd with the quantized W dequantized on the fly
-  K_GEMM_BWD_DX_Q,    // gemm_bwd_dx, quantized W
-  K_GEMM_FROZEN_DX_Q, // gemm_frozen_dx, quantized W
-  K_HEAD_VOCAB,       // reduced vocabulary (mark, compact, target positions)
-  K_HEAD_GATHER,      // gathers of the trainable hidden rows and of the rows of J
-  K_HEAD_LOGITS,      // logits GEMM with the row-statistics epilogue (+ combine)
-  K_HEAD_DZ,          // logits recomputed, softmax gradient epilogue
-  K_HEAD_DH,          // dh += dz W_J (fp32), then the bf16 dh rows
-  K_TOPK_SIM,         // similarity GEMM with the candidate epilogue (+ row norms)
-  K_TOPK_SELECT,      // per-row selection of the k best candidates
-  K_COUNT
-};
+// ----- kernel timing hook (api_util.hpp) ---------------------------------------
 const char *kKernelNames[K_COUNT] = {"gemm_fwd",   "gemm_bwd_dx",   "gemm_frozen_dx",
                                      "lora_down",  "lora_dy_b",     "gemm_fwd_q",
                                      "gemm_bwd_dx_q", "gemm_frozen_dx_q", "head_vocab",
                                      "head_gather", "head_logits", "head_dz", "head_dh",
-                                     "topk_sim", "topk_select"};
+                                     "topk_sim", "topk_select", "embed_fwd", "embed_sort", "embed_grad",
+                                     "token_logp", "policy_loss", "preference_loss", "grad_norm",
+                                     "grad_scale"};
 
 struct EventPair {
   hipEvent_t a, b;
@@ -62,57 +42,29 @@ std::mutex g_prof_mu;
 bool g_prof_on = false;
 std::vector<EventPair> g_prof[K_COUNT];
 
-struct Timed {
-  int id;
-  hipStream_t st;
-  EventPair ev{nullptr, nullptr};
-  bool on = false;
-  Timed(int id_, hipStream_t st_) : id(id_), st(st_) {
-    std::lock_guard<std::mutex> lk(g_prof_mu);
-    if (!g_prof_on) return;
-    if (hipEventCreate(&ev.a) != hipSuccess || hipEventCreate(&ev.b) != hipSuccess) return;
-    on = hipEventRecord(ev.a, st) == hipSuccess;
-  }
-  void done() {
-    if (!on) return;
-    if (hipEventRecord(ev.b, st) != hipSuccess) return;
-    std::lock_guard<std::mutex> lk(g_prof_mu);
-    g_prof[id].push_back(ev);
-    on = false;
-  }
-};
+}  // namespace
 
-// ----- validation helpers ------------------------------------------------------
-constexpr int64_t kMaxElems = (int64_t(1) << 31) - 1;
+lora::Timed::Timed(int id_, hipStream_t st_) : id(id_), st(st_) {
+  std::lock_guard<std::mutex> lk(g_prof_mu);
+  if (!g_prof_on) return;
+  if (hipEventCreate(&a) != hipSuccess || hipEventCreate(&b) != hipSuccess) return;
+  on = hipEventRecord(a, st) == hipSuccess;
+}
+void lora::Timed::done() {
+  if (!on) return;
+  if (hipEventRecord(b, st) != hipSuccess) return;
+  std::lock_guard<std::mutex> lk(g_prof_mu);
+  g_prof[id].push_back({a, b});
+  on = false;
+}
+
+namespace {
+
 constexpr int kMaxRank = 128;
-constexpr int64_t kMaxDim = int64_t(1) << 20;  // keeps every tile's byte offsets within 32 bits
 
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-struct Range {
-  uintptr_t lo, hi;  // [lo, hi)
-  bool set;
-};
-Range rng(const void *p, int64_t bytes) {
-  if (!p || bytes <= 0) return {0, 0, false};
-  uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-  return {lo, lo + (uintptr_t)bytes, true};
-}
-bool overlap(const Range &a, const Range &b) {
-  return a.set && b.set && a.lo < b.hi && b.lo < a.hi;
-}
 bool any_overlap(const std::vector<Range> &outs, const std::vector<Range> &ins) {
-  for (size_t i = 0; i < outs.size(); ++i) {
-    for (const Range &x : ins)
-      if (overlap(outs[i], x)) return true;
-    for (size_t j = i + 1; j < outs.size(); ++j)
-      if (overlap(outs[i], outs[j])) return true;
-  }
-  return false;
+  return lora::any_overlap(outs.data(), outs.size(), ins.data(), ins.size());
 }
-
-size_t esize(lora_dtype_t dt) { return dt == LORA_BF16 ? 2 : 4; }
-size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
 
 lora_status_t check_shapes(int64_t T, int64_t d_in, int64_t d_out, int64_t r, lora_dtype_t dt) {
   if (dt != LORA_BF16 && dt != LORA_F32) return fail(LORA_EINVAL, "unknown dtype");
@@ -408,14 +360,6 @@ bool topk_paired(int64_t V, int64_t k) {
   return V >= TOPK_BLOCK && topk_layout(V, k, true).total <= (size_t(32) << 30);
 }
 
-lora_status_t check_ws(void *ws, size_t ws_bytes, size_t need) {
-  if (need == 0) return LORA_OK;
-  if (!ws) return fail(LORA_EWORKSPACE, "workspace required but ws is NULL");
-  if (ws_bytes < need) return fail(LORA_EWORKSPACE, "workspace too small");
-  if (!aligned16(ws)) return fail(LORA_EINVAL, "workspace not 16-byte aligned");
-  return LORA_OK;
-}
-
 // A quantized frozen weight W [d_out, d_in]: unsigned codes of `bits` bits
 // ([d_out][d_in * bits / 8] bytes; two 4-bit codes per byte, the even input in
 // the low nibble), W = scale * code + offset with one fp32 scale and offset per
@@ -465,11 +409,6 @@ bool narrow_fits(const NarrowWs &nw, void *ws, size_t ws_bytes, const std::vecto
   if (!nw.taken && !nw.u_narrow) return false;
   if (nw.total == 0) return true;
   return ws && ws_bytes >= nw.total && aligned16(ws) && !any_overlap({rng(ws, (int64_t)nw.total)}, operands);
-}
-
-lora_status_t hip_fail(hipError_t e, const char *what) {
-  std::snprintf(g_err, sizeof g_err, "%s: %s", what, hipGetErrorString(e));
-  return LORA_EHIP;
 }
 
 // Forward with a bf16/fp32 W, or (qc != NULL) a quantized one.

@@ -90,6 +90,20 @@ __device__ __forceinline__ u32x4 pack_vec(F32, const float *f) {
   return r;
 }
 
+// The VEC floats of one 16-byte vector of element type E.
+__device__ __forceinline__ void unpack_vec(BF16, u32x4 v, float *f) {
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    f[2 * d] = __builtin_bit_cast(float, v[d] << 16);
+    f[2 * d + 1] = __builtin_bit_cast(float, v[d] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void unpack_vec(F32, u32x4 v, float *f) {
+  const f32x4 x = __builtin_bit_cast(f32x4, v);
+#pragma unroll
+  for (int d = 0; d < 4; ++d) f[d] = x[d];
+}
+
 // Register transpose of a VEC x VEC block.  in[i] holds row i (VEC
 // consecutive columns); out[c] receives column c (VEC consecutive rows).
 __device__ __forceinline__ void transpose_block(BF16, const u32x4 *in, u32x4 *out) {

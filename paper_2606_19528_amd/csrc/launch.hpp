@@ -377,6 +377,74 @@ struct RowSplit {
 };
 RowSplit row_split(int64_t T, int64_t L, int r, Dtype dt);
 
+// ---- embedding lookup and its gradient (embed.hip) ----
+hipError_t launch_embed_fwd(const void *table, const int32_t *ids, void *out, int T, int V, int D, float scale, Dtype d,
+                            hipStream_t st);
+// Sort and workspace (byte offsets) of an embedding gradient: `passes` digits
+// of `digit` bits over `ntile` tiles; the sums over `nchunk` chunks of `chunk`
+// sorted positions.
+struct EmbedPlan {
+  int passes, digit, ntile, chunk, nchunk;
+  size_t key[2], pos[2], seg, segcount, count, partial, total;
+};
+EmbedPlan embed_plan(int64_t T, int64_t V, int64_t D);
+// Sorts the positions by token; with `tokens` also numbers the distinct tokens
+// and lists them there.
+hipError_t launch_embed_sort(const int32_t *ids, int T, int V, const EmbedPlan &p, char *ws, int32_t *tokens, hipStream_t st);
+// out [V][D] (tokens null; accumulate adds to it, else it is overwritten) or
+// [min(T, V)][D] in the order of `tokens`, after launch_embed_sort on the same ws.
+hipError_t launch_embed_grad(const void *dout, float *out, int32_t *tokens, int T, int V, int D, float scale, bool accumulate,
+                             Dtype d, const EmbedPlan &p, char *ws, hipStream_t st);
+
+// ---- losses over the targets' log-probabilities (tokenloss.hip) ----
+struct TokenLoss {
+  const void *z;  // logits [T][ld], the first V columns
+  int64_t ld;
+  int T, V;
+  const int32_t *y;
+  const float *w;  // null: 1
+  float *logp;     // [T]
+  void *dz;        // [T][ld] or null; may be z
+  // workspace: per row (max, log of the sum of exponentials), dL/dlogp, w L
+  float *stat, *coef, *rows;
+  float *loss;
+};
+struct PolicyArgs {
+  const float *adv, *old_logp, *ref;  // ref null: no KL term
+  float lo, hi, kl;                   // ratio bounds 1 - clip_lo, 1 + clip_hi
+};
+struct PairArgs {
+  const float *ref;  // null: 0
+  const int32_t *seq;
+  int pairs;
+  float beta, smooth;
+  float *margins;
+};
+hipError_t launch_token_logp(const TokenLoss &a, Dtype d, hipStream_t st);
+hipError_t launch_policy_loss(const TokenLoss &a, const PolicyArgs &p, Dtype d, hipStream_t st);
+hipError_t launch_preference_loss(const TokenLoss &a, const PairArgs &p, Dtype d, hipStream_t st);
+
+// ---- norm and clipping of a list of gradients (gradclip.hip) ----
+struct GradChunk {  // up to `chunk` elements of one gradient
+  const void *g;
+  void *out;
+  int n, flags;  // bit 0: g is fp32, bit 1: out is fp32
+};
+struct GradEntry {  // one gradient, as handed to the kernel that lays out its chunks
+  const void *g;
+  void *out;
+  int64_t n;
+  int first, flags;  // its first chunk
+};
+constexpr int GRAD_ENTRIES = 96;  // per launch: 3 KB of kernel arguments
+struct GradEntries {
+  GradEntry e[GRAD_ENTRIES];
+};
+constexpr int GRAD_PARTS = 1024;  // workgroups of the norm, one partial sum each
+hipError_t launch_grad_layout(const GradEntries &e, int count, int chunk, GradChunk *out, hipStream_t st);
+hipError_t launch_grad_norm(const GradChunk *c, int nchunk, double *part, float *norm, hipStream_t st);
+hipError_t launch_grad_clip(const GradChunk *c, int nchunk, double *part, float max_norm, float *norm, hipStream_t st);
+
 // Padded row length of the LoRA-step operands (a multiple of the GEMM stage).
 inline int tail_ld(int r, Dtype dt) {
   const int s = dt == DT_BF16 ? 64 : 32;

@@ -41,6 +41,18 @@ class _FewTokenPlan(ctypes.Structure):
     _fields_ += [(n, ctypes.c_size_t) for n in ("fwd_bytes", "bwd_bytes", "fwd_tiled_bytes", "bwd_tiled_bytes")]
 
 
+class _Grad(ctypes.Structure):
+    """lora_grad_t of the C ABI."""
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("dt", ctypes.c_int), ("out_dt", ctypes.c_int)]
+
+
+class _GradList(ctypes.Structure):
+    """lora_grad_list_t of the C ABI."""
+    _fields_ = [("mem", ctypes.c_void_p), ("elems", ctypes.c_int64), ("nchunk", ctypes.c_int32),
+                ("chunk", ctypes.c_int32), ("has_out", ctypes.c_int32)]
+
+
 class LoraError(RuntimeError):
     def __init__(self, status: int, where: str, detail: str):
         super().__init__(f"{where}: status {status} ({detail})")
@@ -103,6 +115,31 @@ def lib() -> ctypes.CDLL:
     L.topk_table_workspace_bytes_paired.restype = sz
     L.topk_table_build.argtypes = [vp, i64, i64, i64, vp, vp, vp, sz, vp]
     L.topk_table_build.restype = i32
+    L.embed_fwd.argtypes = [vp, vp, vp, i64, i64, i64, f32, i32, vp]
+    L.embed_fwd.restype = i32
+    L.embed_bwd_workspace_bytes.argtypes = [i64, i64, i64]
+    L.embed_bwd_workspace_bytes.restype = sz
+    L.embed_bwd.argtypes = [vp, vp, vp, i64, i64, i64, f32, i32, i32, vp, sz, vp]
+    L.embed_bwd.restype = i32
+    L.embed_bwd_rows.argtypes = [vp, vp, vp, vp, i64, i64, i64, f32, i32, vp, sz, vp]
+    L.embed_bwd_rows.restype = i32
+    L.token_loss_workspace_bytes.argtypes = [i32, i64, i64, i64, i64, i32]
+    L.token_loss_workspace_bytes.restype = sz
+    L.token_logp.argtypes = [vp, i64, vp, vp, vp, i64, i64, i32, vp, sz, vp]
+    L.token_logp.restype = i32
+    L.policy_loss.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, f32, f32, f32, i32, vp, sz, vp]
+    L.policy_loss.restype = i32
+    L.preference_loss.argtypes = [vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, vp, i64, i64, f32, f32, i32, vp, sz, vp]
+    L.preference_loss.restype = i32
+    GP, LP = ctypes.POINTER(_Grad), ctypes.POINTER(_GradList)
+    L.grad_list_bytes.argtypes = [GP, i64]
+    L.grad_list_bytes.restype = sz
+    L.grad_list_init.argtypes = [LP, GP, i64, vp, sz, vp]
+    L.grad_list_init.restype = i32
+    L.grad_norm.argtypes = [LP, vp, vp]
+    L.grad_norm.restype = i32
+    L.grad_clip.argtypes = [LP, f32, vp, vp]
+    L.grad_clip.restype = i32
     L.lora_status_str.argtypes = [i32]
     L.lora_status_str.restype = ctypes.c_char_p
     L.lora_last_error.argtypes = []
@@ -435,6 +472,194 @@ def lora_ckpt_backward(nodes, g_n, dx0, host_stash, ws, compute_stream=None, cop
                                   _stream(copy_stream))
     _check(st, "lora_ckpt_backward")
     return dx0
+
+
+# --- embedding, losses over the targets, clipping ------------------------------------
+def _want(t, name: str, dtype, shape=None):
+    """Refuses a tensor of another type, shape or place than the call takes."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU")
+    return t
+
+
+def embed_fwd(table, ids, out, scale: float = 1.0, stream=None):
+    """out[t] = scale table[ids[t]]; an id outside the table gives zeros."""
+    import torch
+
+    (V, D), T = table.shape, ids.shape[0]
+    dt = _dtype_code(table)
+    _want(table, "table", table.dtype), _want(ids, "ids", torch.int32, (T,)), _want(out, "out", table.dtype, (T, D))
+    st = lib().embed_fwd(_ptr(table), _ptr(ids), _ptr(out), T, V, D, float(scale), dt, _stream(stream))
+    _check(st, "embed_fwd")
+    return out
+
+
+def embed_bwd_workspace_bytes(T: int, V: int, D: int) -> int:
+    n = lib().embed_bwd_workspace_bytes(T, V, D)
+    if n == ctypes.c_size_t(-1).value:
+        raise LoraError(LORA_EINVAL, "embed_bwd_workspace_bytes", lib().lora_last_error().decode())
+    return int(n)
+
+
+def embed_bwd(ids, dout, dtable, scale: float = 1.0, accumulate: bool = False, ws=None, stream=None):
+    """dtable[v] = scale times the sum of dout over the positions of token v
+    (added to dtable with `accumulate`)."""
+    import torch
+
+    (T, D), V = dout.shape, dtable.shape[0]
+    dt = _dtype_code(dout)
+    _want(ids, "ids", torch.int32, (T,)), _want(dout, "dout", dout.dtype), _want(dtable, "dtable", torch.float32, (V, D))
+    ws, ws_bytes = _ws(ws, embed_bwd_workspace_bytes(T, V, D), dout, stream)
+    st = lib().embed_bwd(_ptr(ids), _ptr(dout), _ptr(dtable), T, V, D, float(scale), 1 if accumulate else 0, dt, _ptr(ws),
+                         ws_bytes, _stream(stream))
+    _check(st, "embed_bwd")
+    return dtable
+
+
+def embed_bwd_rows(ids, dout, V: int, tokens, rows, scale: float = 1.0, ws=None, stream=None):
+    """embed_bwd without the rows of absent tokens: tokens [min(T, V)] receives the
+    distinct ids in ascending order and then -1, rows their gradients and then zeros."""
+    import torch
+
+    T, D = dout.shape
+    dt = _dtype_code(dout)
+    _want(ids, "ids", torch.int32, (T,)), _want(dout, "dout", dout.dtype)
+    _want(tokens, "tokens", torch.int32, (min(T, V),)), _want(rows, "rows", torch.float32, (min(T, V), D))
+    ws, ws_bytes = _ws(ws, embed_bwd_workspace_bytes(T, V, D), dout, stream)
+    st = lib().embed_bwd_rows(_ptr(ids), _ptr(dout), _ptr(tokens), _ptr(rows), T, V, D, float(scale), dt, _ptr(ws), ws_bytes,
+                              _stream(stream))
+    _check(st, "embed_bwd_rows")
+    return tokens, rows
+
+
+TOKEN_LOSS_OP_LOGP, TOKEN_LOSS_OP_POLICY, TOKEN_LOSS_OP_PREFERENCE = 0, 1, 2
+
+
+def token_loss_workspace_bytes(op: int, T: int, V: int, ldz: int, npairs: int = 0, dt: int = LORA_BF16) -> int:
+    n = lib().token_loss_workspace_bytes(op, T, V, ldz, npairs, dt)
+    if n == ctypes.c_size_t(-1).value:
+        raise LoraError(LORA_EINVAL, "token_loss_workspace_bytes", lib().lora_last_error().decode())
+    return int(n)
+
+
+def _loss_inputs(op, logits, targets, weights, logp, dlogits, vocab, npairs, ws, stream, rows):
+    """(T, V, ldz, type code, workspace, its bytes) of a loss call; `rows` names its
+    further fp32 [T] inputs."""
+    import torch
+
+    T, ldz = logits.shape
+    V = ldz if vocab is None else int(vocab)
+    dt = _dtype_code(logits)
+    _want(logits, "logits", logits.dtype), _want(targets, "targets", torch.int32, (T,))
+    for name, t in {"weights": weights, "logp": logp, **rows}.items():
+        if t is not None:
+            _want(t, name, torch.float32, (T,))
+    if dlogits is not None:
+        _want(dlogits, "dlogits", logits.dtype, (T, ldz))
+    ws, ws_bytes = _ws(ws, token_loss_workspace_bytes(op, T, V, ldz, npairs, dt), logits, stream)
+    return T, V, ldz, dt, ws, ws_bytes
+
+
+def token_logp(logits, targets, logp, weights=None, vocab=None, ws=None, stream=None):
+    """logp[t] = log softmax(logits[t, :vocab])[targets[t]]; 0 where weights[t] is 0."""
+    T, V, ldz, dt, ws, ws_bytes = _loss_inputs(TOKEN_LOSS_OP_LOGP, logits, targets, weights, logp, None, vocab, 0, ws, stream,
+                                               {})
+    st = lib().token_logp(_ptr(logits), ldz, _ptr(targets), _ptr(weights), _ptr(logp), T, V, dt, _ptr(ws), ws_bytes,
+                          _stream(stream))
+    _check(st, "token_logp")
+    return logp
+
+
+def policy_loss(logits, targets, weights, advantages, old_logp, ref_logp, loss, logp, dlogits=None, clip_lo: float = 0.2,
+                clip_hi: float = 0.2, kl_coef: float = 0.0, vocab=None, ws=None, stream=None):
+    """Clipped policy loss with a KL term (see the header): fills loss [1], logp [T]
+    and, when given, dlogits (which may be logits)."""
+    import torch
+
+    T, V, ldz, dt, ws, ws_bytes = _loss_inputs(TOKEN_LOSS_OP_POLICY, logits, targets, weights, logp, dlogits, vocab, 0, ws,
+                                               stream, {"advantages": advantages, "old_logp": old_logp, "ref_logp": ref_logp})
+    _want(loss, "loss", torch.float32, (1,))
+    st = lib().policy_loss(_ptr(logits), ldz, _ptr(targets), _ptr(weights), _ptr(advantages), _ptr(old_logp), _ptr(ref_logp),
+                           _ptr(loss), _ptr(logp), _ptr(dlogits), T, V, float(clip_lo), float(clip_hi), float(kl_coef), dt,
+                           _ptr(ws), ws_bytes, _stream(stream))
+    _check(st, "policy_loss")
+    return loss
+
+
+def preference_loss(logits, targets, weights, ref_logp, seq, loss, margins, logp, dlogits=None, beta: float = 0.1,
+                    label_smoothing: float = 0.0, vocab=None, ws=None, stream=None):
+    """Preference loss of the pairs of sequences that seq [2 pairs + 1] delimits (see
+    the header): fills loss [1], margins [pairs], logp [T] and, when given, dlogits."""
+    import torch
+
+    npairs = margins.shape[0]
+    T, V, ldz, dt, ws, ws_bytes = _loss_inputs(TOKEN_LOSS_OP_PREFERENCE, logits, targets, weights, logp, dlogits, vocab, npairs,
+                                               ws, stream, {"ref_logp": ref_logp})
+    _want(loss, "loss", torch.float32, (1,)), _want(margins, "margins", torch.float32, (npairs,))
+    _want(seq, "seq", torch.int32, (2 * npairs + 1,))
+    st = lib().preference_loss(_ptr(logits), ldz, _ptr(targets), _ptr(weights), _ptr(ref_logp), _ptr(seq), npairs, _ptr(loss),
+                               _ptr(margins), _ptr(logp), _ptr(dlogits), T, V, float(beta), float(label_smoothing), dt,
+                               _ptr(ws), ws_bytes, _stream(stream))
+    _check(st, "preference_loss")
+    return loss
+
+
+class GradList:
+    """Gradients laid out for grad_norm and grad_clip (grad_list).  Holds the
+    tensors, so that their memory stays theirs."""
+
+    def __init__(self, grads, out=None, stream=None):
+        import torch
+
+        grads = list(grads)
+        out = grads if out is None else list(out)
+        if len(out) != len(grads):
+            raise ValueError("as many outputs as gradients are required")
+        arr = (_Grad * max(len(grads), 1))()
+        for i, (g, o) in enumerate(zip(grads, out)):
+            for name, t in (("a gradient", g), ("an output", o)):
+                _want(t, name, t.dtype)
+                _ptr(t)
+            if o.numel() != g.numel():
+                raise ValueError("an output has another size than its gradient")
+            arr[i] = _Grad(g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(g), _dtype_code(o))
+        n = lib().grad_list_bytes(arr, len(grads))
+        if n == ctypes.c_size_t(-1).value:
+            raise LoraError(LORA_EINVAL, "grad_list_bytes", lib().lora_last_error().decode())
+        self.mem, nbytes = _ws(None, int(n), grads[0], stream)
+        self.list = _GradList()
+        self.tensors = (grads, out)
+        _check(lib().grad_list_init(ctypes.byref(self.list), arr, len(grads), _ptr(self.mem), nbytes, _stream(stream)),
+               "grad_list_init")
+
+
+def grad_list(grads, out=None, stream=None) -> GradList:
+    """Lays out a step's gradients (bf16 or fp32 tensors) once for grad_norm and
+    grad_clip; `out` receives the clipped gradients (default: in place)."""
+    return GradList(grads, out, stream)
+
+
+def grad_norm(grads: GradList, norm, stream=None):
+    """norm [1] = global norm of the listed gradients."""
+    import torch
+
+    _want(norm, "norm", torch.float32, (1,))
+    _check(lib().grad_norm(ctypes.byref(grads.list), _ptr(norm), _stream(stream)), "grad_norm")
+    return norm
+
+
+def grad_clip(grads: GradList, max_norm: float, norm, stream=None):
+    """Scales the listed gradients so that their global norm is at most max_norm;
+    norm [2] receives the norm before and the factor."""
+    import torch
+
+    _want(norm, "norm", torch.float32, (2,))
+    _check(lib().grad_clip(ctypes.byref(grads.list), float(max_norm), _ptr(norm), _stream(stream)), "grad_clip")
+    return norm
 
 
 # --- kernel timing hook (benchmarks) -----------------------------------------------
