@@ -405,10 +405,19 @@ struct TokenLoss {
   const float *w;  // null: 1
   float *logp;     // [T]
   void *dz;        // [T][ld] or null; may be z
-  // workspace: per row (max, log of the sum of exponentials), dL/dlogp, w L
-  float *stat, *coef, *rows;
   float *loss;
+  int parts, part_vecs;  // loss_plan
+  // workspace: (maximum, sum of exponentials) of each part of each row, and behind
+  // them of each row (preference); the targets' logits; w dL/dlogp (preference);
+  // w L (policy) or a pair's loss
+  float *stat, *ztgt, *coef, *rows;
 };
+// Parts of a row, a workgroup each, in the launches for few rows, and their
+// length in 16-byte vectors.
+struct LossPlan {
+  int parts, part_vecs;
+};
+LossPlan loss_plan(int64_t T, int64_t V, int64_t ld, Dtype d);
 struct PolicyArgs {
   const float *adv, *old_logp, *ref;  // ref null: no KL term
   float lo, hi, kl;                   // ratio bounds 1 - clip_lo, 1 + clip_hi

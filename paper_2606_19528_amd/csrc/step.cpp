@@ -74,22 +74,22 @@ lora_status_t embed_grad(const int32_t *ids, const void *dout, float *out, int32
 
 // ----- losses over the targets' log-probabilities ---------------------------------
 struct LossLayout {
-  size_t stat, coef, rows, total;
+  LossPlan plan;
+  size_t stat, ztgt, coef, rows, total;
 };
-LossLayout loss_layout(int op, int64_t T, int64_t pairs) {
+LossLayout loss_layout(int op, int64_t T, int64_t V, int64_t ldz, int64_t pairs, lora_dtype_t dt) {
   LossLayout L{};
+  L.plan = loss_plan(T, V, ldz, dtype(dt));
+  const bool pref = op == TOKEN_LOSS_OP_PREFERENCE;
   size_t off = 0;
-  if (op == TOKEN_LOSS_OP_PREFERENCE) {
-    L.stat = off;
-    off += round256((size_t)T * 8);
-    L.coef = off;
-    off += round256((size_t)T * 4);
-    L.rows = off;
-    off += round256((size_t)pairs * 4);
-  } else if (op == TOKEN_LOSS_OP_POLICY) {
-    L.rows = off;
-    off += round256((size_t)T * 4);
-  }
+  L.stat = off;  // of the parts, and of the rows
+  off += pref || L.plan.parts > 1 ? round256((size_t)T * (L.plan.parts + (pref ? 1 : 0)) * 8) : 0;
+  L.ztgt = off;
+  off += pref || L.plan.parts > 1 ? round256((size_t)T * 4) : 0;
+  L.coef = off;
+  off += pref ? round256((size_t)T * 4) : 0;
+  L.rows = off;
+  off += op == TOKEN_LOSS_OP_LOGP ? 0 : round256((size_t)(pref ? pairs : T) * 4);
   L.total = off;
   return L;
 }
@@ -110,13 +110,13 @@ lora_status_t check_loss_sizes(int op, int64_t T, int64_t V, int64_t ldz, int64_
 // are the inputs and `out` the outputs of one of them, besides logits, targets,
 // weights, logp and dlogits.
 lora_status_t check_loss(int op, const void *logits, int64_t ldz, const int32_t *targets, const float *weights, float *logp,
-                         void *dlogits, int64_t T, int64_t pairs, lora_dtype_t dt, const Range *more,
+                         void *dlogits, int64_t T, int64_t V, int64_t pairs, lora_dtype_t dt, const Range *more,
                          size_t n_more, const Range *out, size_t n_out, void *ws, size_t ws_bytes, LossLayout *L) {
   lora_status_t s;
   if (!logits || !targets || !logp) return fail(LORA_EINVAL, "logits, targets and logp are required");
   const void *ptrs[] = {logits, targets, weights, logp, dlogits};
   if (misaligned(ptrs)) return fail(LORA_EINVAL, "pointers must be 16-byte aligned");
-  *L = loss_layout(op, T, pairs);
+  *L = loss_layout(op, T, V, ldz, pairs, dt);
   if ((s = check_ws(ws, ws_bytes, L->total)) != LORA_OK) return s;
   const int64_t zb = T * ldz * (int64_t)esize(dt);
   Range ins[8], outs[8];
@@ -135,7 +135,8 @@ lora_status_t check_loss(int op, const void *logits, int64_t ldz, const int32_t 
 }
 
 TokenLoss loss_args(const void *logits, int64_t ldz, const int32_t *targets, const float *weights, float *logp, void *dlogits,
-                    float *loss, int64_t T, int64_t V) {
+                    float *loss, int64_t T, int64_t V, const LossLayout &L, void *ws) {
+  char *wsb = (char *)ws;
   TokenLoss a{};
   a.z = logits;
   a.ld = ldz;
@@ -146,6 +147,12 @@ TokenLoss loss_args(const void *logits, int64_t ldz, const int32_t *targets, con
   a.logp = logp;
   a.dz = dlogits;
   a.loss = loss;
+  a.parts = L.plan.parts;
+  a.part_vecs = L.plan.part_vecs;
+  a.stat = (float *)(wsb + L.stat);
+  a.ztgt = (float *)(wsb + L.ztgt);
+  a.coef = L.coef == L.rows ? nullptr : (float *)(wsb + L.coef);
+  a.rows = (float *)(wsb + L.rows);
   return a;
 }
 
@@ -274,7 +281,7 @@ lora_status_t embed_bwd_rows(const int32_t *ids, const void *dout, int32_t *toke
 
 size_t token_loss_workspace_bytes(token_loss_op_t op, int64_t T, int64_t V, int64_t ldz, int64_t npairs, lora_dtype_t dt) {
   if (check_loss_sizes(op, T, V, ldz, npairs, dt) != LORA_OK) return (size_t)-1;
-  return loss_layout(op, T, npairs).total;
+  return loss_layout(op, T, V, ldz, npairs, dt).total;
 }
 
 lora_status_t token_logp(const void *logits, int64_t ldz, const int32_t *targets, const float *weights, float *logp,
@@ -282,10 +289,10 @@ lora_status_t token_logp(const void *logits, int64_t ldz, const int32_t *targets
   LossLayout L;
   lora_status_t s = check_loss_sizes(TOKEN_LOSS_OP_LOGP, T, V, ldz, 0, dt);
   if (s != LORA_OK) return s;
-  s = check_loss(TOKEN_LOSS_OP_LOGP, logits, ldz, targets, weights, logp, nullptr, T, 0, dt, nullptr, 0, nullptr, 0, ws,
+  s = check_loss(TOKEN_LOSS_OP_LOGP, logits, ldz, targets, weights, logp, nullptr, T, V, 0, dt, nullptr, 0, nullptr, 0, ws,
                  ws_bytes, &L);
   if (s != LORA_OK) return s;
-  const TokenLoss a = loss_args(logits, ldz, targets, weights, logp, nullptr, nullptr, T, V);
+  const TokenLoss a = loss_args(logits, ldz, targets, weights, logp, nullptr, nullptr, T, V, L, ws);
   hipStream_t st = (hipStream_t)hip_stream;
   Timed t(K_TOKEN_LOGP, st);
   const hipError_t e = launch_token_logp(a, dtype(dt), st);
@@ -307,11 +314,10 @@ lora_status_t policy_loss(const void *logits, int64_t ldz, const int32_t *target
   if (misaligned(ptrs)) return fail(LORA_EINVAL, "pointers must be 16-byte aligned");
   const Range ins[] = {rng(advantages, T * 4), rng(old_logp, T * 4), rng(ref_logp, T * 4)}, outs[] = {rng(loss, 4)};
   LossLayout L;
-  s = check_loss(TOKEN_LOSS_OP_POLICY, logits, ldz, targets, weights, logp, dlogits, T, 0, dt, ins, 3, outs, 1, ws, ws_bytes,
+  s = check_loss(TOKEN_LOSS_OP_POLICY, logits, ldz, targets, weights, logp, dlogits, T, V, 0, dt, ins, 3, outs, 1, ws, ws_bytes,
                  &L);
   if (s != LORA_OK) return s;
-  TokenLoss a = loss_args(logits, ldz, targets, weights, logp, dlogits, loss, T, V);
-  a.rows = (float *)((char *)ws + L.rows);
+  const TokenLoss a = loss_args(logits, ldz, targets, weights, logp, dlogits, loss, T, V, L, ws);
   const PolicyArgs p{advantages, old_logp, kl_coef != 0.0f ? ref_logp : nullptr, 1.0f - clip_lo, 1.0f + clip_hi, kl_coef};
   hipStream_t st = (hipStream_t)hip_stream;
   Timed t(K_POLICY_LOSS, st);
@@ -333,13 +339,10 @@ lora_status_t preference_loss(const void *logits, int64_t ldz, const int32_t *ta
   if (misaligned(ptrs)) return fail(LORA_EINVAL, "pointers must be 16-byte aligned");
   const Range ins[] = {rng(ref_logp, T * 4), rng(seq, (2 * npairs + 1) * 4)}, outs[] = {rng(loss, 4), rng(margins, npairs * 4)};
   LossLayout L;
-  s = check_loss(TOKEN_LOSS_OP_PREFERENCE, logits, ldz, targets, weights, logp, dlogits, T, npairs, dt, ins, 2, outs, 2, ws,
+  s = check_loss(TOKEN_LOSS_OP_PREFERENCE, logits, ldz, targets, weights, logp, dlogits, T, V, npairs, dt, ins, 2, outs, 2, ws,
                  ws_bytes, &L);
   if (s != LORA_OK) return s;
-  TokenLoss a = loss_args(logits, ldz, targets, weights, logp, dlogits, loss, T, V);
-  a.stat = (float *)((char *)ws + L.stat);
-  a.coef = (float *)((char *)ws + L.coef);
-  a.rows = (float *)((char *)ws + L.rows);
+  const TokenLoss a = loss_args(logits, ldz, targets, weights, logp, dlogits, loss, T, V, L, ws);
   const PairArgs p{ref_logp, seq, (int)npairs, beta, label_smoothing, margins};
   hipStream_t st = (hipStream_t)hip_stream;
   Timed t(K_PREFERENCE_LOSS, st);

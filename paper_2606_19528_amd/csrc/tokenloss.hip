@@ -1,12 +1,14 @@
 // tokenloss.hip -- log-probabilities of given tokens under rows of logits, and
 // the policy and preference losses over them with their gradients with
 // respect to the logits.
-//   m_t = max_j z_tj,  l_t = log sum_j exp(z_tj - m_t),
-//   logp_t = (z_t[y_t] - m_t) - l_t
-//   dz_tj = c_t ([j = y_t] - exp((z_tj - m_t) - l_t)),   c_t = w_t dL_t/dlogp_t
-// m and l are kept apart: a row whose logits are all the type's lowest value
-// has the finite m of that size, beside which l would be rounded away.
+//   m_t = max_j z_tj,  s_t = sum_j exp(z_tj - m_t),
+//   logp_t = (z_t[y_t] - m_t) - log s_t
+//   dz_tj = c_t [j = y_t] - (c_t / s_t) exp(z_tj - m_t),   c_t = w_t dL_t/dlogp_t
+// m and s are kept apart: a row whose logits are all the type's lowest value
+// has the finite m of that size, beside which log s would be rounded away.
 // Differences are taken before the scaling to base 2 for the same reason.
+// logp is held in 64 bits until it is rounded for the output: in 32 bits the rounding of
+// log s and logp would be most of the error of a margin, a difference of sums of logp.
 // Rows of weight 0 are not read; their logp is 0 and their gradient a row of zeros.
 #include "kernels.hpp"
 #include "launch.hpp"
@@ -26,22 +28,30 @@ __device__ __forceinline__ Stat stat_join(Stat a, Stat b) {
   const float m = fmaxf(a.m, b.m), r = finite_max(m);
   return {m, a.s * exp_diff(a.m, r) + b.s * exp_diff(b.m, r)};
 }
+__device__ __forceinline__ Stat wave_stat(Stat a) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) a = stat_join(a, Stat{__shfl_xor(a.m, off), __shfl_xor(a.s, off)});
+  return a;
+}
 template <int N>
-__device__ __forceinline__ void stat_add(Stat &a, const float *f) {
+__device__ __forceinline__ float max_of(const float *f) {
   float v = f[0];
 #pragma unroll
   for (int e = 1; e < N; ++e) v = fmaxf(v, f[e]);
-  const float m = fmaxf(a.m, v), r = finite_max(m);
+  return v;
+}
+template <int N>
+__device__ __forceinline__ void stat_add(Stat &a, const float *f) {
+  const float m = fmaxf(a.m, max_of<N>(f)), r = finite_max(m);
   float s = a.s * exp_diff(a.m, r);
 #pragma unroll
   for (int e = 0; e < N; ++e) s += exp_diff(f[e], r);
   a = {m, s};
 }
-
+// Joined over a workgroup of NT threads, in one order.
 template <int NT>
 __device__ __forceinline__ Stat block_stat(Stat a, Stat *red) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) a = stat_join(a, Stat{__shfl_xor(a.m, off), __shfl_xor(a.s, off)});
+  a = wave_stat(a);
   if (NT == 64) return a;
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
@@ -52,95 +62,85 @@ __device__ __forceinline__ Stat block_stat(Stat a, Stat *red) {
   return a;
 }
 
-// Vector i of a row of V logits, -inf past its end (a row's storage is whole vectors).
+// Vector i of a row of V elements with those past the row's end replaced by the
+// bits `fill` (a row's storage is whole vectors).
+__device__ __forceinline__ u32x4 cut_row(BF16, u32x4 x, int i, int V, uint32_t fill) {
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    if (i * 8 + 2 * d + 1 >= V) x[d] = (x[d] & 0xffffu) | (fill << 16);
+    if (i * 8 + 2 * d >= V) x[d] = fill | (fill << 16);
+  }
+  return x;
+}
+__device__ __forceinline__ u32x4 cut_row(F32, u32x4 x, int i, int V, uint32_t fill) {
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+    if (i * 4 + d >= V) x[d] = fill;
+  return x;
+}
+__device__ __forceinline__ uint32_t neg_inf_bits(BF16) { return 0xff80u; }
+__device__ __forceinline__ uint32_t neg_inf_bits(F32) { return 0xff800000u; }
+// A vector of logits into the statistics.
 template <typename E>
-__device__ __forceinline__ void load_logits(const u32x4 *row, int i, int V, float *f) {
-  unpack_vec(E(), row[i], f);
-  if ((i + 1) * E::VEC > V) {
+__device__ __forceinline__ void stat_vec(Stat &st, u32x4 x) {
+  float f[E::VEC];
+  unpack_vec(E(), x, f);
+  stat_add<E::VEC>(st, f);
+}
+__device__ __forceinline__ u32x4 pack_pairs(BF16, const float *f) {
+  return u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+}
+__device__ __forceinline__ u32x4 pack_pairs(F32, const float *f) { return pack_vec(F32(), f); }
+// Vector i of dz (k = -c / s), elements past the row's end included.
+template <typename E>
+__device__ __forceinline__ u32x4 dz_vec(u32x4 x, int i, float m, float k, float c, int y) {
+  float f[E::VEC];
+  unpack_vec(E(), x, f);
+#pragma unroll
+  for (int e = 0; e < E::VEC; ++e) f[e] = k * exp_diff(f[e], m);
+  const int ye = y - i * E::VEC;
+  if ((unsigned)ye < (unsigned)E::VEC) {
 #pragma unroll
     for (int e = 0; e < E::VEC; ++e)
-      if (i * E::VEC + e >= V) f[e] = -INFINITY;
+      if (e == ye) f[e] += c;
   }
-}
-
-constexpr int TL_NT = 256;
-
-// max and log of the sum of exponentials of a row, for the whole workgroup.
-template <typename E>
-__device__ __forceinline__ Stat row_stat(const u32x4 *row, int V, Stat *red) {
-  Stat a{-INFINITY, 0.0f};
-  const int nv = (V + E::VEC - 1) / E::VEC;
-  for (int i = threadIdx.x; i < nv; i += TL_NT) {
-    float f[E::VEC];
-    load_logits<E>(row, i, V, f);
-    stat_add<E::VEC>(a, f);
-  }
-  a = block_stat<TL_NT>(a, red);
-  return {a.m, logf(a.s)};
+  return pack_pairs(E(), f);
 }
 
 template <typename E>
-__device__ __forceinline__ float target_logp(const TokenLoss &a, int64_t t, Stat st) {
+__device__ __forceinline__ const u32x4 *row_ptr(const TokenLoss &a, int64_t t) {
+  return (const u32x4 *)((const typename E::T *)a.z + t * a.ld);
+}
+template <typename E>
+__device__ __forceinline__ u32x4 *dz_ptr(const TokenLoss &a, int64_t t) {
+  return (u32x4 *)((typename E::T *)a.dz + t * a.ld);
+}
+__device__ __forceinline__ float weight(const TokenLoss &a, int64_t t) { return a.w ? a.w[t] : 1.0f; }
+
+// The target's logit of row t; NaN for a target outside the vocabulary.
+template <typename E>
+__device__ __forceinline__ float target_logit(const TokenLoss &a, int64_t t) {
   const int y = a.y[t];
-  if (y < 0 || y >= a.V) return NAN;
-  return (E::to_float(((const typename E::T *)a.z)[t * a.ld + y]) - st.m) - st.s;
+  return y >= 0 && y < a.V ? E::to_float(((const typename E::T *)a.z)[t * a.ld + y]) : NAN;
 }
-
-// Row t of dz from its statistics and c.
-template <typename E>
-__device__ __forceinline__ void write_dz(const TokenLoss &a, int64_t t, Stat st, float c) {
-  const int nv = (int)(a.ld / E::VEC);
-  const u32x4 *row = (const u32x4 *)((const typename E::T *)a.z + t * a.ld);
-  u32x4 *out = (u32x4 *)((typename E::T *)a.dz + t * a.ld);
-  if (c == 0.0f) {
-    for (int i = threadIdx.x; i < nv; i += TL_NT) out[i] = zero16();
-    return;
-  }
-  const int y = a.y[t];
-  const float l2 = st.s * kLog2e;
-  for (int i = threadIdx.x; i < nv; i += TL_NT) {
-    u32x4 x = zero16();
-    if (i * E::VEC < a.V) {
-      float f[E::VEC];
-      load_logits<E>(row, i, a.V, f);
-#pragma unroll
-      for (int e = 0; e < E::VEC; ++e) {
-        const float p = __builtin_amdgcn_exp2f((f[e] - st.m) * kLog2e - l2);
-        f[e] = i * E::VEC + e >= a.V ? 0.0f : -c * p;
-        if (i * E::VEC + e == y) f[e] += c;
-      }
-      x = pack_vec(E(), f);
-    }
-    out[i] = x;
-  }
+// log s to fp32's relative precision of s itself: the hardware's base-2 logarithm,
+// corrected by what s 2^-l2 leaves of 1 (its square is below 2^-40).
+__device__ __forceinline__ double log_sum(float s) {
+  const float l2 = __builtin_amdgcn_logf(s);
+  const float e = fmaf(s, __builtin_amdgcn_exp2f(-l2), -1.0f);
+  return (double)l2 * 0.6931471805599453094 + (double)e;
 }
-
-// logp, and for a loss that comes later the row's statistics and a zero c.
-template <typename E>
-__global__ __launch_bounds__(TL_NT) void token_logp_kernel(TokenLoss a) {
-  __shared__ Stat red[TL_NT / 64];
-  const int64_t t = blockIdx.x;
-  Stat st{0.0f, 0.0f};
-  const bool live = !a.w || a.w[t] != 0.0f;
-  if (live) st = row_stat<E>((const u32x4 *)((const typename E::T *)a.z + t * a.ld), a.V, red);
-  if (threadIdx.x) return;
-  a.logp[t] = live ? target_logp<E>(a, t, st) : 0.0f;
-  if (a.stat) {
-    a.stat[2 * t] = st.m;
-    a.stat[2 * t + 1] = st.s;
-    a.coef[t] = 0.0f;
-  }
-}
+__device__ __forceinline__ double logp_of(float zy, Stat st) { return ((double)zy - (double)st.m) - log_sum(st.s); }
 
 // The policy loss of a position and its derivative with respect to logp.
-__device__ __forceinline__ void policy_terms(const PolicyArgs &p, int64_t t, float logp, float *loss, float *grad) {
-  const float adv = p.adv[t], ratio = expf(logp - p.old_logp[t]);
-  // (an unordered comparison takes the bound's side only when the bound is less: NaN stays NaN)
+__device__ __forceinline__ void policy_terms(const PolicyArgs &p, int64_t t, double logp, float *loss, float *grad) {
+  const float adv = p.adv[t], ratio = expf((float)(logp - (double)p.old_logp[t]));
+  // (an unordered comparison does not clip: NaN stays NaN)
   const float held = fminf(fmaxf(ratio, p.lo), p.hi) * adv, free = ratio * adv;
   const bool clipped = held < free;
   float l = clipped ? -held : -free, g = clipped ? 0.0f : -free;
   if (p.ref) {
-    const float d = p.ref[t] - logp, x = expm1f(d);
+    const float d = (float)((double)p.ref[t] - logp), x = expm1f(d);
     l += p.kl * (x - d);
     g -= p.kl * x;
   }
@@ -148,39 +148,57 @@ __device__ __forceinline__ void policy_terms(const PolicyArgs &p, int64_t t, flo
   *grad = g;
 }
 
+// ---- statistics of rows, or of parts of rows -------------------------------------
+constexpr int TL_NT = 256;
+
+// Part p of a row: vectors [p, p + 1) * part_vecs.
 template <typename E>
-__global__ __launch_bounds__(TL_NT) void policy_kernel(TokenLoss a, PolicyArgs p) {
+__global__ __launch_bounds__(TL_NT) void token_stat_kernel(TokenLoss a, Stat *stat) {
   __shared__ Stat red[TL_NT / 64];
-  const int64_t t = blockIdx.x;
-  const float w = a.w ? a.w[t] : 1.0f;
-  Stat st{0.0f, 0.0f};
-  float c = 0.0f;
-  if (w != 0.0f) {
-    st = row_stat<E>((const u32x4 *)((const typename E::T *)a.z + t * a.ld), a.V, red);
-    const float logp = target_logp<E>(a, t, st);
-    float l, g;
-    policy_terms(p, t, logp, &l, &g);
-    c = w * g;
-    if (threadIdx.x == 0) {
-      a.logp[t] = logp;
-      a.rows[t] = w * l;
-    }
-  } else if (threadIdx.x == 0) {
-    a.logp[t] = 0.0f;
-    a.rows[t] = 0.0f;
+  const int64_t t = blockIdx.x / a.parts;
+  const int p = blockIdx.x % a.parts;
+  if (a.coef && p == 0 && threadIdx.x == 0) a.coef[t] = 0.0f;
+  if (weight(a, t) == 0.0f) {
+    if (!stat && threadIdx.x == 0) a.logp[t] = 0.0f;
+    return;
   }
-  if (a.dz) {
-    __syncthreads();  // dz may be z: every thread has the target's logit before its row changes
-    write_dz<E>(a, t, st, c);
+  const u32x4 *row = row_ptr<E>(a, t);
+  const int nv = (a.V + E::VEC - 1) / E::VEC, end = min(nv, (p + 1) * a.part_vecs);
+  Stat st{-INFINITY, 0.0f};
+  for (int i = p * a.part_vecs + threadIdx.x; i < end; i += TL_NT) {
+    u32x4 x = row[i];
+    if ((i + 1) * E::VEC > a.V) x = cut_row(E(), x, i, a.V, neg_inf_bits(E()));
+    stat_vec<E>(st, x);
   }
+  st = block_stat<TL_NT>(st, red);
+  if (threadIdx.x) return;
+  if (stat) stat[blockIdx.x] = st;
+  else a.logp[t] = (float)logp_of(target_logit<E>(a, t), st);
+  // (a later launch may put dz in the logits' place, one part before another)
+  if (stat && p == 0) a.ztgt[t] = target_logit<E>(a, t);
 }
 
-template <typename E>
-__global__ __launch_bounds__(TL_NT) void token_dz_kernel(TokenLoss a) {
-  const int64_t t = blockIdx.x;
-  write_dz<E>(a, t, Stat{a.stat[2 * t], a.stat[2 * t + 1]}, a.coef[t]);
+// A row's statistics from those of its parts (at most 64): in every lane of a
+// wave, or by one thread.
+__device__ __forceinline__ Stat joined_stat(const TokenLoss &a, const Stat *stat, int64_t t) {
+  const int lane = threadIdx.x & 63;
+  return wave_stat(lane < a.parts ? stat[t * a.parts + lane] : Stat{-INFINITY, 0.0f});
+}
+__device__ __forceinline__ Stat thread_stat(const TokenLoss &a, const Stat *stat, int64_t t) {
+  Stat st = stat[t * a.parts];
+  for (int p = 1; p < a.parts; ++p) st = stat_join(st, stat[t * a.parts + p]);
+  return st;
 }
 
+__global__ __launch_bounds__(TL_NT) void logp_join_kernel(TokenLoss a, const Stat *stat) {
+  const int64_t t = (int64_t)blockIdx.x * (TL_NT / 64) + (threadIdx.x >> 6);
+  if (t >= a.T) return;
+  float logp = 0.0f;
+  if (weight(a, t) != 0.0f) logp = (float)logp_of(a.ztgt[t], joined_stat(a, stat, t));
+  if ((threadIdx.x & 63) == 0) a.logp[t] = logp;
+}
+
+// ---- sums over positions -----------------------------------------------------------
 // Sum over a workgroup of NT threads in a fixed order.
 template <int NT>
 __device__ __forceinline__ double block_sum(double x, double *red) {
@@ -194,69 +212,336 @@ __device__ __forceinline__ double block_sum(double x, double *red) {
   for (int w = 1; w < NT / 64; ++w) x += red[w];
   return x;
 }
+// loss = scale * sum of rows[0 .. n), by one workgroup.
+template <int NT>
+__device__ __forceinline__ void sum_rows(const float *rows, int64_t n, double scale, float *loss, double *red) {
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < n; i += NT) s += rows[i];
+  s = block_sum<NT>(s, red);
+  if (threadIdx.x == 0) loss[0] = (float)(s * scale);
+}
 
 constexpr int LS_NT = 1024;
-// loss = scale * sum of rows[0 .. n), by one workgroup.
 __global__ __launch_bounds__(LS_NT) void loss_sum_kernel(const float *rows, int n, double scale, float *loss) {
   __shared__ double red[LS_NT / 64];
-  double s = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += LS_NT) s += rows[i];
-  s = block_sum<LS_NT>(s, red);
-  if (threadIdx.x == 0) loss[0] = (float)(s * scale);
+  sum_rows<LS_NT>(rows, n, scale, loss, red);
+}
+
+// ---- dz in a launch after the statistics ---------------------------------------------
+// Part p of row t of dz from its maximum m, sum s and c, by a workgroup.
+template <typename E>
+__device__ __forceinline__ void write_dz(const TokenLoss &a, int64_t t, int p, Stat st, float c, int y) {
+  const int nv = (int)(a.ld / E::VEC), nz = (a.V + E::VEC - 1) / E::VEC;
+  const int end = p + 1 == a.parts ? nv : min(nv, (p + 1) * a.part_vecs);
+  const u32x4 *row = row_ptr<E>(a, t);
+  u32x4 *out = dz_ptr<E>(a, t);
+  int i = p * a.part_vecs + threadIdx.x;
+  if (c != 0.0f) {
+    const float k = -c / st.s;
+    for (; i < end && i < nz; i += TL_NT) {
+      u32x4 d = dz_vec<E>(row[i], i, st.m, k, c, y);
+      if ((i + 1) * E::VEC > a.V) d = cut_row(E(), d, i, a.V, 0u);
+      out[i] = d;
+    }
+  }
+  for (; i < end; i += TL_NT) out[i] = zero16();
+}
+
+// Policy loss of few rows, after token_stat_kernel: each workgroup writes one
+// part of a row of dz; the last one sums the loss, a thread a row.
+template <typename E>
+__global__ __launch_bounds__(TL_NT) void policy_parts_kernel(TokenLoss a, PolicyArgs p, const Stat *stat) {
+  __shared__ double red[TL_NT / 64];
+  if (blockIdx.x == gridDim.x - 1) {
+    double sum = 0.0;
+    for (int64_t t = threadIdx.x; t < a.T; t += TL_NT) {
+      const float w = weight(a, t);
+      double logp = 0.0;
+      if (w != 0.0f) {
+        float l, g;
+        logp = logp_of(a.ztgt[t], thread_stat(a, stat, t));
+        policy_terms(p, t, logp, &l, &g);
+        sum += w * l;
+      }
+      a.logp[t] = (float)logp;
+    }
+    sum = block_sum<TL_NT>(sum, red);
+    if (threadIdx.x == 0) a.loss[0] = (float)sum;
+    return;
+  }
+  const int64_t t = blockIdx.x / a.parts;
+  const float w = weight(a, t);
+  Stat st{0.0f, 1.0f};
+  float c = 0.0f;
+  int y = -1;
+  if (w != 0.0f) {
+    float l, g;
+    st = joined_stat(a, stat, t);
+    policy_terms(p, t, logp_of(a.ztgt[t], st), &l, &g);
+    c = w * g;
+    y = a.y[t];
+  }
+  write_dz<E>(a, t, blockIdx.x % a.parts, st, c, y);
 }
 
 // softplus(x) = log(1 + exp x)
 __device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.0f) + log1pf(expf(-fabsf(x))); }
 
-// One workgroup a pair: margin, loss and the rows' c.
-__global__ __launch_bounds__(TL_NT) void pair_kernel(TokenLoss a, PairArgs p) {
-  __shared__ double red[TL_NT / 64];
+// One workgroup a pair, a thread a row: logp and statistics of its rows, margin,
+// loss and the rows' c.  The first and the last pair take the rows outside all of
+// them along (their c is 0: token_stat_kernel).
+constexpr int PR_NT = 512;
+__global__ __launch_bounds__(PR_NT) void pair_kernel(TokenLoss a, PairArgs p, const Stat *stat, Stat *rowstat) {
+  __shared__ double red[PR_NT / 64];
   const int i = blockIdx.x;
   const int b0 = min(max(p.seq[2 * i], 0), a.T), b1 = min(max(p.seq[2 * i + 1], b0), a.T), b2 = min(max(p.seq[2 * i + 2], b1), a.T);
+  const int64_t first = i == 0 ? 0 : b0, last = i == p.pairs - 1 ? a.T : b2;
   double d = 0.0;
-  for (int t = b0 + threadIdx.x; t < b2; t += TL_NT) {
-    const float w = a.w ? a.w[t] : 1.0f;
-    if (w == 0.0f) continue;
-    const double x = (double)w * ((double)a.logp[t] - (p.ref ? (double)p.ref[t] : 0.0));
-    d += t < b1 ? x : -x;
+  for (int64_t t = first + threadIdx.x; t < last; t += PR_NT) {
+    const float w = weight(a, t);
+    double logp = 0.0;
+    if (w != 0.0f) {
+      const Stat st = thread_stat(a, stat, t);
+      logp = logp_of(a.ztgt[t], st);
+      rowstat[t] = st;
+      if (t >= b0 && t < b2) {
+        const double x = (double)w * (logp - (p.ref ? (double)p.ref[t] : 0.0));
+        d += t < b1 ? x : -x;
+      }
+    }
+    a.logp[t] = (float)logp;
   }
-  const float margin = p.beta * (float)block_sum<TL_NT>(d, red);
-  const float s = p.smooth, up = 1.0f / (1.0f + expf(-margin)), down = 1.0f / (1.0f + expf(margin));
+  const double margin = (double)p.beta * block_sum<PR_NT>(d, red);
+  const float mg = (float)margin, s = p.smooth, up = 1.0f / (1.0f + expf(-mg)), down = 1.0f / (1.0f + expf(mg));
   const float g = p.beta / p.pairs * (s * up - (1.0f - s) * down);
-  for (int t = b0 + threadIdx.x; t < b2; t += TL_NT) {
-    const float w = a.w ? a.w[t] : 1.0f;
-    a.coef[t] = w == 0.0f ? 0.0f : w * (t < b1 ? g : -g);
+  for (int64_t t = b0 + threadIdx.x; t < b2; t += PR_NT) {
+    const float w = weight(a, t);
+    if (w != 0.0f) a.coef[t] = w * (t < b1 ? g : -g);
   }
   if (threadIdx.x == 0) {
-    p.margins[i] = margin;
-    float l = (1.0f - s) * softplus(-margin);
-    if (s != 0.0f) l += s * softplus(margin);
+    p.margins[i] = mg;
+    float l = (1.0f - s) * softplus(-mg);
+    if (s != 0.0f) l += s * softplus(mg);
     a.rows[i] = l;
   }
 }
 
+// dz, and by the last workgroup the loss.
+template <typename E>
+__global__ __launch_bounds__(TL_NT) void pair_dz_kernel(TokenLoss a, const Stat *rowstat, int pairs) {
+  __shared__ double red[TL_NT / 64];
+  if (blockIdx.x == gridDim.x - 1) {
+    sum_rows<TL_NT>(a.rows, pairs, 1.0 / pairs, a.loss, red);
+    return;
+  }
+  const int64_t t = blockIdx.x / a.parts;
+  const float c = a.coef[t];
+  write_dz<E>(a, t, blockIdx.x % a.parts, c != 0.0f ? rowstat[t] : Stat{0.0f, 1.0f}, c, a.y[t]);
+}
+
+// ---- policy loss of many rows: a row stays in registers -------------------------------
+// A workgroup of NT threads holds a row of up to NT NV vectors, so the logits
+// are read once.  A row's vectors are replaced by the next row's as they are
+// turned into dz, which keeps loads and stores in flight while the exponentials
+// are computed.  Rows are addressed as buffers of their own length: what a
+// thread loads past the end is 0, what it stores there is dropped, and the
+// vectors need one address register.
+template <typename E, int NT, int NV>
+__global__ __launch_bounds__(NT, 4) void policy_rows_kernel(TokenLoss a, PolicyArgs p) {
+  __shared__ Stat red[NT / 64 < 1 ? 1 : NT / 64];
+  const int nz = (a.V + E::VEC - 1) / E::VEC, nv = (int)(a.ld / E::VEC);
+  const int tid = threadIdx.x, off = tid * 16;
+  constexpr int LAG = NV < 5 ? NV : 5;
+  constexpr int SPAN = NT * E::VEC;  // elements of one vector of every thread
+  u32x4 x[NV];
+  auto buffer = [&](const void *q, int vecs) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(q), 0, vecs * 16, 0x00020000);
+  };
+  // The next row from t on of this workgroup with a weight, the others' dz cleared.
+  auto next_row = [&](int64_t t) {
+    for (; t < a.T && weight(a, t) == 0.0f; t += gridDim.x) {
+      if (a.dz) {
+        u32x4 *out = dz_ptr<E>(a, t);
+        for (int i = tid; i < nv; i += NT) out[i] = zero16();
+      }
+      if (tid == 0) {
+        a.logp[t] = 0.0f;
+        a.rows[t] = 0.0f;
+      }
+    }
+    return t;
+  };
+  int64_t t = next_row(blockIdx.x);
+  if (t >= a.T) return;
+  auto rs = buffer(row_ptr<E>(a, t), nz);
+#pragma unroll
+  for (int v = 0; v < NV; ++v) x[v] = __builtin_amdgcn_raw_buffer_load_b128(rs, off, v * NT * 16, 0);
+  Stat st{-INFINITY, 0.0f};
+  int V = a.V;
+  auto take = [&](int v) {  // vector v into the row's statistics
+    if (v * SPAN < V) {
+      if ((v + 1) * SPAN > V) x[v] = cut_row(E(), x[v], v * NT + tid, V, neg_inf_bits(E()));
+      stat_vec<E>(st, x[v]);
+    }
+    // (the vector stays packed: without this the compiler keeps its elements for dz, and spills)
+    asm volatile("" : "+v"(x[v]));
+  };
+#pragma unroll
+  for (int v = 0; v < NV; ++v) take(v);
+  while (t < a.T) {
+    asm volatile("" : "+s"(V));  // (what depends on V is recomputed for each row, not kept in registers)
+    st = block_stat<NT>(st, red);
+    const double logp = logp_of(target_logit<E>(a, t), st);
+    float l, g;
+    policy_terms(p, t, logp, &l, &g);
+    const float w = weight(a, t), c = w * g;
+    if (tid == 0) {
+      a.logp[t] = (float)logp;
+      a.rows[t] = w * l;
+    }
+    const int64_t tn = next_row(t + gridDim.x);
+    rs = buffer(row_ptr<E>(a, tn < a.T ? tn : t), tn < a.T ? nz : 0);
+    const float m = st.m, k = -c / st.s;
+    const int y = a.y[t];
+    st = Stat{-INFINITY, 0.0f};
+    if (NT > 64) __syncthreads();  // dz may be z: the target's logit has been read by every wave
+    const auto os = buffer(a.dz ? dz_ptr<E>(a, t) : nullptr, a.dz ? nv : 0);
+#pragma unroll
+    for (int v = 0; v < NV + LAG; ++v) {
+      if (v < NV) {
+        u32x4 d = zero16();
+        if (a.dz && c != 0.0f && v * SPAN < V) {
+          d = dz_vec<E>(x[v], v * NT + tid, m, k, c, y);
+          if ((v + 1) * SPAN > V) d = cut_row(E(), d, v * NT + tid, V, 0u);
+        }
+        __builtin_amdgcn_raw_buffer_store_b128(d, os, off, v * NT * 16, 0);
+        x[v] = __builtin_amdgcn_raw_buffer_load_b128(rs, off, v * NT * 16, 0);
+      }
+      if (v >= LAG) take(v - LAG);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (a.dz)
+      for (int i = NV * NT + tid; i < nv; i += NT) dz_ptr<E>(a, t)[i] = zero16();
+    t = tn;
+  }
+}
+
+// The same for rows that no workgroup holds: read twice.
+constexpr int PL_NT = 1024;
+template <typename E>
+__global__ __launch_bounds__(PL_NT) void policy_long_kernel(TokenLoss a, PolicyArgs p) {
+  __shared__ Stat red[PL_NT / 64];
+  const int64_t t = blockIdx.x;
+  const int nv = (int)(a.ld / E::VEC), nz = (a.V + E::VEC - 1) / E::VEC;
+  const float w = weight(a, t);
+  Stat st{-INFINITY, 0.0f};
+  float c = 0.0f, l = 0.0f;
+  double logp = 0.0;
+  if (w != 0.0f) {
+    const u32x4 *row = row_ptr<E>(a, t);
+    for (int i = threadIdx.x; i < nz; i += PL_NT) {
+      u32x4 x = row[i];
+      if ((i + 1) * E::VEC > a.V) x = cut_row(E(), x, i, a.V, neg_inf_bits(E()));
+      stat_vec<E>(st, x);
+    }
+    st = block_stat<PL_NT>(st, red);
+    float g;
+    logp = logp_of(target_logit<E>(a, t), st);
+    policy_terms(p, t, logp, &l, &g);
+    c = w * g;
+    l *= w;
+  }
+  if (threadIdx.x == 0) {
+    a.logp[t] = (float)logp;
+    a.rows[t] = l;
+  }
+  if (!a.dz) return;
+  __syncthreads();  // dz may be z: the target's logit has been read by every wave
+  u32x4 *out = dz_ptr<E>(a, t);
+  int i = threadIdx.x;
+  if (c != 0.0f) {
+    const u32x4 *row = row_ptr<E>(a, t);
+    const float k = -c / st.s;
+    const int y = a.y[t];
+    for (; i < nz; i += PL_NT) {
+      u32x4 d = dz_vec<E>(row[i], i, st.m, k, c, y);
+      if ((i + 1) * E::VEC > a.V) d = cut_row(E(), d, i, a.V, 0u);
+      out[i] = d;
+    }
+  }
+  for (; i < nv; i += PL_NT) out[i] = zero16();
+}
+
+// Parts of a row in the launches that take few rows: enough for about 8192
+// workgroups, none under 8 KB, at most a wave's lanes.
+LossPlan loss_plan(int64_t T, int64_t V, int64_t ld, Dtype d) {
+  const int64_t vec = d == DT_BF16 ? 8 : 4, nz = (V + vec - 1) / vec;
+  LossPlan p{};
+  const int64_t most = nz / 512, want = (8192 + T - 1) / T;
+  p.parts = (int)(most < 1 ? 1 : most < want ? most : want);
+  if (p.parts > 64) p.parts = 64;
+  p.part_vecs = (int)((nz + p.parts - 1) / p.parts);
+  p.parts = (int)((nz + p.part_vecs - 1) / p.part_vecs);
+  return p;
+}
+
 hipError_t launch_token_logp(const TokenLoss &a, Dtype d, hipStream_t st) {
-  if (d == DT_BF16) hipLaunchKernelGGL(token_logp_kernel<BF16>, dim3(a.T), dim3(TL_NT), 0, st, a);
-  else hipLaunchKernelGGL(token_logp_kernel<F32>, dim3(a.T), dim3(TL_NT), 0, st, a);
+  Stat *stat = a.parts > 1 ? (Stat *)a.stat : nullptr;
+  const dim3 grid((unsigned)((int64_t)a.T * a.parts)), join((a.T + TL_NT / 64 - 1) / (TL_NT / 64));
+  if (d == DT_BF16) {
+    hipLaunchKernelGGL(token_stat_kernel<BF16>, grid, dim3(TL_NT), 0, st, a, stat);
+  } else {
+    hipLaunchKernelGGL(token_stat_kernel<F32>, grid, dim3(TL_NT), 0, st, a, stat);
+  }
+  if (stat) hipLaunchKernelGGL(logp_join_kernel, join, dim3(TL_NT), 0, st, a, stat);
   return hipGetLastError();
+}
+
+template <typename E, int NT, int NV>
+static void policy_rows(const TokenLoss &a, const PolicyArgs &p, int per_cu, hipStream_t st) {
+  const int grid = a.T < 256 * per_cu ? a.T : 256 * per_cu;
+  hipLaunchKernelGGL((policy_rows_kernel<E, NT, NV>), dim3(grid), dim3(NT), 0, st, a, p);
+}
+
+constexpr int POLICY_ROWS = 768;
+template <typename E>
+static void policy_launches(const TokenLoss &a, const PolicyArgs &p, hipStream_t st) {
+  if (a.T < POLICY_ROWS && a.parts > 1) {
+    Stat *stat = (Stat *)a.stat;
+    hipLaunchKernelGGL(token_stat_kernel<E>, dim3((unsigned)((int64_t)a.T * a.parts)), dim3(TL_NT), 0, st, a, stat);
+    hipLaunchKernelGGL(policy_parts_kernel<E>, dim3((unsigned)(a.dz ? (int64_t)a.T * a.parts + 1 : 1)), dim3(TL_NT), 0, st, a,
+                       p, stat);
+    return;
+  }
+  const int nz = (a.V + E::VEC - 1) / E::VEC;
+  if (nz <= 64 * 8) policy_rows<E, 64, 8>(a, p, 16, st);
+  else if (nz <= 256 * 8) policy_rows<E, 256, 8>(a, p, 4, st);
+  else if (nz <= 256 * 16) policy_rows<E, 256, 16>(a, p, 4, st);
+  else if (nz <= 1024 * 8) policy_rows<E, 1024, 8>(a, p, 1, st);
+  else if (nz <= 1024 * 16) policy_rows<E, 1024, 16>(a, p, 1, st);
+  else if (nz <= 1024 * 20) policy_rows<E, 1024, 20>(a, p, 1, st);
+  else hipLaunchKernelGGL(policy_long_kernel<E>, dim3(a.T), dim3(PL_NT), 0, st, a, p);
+  hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(LS_NT), 0, st, a.rows, a.T, 1.0, a.loss);
 }
 
 hipError_t launch_policy_loss(const TokenLoss &a, const PolicyArgs &p, Dtype d, hipStream_t st) {
-  if (d == DT_BF16) hipLaunchKernelGGL(policy_kernel<BF16>, dim3(a.T), dim3(TL_NT), 0, st, a, p);
-  else hipLaunchKernelGGL(policy_kernel<F32>, dim3(a.T), dim3(TL_NT), 0, st, a, p);
-  hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(LS_NT), 0, st, a.rows, a.T, 1.0, a.loss);
+  if (d == DT_BF16) policy_launches<BF16>(a, p, st);
+  else policy_launches<F32>(a, p, st);
   return hipGetLastError();
 }
 
+template <typename E>
+static void pair_launches(const TokenLoss &a, const PairArgs &p, hipStream_t st) {
+  Stat *stat = (Stat *)a.stat, *rowstat = stat + (int64_t)a.T * a.parts;
+  const dim3 grid((unsigned)((int64_t)a.T * a.parts));
+  hipLaunchKernelGGL(token_stat_kernel<E>, grid, dim3(TL_NT), 0, st, a, stat);
+  hipLaunchKernelGGL(pair_kernel, dim3(p.pairs), dim3(PR_NT), 0, st, a, p, stat, rowstat);
+  hipLaunchKernelGGL(pair_dz_kernel<E>, dim3(a.dz ? grid.x + 1 : 1), dim3(TL_NT), 0, st, a, rowstat, p.pairs);
+}
+
 hipError_t launch_preference_loss(const TokenLoss &a, const PairArgs &p, Dtype d, hipStream_t st) {
-  hipError_t e = launch_token_logp(a, d, st);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(pair_kernel, dim3(p.pairs), dim3(TL_NT), 0, st, a, p);
-  hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(LS_NT), 0, st, a.rows, p.pairs, 1.0 / p.pairs, a.loss);
-  if (a.dz) {
-    if (d == DT_BF16) hipLaunchKernelGGL(token_dz_kernel<BF16>, dim3(a.T), dim3(TL_NT), 0, st, a);
-    else hipLaunchKernelGGL(token_dz_kernel<F32>, dim3(a.T), dim3(TL_NT), 0, st, a);
-  }
+  if (d == DT_BF16) pair_launches<BF16>(a, p, st);
+  else pair_launches<F32>(a, p, st);
   return hipGetLastError();
 }
 
