@@ -228,8 +228,14 @@ __global__ __launch_bounds__(LS_NT) void loss_sum_kernel(const float *rows, int 
 }
 
 // ---- dz in a launch after the statistics ---------------------------------------------
-// Part p of row t of dz from its maximum m, sum s and c, by a workgroup.
-template <typename E>
+// Part p of row t of dz from its maximum m, sum s and c, by a workgroup.  NTS:
+// stores that pass the last-level cache by.
+template <bool NTS>
+__device__ __forceinline__ void put_dz(u32x4 d, u32x4 *out) {
+  if (NTS) __builtin_nontemporal_store(d, out);
+  else *out = d;
+}
+template <typename E, bool NTS>
 __device__ __forceinline__ void write_dz(const TokenLoss &a, int64_t t, int p, Stat st, float c, int y) {
   const int nv = (int)(a.ld / E::VEC), nz = (a.V + E::VEC - 1) / E::VEC;
   const int end = p + 1 == a.parts ? nv : min(nv, (p + 1) * a.part_vecs);
@@ -241,10 +247,10 @@ __device__ __forceinline__ void write_dz(const TokenLoss &a, int64_t t, int p, S
     for (; i < end && i < nz; i += TL_NT) {
       u32x4 d = dz_vec<E>(row[i], i, st.m, k, c, y);
       if ((i + 1) * E::VEC > a.V) d = cut_row(E(), d, i, a.V, 0u);
-      out[i] = d;
+      put_dz<NTS>(d, out + i);
     }
   }
-  for (; i < end; i += TL_NT) out[i] = zero16();
+  for (; i < end; i += TL_NT) put_dz<NTS>(zero16(), out + i);
 }
 
 // Policy loss of few rows, after token_stat_kernel: each workgroup writes one
@@ -281,7 +287,7 @@ __global__ __launch_bounds__(TL_NT) void policy_parts_kernel(TokenLoss a, Policy
     c = w * g;
     y = a.y[t];
   }
-  write_dz<E>(a, t, blockIdx.x % a.parts, st, c, y);
+  write_dz<E, false>(a, t, blockIdx.x % a.parts, st, c, y);
 }
 
 // softplus(x) = log(1 + exp x)
@@ -326,17 +332,19 @@ __global__ __launch_bounds__(PR_NT) void pair_kernel(TokenLoss a, PairArgs p, co
   }
 }
 
-// dz, and by the last workgroup the loss.
-template <typename E>
+// dz, and by the last workgroup the loss.  The rows go backwards: the last ones
+// that token_stat_kernel read may still be in the last-level cache.
+template <typename E, bool NTS>
 __global__ __launch_bounds__(TL_NT) void pair_dz_kernel(TokenLoss a, const Stat *rowstat, int pairs) {
   __shared__ double red[TL_NT / 64];
   if (blockIdx.x == gridDim.x - 1) {
     sum_rows<TL_NT>(a.rows, pairs, 1.0 / pairs, a.loss, red);
     return;
   }
-  const int64_t t = blockIdx.x / a.parts;
+  const unsigned b = gridDim.x - 2 - blockIdx.x;
+  const int64_t t = b / a.parts;
   const float c = a.coef[t];
-  write_dz<E>(a, t, blockIdx.x % a.parts, c != 0.0f ? rowstat[t] : Stat{0.0f, 1.0f}, c, a.y[t]);
+  write_dz<E, NTS>(a, t, b % a.parts, c != 0.0f ? rowstat[t] : Stat{0.0f, 1.0f}, c, a.y[t]);
 }
 
 // ---- policy loss of many rows: a row stays in registers -------------------------------
@@ -345,7 +353,8 @@ __global__ __launch_bounds__(TL_NT) void pair_dz_kernel(TokenLoss a, const Stat 
 // turned into dz, which keeps loads and stores in flight while the exponentials
 // are computed.  Rows are addressed as buffers of their own length: what a
 // thread loads past the end is 0, what it stores there is dropped, and the
-// vectors need one address register.
+// vectors need one address register.  What a longer row has beyond is read
+// twice; with one row a CU on the way, the second read comes from the last-level cache.
 template <typename E, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void policy_rows_kernel(TokenLoss a, PolicyArgs p) {
   __shared__ Stat red[NT / 64 < 1 ? 1 : NT / 64];
@@ -390,6 +399,13 @@ __global__ __launch_bounds__(NT, 4) void policy_rows_kernel(TokenLoss a, PolicyA
   for (int v = 0; v < NV; ++v) take(v);
   while (t < a.T) {
     asm volatile("" : "+s"(V));  // (what depends on V is recomputed for each row, not kept in registers)
+    const u32x4 *zrow = row_ptr<E>(a, t);
+#pragma unroll 4
+    for (int i = NV * NT + tid; i < nz; i += NT) {
+      u32x4 r = zrow[i];
+      if ((i + 1) * E::VEC > V) r = cut_row(E(), r, i, V, neg_inf_bits(E()));
+      stat_vec<E>(st, r);
+    }
     st = block_stat<NT>(st, red);
     const double logp = logp_of(target_logit<E>(a, t), st);
     float l, g;
@@ -420,56 +436,21 @@ __global__ __launch_bounds__(NT, 4) void policy_rows_kernel(TokenLoss a, PolicyA
       if (v >= LAG) take(v - LAG);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (a.dz)
-      for (int i = NV * NT + tid; i < nv; i += NT) dz_ptr<E>(a, t)[i] = zero16();
+    if (a.dz) {
+      u32x4 *out = dz_ptr<E>(a, t);
+      int i = NV * NT + tid;
+      if (c != 0.0f) {
+#pragma unroll 4
+        for (; i < nz; i += NT) {
+          u32x4 d = dz_vec<E>(zrow[i], i, m, k, c, y);
+          if ((i + 1) * E::VEC > V) d = cut_row(E(), d, i, V, 0u);
+          out[i] = d;
+        }
+      }
+      for (; i < nv; i += NT) out[i] = zero16();
+    }
     t = tn;
   }
-}
-
-// The same for rows that no workgroup holds: read twice.
-constexpr int PL_NT = 1024;
-template <typename E>
-__global__ __launch_bounds__(PL_NT) void policy_long_kernel(TokenLoss a, PolicyArgs p) {
-  __shared__ Stat red[PL_NT / 64];
-  const int64_t t = blockIdx.x;
-  const int nv = (int)(a.ld / E::VEC), nz = (a.V + E::VEC - 1) / E::VEC;
-  const float w = weight(a, t);
-  Stat st{-INFINITY, 0.0f};
-  float c = 0.0f, l = 0.0f;
-  double logp = 0.0;
-  if (w != 0.0f) {
-    const u32x4 *row = row_ptr<E>(a, t);
-    for (int i = threadIdx.x; i < nz; i += PL_NT) {
-      u32x4 x = row[i];
-      if ((i + 1) * E::VEC > a.V) x = cut_row(E(), x, i, a.V, neg_inf_bits(E()));
-      stat_vec<E>(st, x);
-    }
-    st = block_stat<PL_NT>(st, red);
-    float g;
-    logp = logp_of(target_logit<E>(a, t), st);
-    policy_terms(p, t, logp, &l, &g);
-    c = w * g;
-    l *= w;
-  }
-  if (threadIdx.x == 0) {
-    a.logp[t] = (float)logp;
-    a.rows[t] = l;
-  }
-  if (!a.dz) return;
-  __syncthreads();  // dz may be z: the target's logit has been read by every wave
-  u32x4 *out = dz_ptr<E>(a, t);
-  int i = threadIdx.x;
-  if (c != 0.0f) {
-    const u32x4 *row = row_ptr<E>(a, t);
-    const float k = -c / st.s;
-    const int y = a.y[t];
-    for (; i < nz; i += PL_NT) {
-      u32x4 d = dz_vec<E>(row[i], i, st.m, k, c, y);
-      if ((i + 1) * E::VEC > a.V) d = cut_row(E(), d, i, a.V, 0u);
-      out[i] = d;
-    }
-  }
-  for (; i < nv; i += PL_NT) out[i] = zero16();
 }
 
 // Parts of a row in the launches that take few rows: enough for about 8192
@@ -503,7 +484,7 @@ static void policy_rows(const TokenLoss &a, const PolicyArgs &p, int per_cu, hip
   hipLaunchKernelGGL((policy_rows_kernel<E, NT, NV>), dim3(grid), dim3(NT), 0, st, a, p);
 }
 
-constexpr int POLICY_ROWS = 768;
+constexpr int POLICY_ROWS = 192;
 template <typename E>
 static void policy_launches(const TokenLoss &a, const PolicyArgs &p, hipStream_t st) {
   if (a.T < POLICY_ROWS && a.parts > 1) {
@@ -519,8 +500,7 @@ static void policy_launches(const TokenLoss &a, const PolicyArgs &p, hipStream_t
   else if (nz <= 256 * 16) policy_rows<E, 256, 16>(a, p, 4, st);
   else if (nz <= 1024 * 8) policy_rows<E, 1024, 8>(a, p, 1, st);
   else if (nz <= 1024 * 16) policy_rows<E, 1024, 16>(a, p, 1, st);
-  else if (nz <= 1024 * 20) policy_rows<E, 1024, 20>(a, p, 1, st);
-  else hipLaunchKernelGGL(policy_long_kernel<E>, dim3(a.T), dim3(PL_NT), 0, st, a, p);
+  else policy_rows<E, 1024, 20>(a, p, 1, st);
   hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(LS_NT), 0, st, a.rows, a.T, 1.0, a.loss);
 }
 
@@ -536,7 +516,14 @@ static void pair_launches(const TokenLoss &a, const PairArgs &p, hipStream_t st)
   const dim3 grid((unsigned)((int64_t)a.T * a.parts));
   hipLaunchKernelGGL(token_stat_kernel<E>, grid, dim3(TL_NT), 0, st, a, stat);
   hipLaunchKernelGGL(pair_kernel, dim3(p.pairs), dim3(PR_NT), 0, st, a, p, stat, rowstat);
-  hipLaunchKernelGGL(pair_dz_kernel<E>, dim3(a.dz ? grid.x + 1 : 1), dim3(TL_NT), 0, st, a, rowstat, p.pairs);
+  // Logits that outgrow the last-level cache (256 MB): dz is kept out of it, for the second
+  // read of the logits (2048 x 151936 bf16, 622 MB: statistics and dz 60 + 185 us, else
+  // 96 + 178).  Smaller ones: dz stays there for the product that reads it next.
+  const dim3 dzgrid(a.dz ? grid.x + 1 : 1);
+  if ((int64_t)a.T * a.ld * (16 / E::VEC) > (int64_t)256 << 20)
+    hipLaunchKernelGGL((pair_dz_kernel<E, true>), dzgrid, dim3(TL_NT), 0, st, a, rowstat, p.pairs);
+  else
+    hipLaunchKernelGGL((pair_dz_kernel<E, false>), dzgrid, dim3(TL_NT), 0, st, a, rowstat, p.pairs);
 }
 
 hipError_t launch_preference_loss(const TokenLoss &a, const PairArgs &p, Dtype d, hipStream_t st) {

@@ -196,7 +196,8 @@ def _stream(stream):
     import torch
 
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # (the current stream's handle; building torch's Stream object for it takes 3 us)
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -475,15 +476,31 @@ def lora_ckpt_backward(nodes, g_n, dx0, host_stash, ws, compute_stream=None, cop
 
 
 # --- embedding, losses over the targets, clipping ------------------------------------
-def _want(t, name: str, dtype, shape=None):
-    """Refuses a tensor of another type, shape or place than the call takes."""
+def _arg(t, name: str, dtype, shape):
+    """Address of a tensor argument; refuses one of another type, shape, layout or
+    place than the call takes."""
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be on the GPU")
-    return t
+    if not t.is_contiguous():
+        raise ValueError("tensors must be contiguous (row-major, no padding)")
+    return t.data_ptr()
+
+
+def _opt(t, name: str, dtype, shape):
+    return None if t is None else _arg(t, name, dtype, shape)
+
+
+def _ws_for(ws, query, like, stream):
+    """(address, bytes) of the caller's workspace, or of a temporary one of the size
+    that `query` reports, and the tensor itself."""
+    if ws is None:
+        ws, nbytes = _ws(None, query(), like, stream)
+        return (None, 0, None) if ws is None else (ws.data_ptr(), nbytes, ws)
+    return _ptr(ws), ws.numel() * ws.element_size(), ws
 
 
 def embed_fwd(table, ids, out, scale: float = 1.0, stream=None):
@@ -491,9 +508,9 @@ def embed_fwd(table, ids, out, scale: float = 1.0, stream=None):
     import torch
 
     (V, D), T = table.shape, ids.shape[0]
-    dt = _dtype_code(table)
-    _want(table, "table", table.dtype), _want(ids, "ids", torch.int32, (T,)), _want(out, "out", table.dtype, (T, D))
-    st = lib().embed_fwd(_ptr(table), _ptr(ids), _ptr(out), T, V, D, float(scale), dt, _stream(stream))
+    dt, ty = _dtype_code(table), table.dtype
+    st = lib().embed_fwd(_arg(table, "table", ty, (V, D)), _arg(ids, "ids", torch.int32, (T,)), _arg(out, "out", ty, (T, D)),
+                         T, V, D, scale, dt, _stream(stream))
     _check(st, "embed_fwd")
     return out
 
@@ -512,10 +529,10 @@ def embed_bwd(ids, dout, dtable, scale: float = 1.0, accumulate: bool = False, w
 
     (T, D), V = dout.shape, dtable.shape[0]
     dt = _dtype_code(dout)
-    _want(ids, "ids", torch.int32, (T,)), _want(dout, "dout", dout.dtype), _want(dtable, "dtable", torch.float32, (V, D))
-    ws, ws_bytes = _ws(ws, embed_bwd_workspace_bytes(T, V, D), dout, stream)
-    st = lib().embed_bwd(_ptr(ids), _ptr(dout), _ptr(dtable), T, V, D, float(scale), 1 if accumulate else 0, dt, _ptr(ws),
-                         ws_bytes, _stream(stream))
+    args = (_arg(ids, "ids", torch.int32, (T,)), _arg(dout, "dout", dout.dtype, (T, D)),
+            _arg(dtable, "dtable", torch.float32, (V, D)))
+    wp, wn, ws = _ws_for(ws, lambda: embed_bwd_workspace_bytes(T, V, D), dout, stream)
+    st = lib().embed_bwd(*args, T, V, D, scale, 1 if accumulate else 0, dt, wp, wn, _stream(stream))
     _check(st, "embed_bwd")
     return dtable
 
@@ -526,12 +543,11 @@ def embed_bwd_rows(ids, dout, V: int, tokens, rows, scale: float = 1.0, ws=None,
     import torch
 
     T, D = dout.shape
-    dt = _dtype_code(dout)
-    _want(ids, "ids", torch.int32, (T,)), _want(dout, "dout", dout.dtype)
-    _want(tokens, "tokens", torch.int32, (min(T, V),)), _want(rows, "rows", torch.float32, (min(T, V), D))
-    ws, ws_bytes = _ws(ws, embed_bwd_workspace_bytes(T, V, D), dout, stream)
-    st = lib().embed_bwd_rows(_ptr(ids), _ptr(dout), _ptr(tokens), _ptr(rows), T, V, D, float(scale), dt, _ptr(ws), ws_bytes,
-                              _stream(stream))
+    dt, n = _dtype_code(dout), min(T, V)
+    args = (_arg(ids, "ids", torch.int32, (T,)), _arg(dout, "dout", dout.dtype, (T, D)),
+            _arg(tokens, "tokens", torch.int32, (n,)), _arg(rows, "rows", torch.float32, (n, D)))
+    wp, wn, ws = _ws_for(ws, lambda: embed_bwd_workspace_bytes(T, V, D), dout, stream)
+    st = lib().embed_bwd_rows(*args, T, V, D, scale, dt, wp, wn, _stream(stream))
     _check(st, "embed_bwd_rows")
     return tokens, rows
 
@@ -546,30 +562,16 @@ def token_loss_workspace_bytes(op: int, T: int, V: int, ldz: int, npairs: int = 
     return int(n)
 
 
-def _loss_inputs(op, logits, targets, weights, logp, dlogits, vocab, npairs, ws, stream, rows):
-    """(T, V, ldz, type code, workspace, its bytes) of a loss call; `rows` names its
-    further fp32 [T] inputs."""
+def token_logp(logits, targets, logp, weights=None, vocab=None, ws=None, stream=None):
+    """logp[t] = log softmax(logits[t, :vocab])[targets[t]]; 0 where weights[t] is 0."""
     import torch
 
     T, ldz = logits.shape
-    V = ldz if vocab is None else int(vocab)
-    dt = _dtype_code(logits)
-    _want(logits, "logits", logits.dtype), _want(targets, "targets", torch.int32, (T,))
-    for name, t in {"weights": weights, "logp": logp, **rows}.items():
-        if t is not None:
-            _want(t, name, torch.float32, (T,))
-    if dlogits is not None:
-        _want(dlogits, "dlogits", logits.dtype, (T, ldz))
-    ws, ws_bytes = _ws(ws, token_loss_workspace_bytes(op, T, V, ldz, npairs, dt), logits, stream)
-    return T, V, ldz, dt, ws, ws_bytes
-
-
-def token_logp(logits, targets, logp, weights=None, vocab=None, ws=None, stream=None):
-    """logp[t] = log softmax(logits[t, :vocab])[targets[t]]; 0 where weights[t] is 0."""
-    T, V, ldz, dt, ws, ws_bytes = _loss_inputs(TOKEN_LOSS_OP_LOGP, logits, targets, weights, logp, None, vocab, 0, ws, stream,
-                                               {})
-    st = lib().token_logp(_ptr(logits), ldz, _ptr(targets), _ptr(weights), _ptr(logp), T, V, dt, _ptr(ws), ws_bytes,
-                          _stream(stream))
+    V, dt, f32 = ldz if vocab is None else vocab, _dtype_code(logits), torch.float32
+    args = (_arg(logits, "logits", logits.dtype, (T, ldz)), ldz, _arg(targets, "targets", torch.int32, (T,)),
+            _opt(weights, "weights", f32, (T,)), _arg(logp, "logp", f32, (T,)))
+    wp, wn, ws = _ws_for(ws, lambda: token_loss_workspace_bytes(TOKEN_LOSS_OP_LOGP, T, V, ldz, 0, dt), logits, stream)
+    st = lib().token_logp(*args, T, V, dt, wp, wn, _stream(stream))
     _check(st, "token_logp")
     return logp
 
@@ -580,12 +582,14 @@ def policy_loss(logits, targets, weights, advantages, old_logp, ref_logp, loss, 
     and, when given, dlogits (which may be logits)."""
     import torch
 
-    T, V, ldz, dt, ws, ws_bytes = _loss_inputs(TOKEN_LOSS_OP_POLICY, logits, targets, weights, logp, dlogits, vocab, 0, ws,
-                                               stream, {"advantages": advantages, "old_logp": old_logp, "ref_logp": ref_logp})
-    _want(loss, "loss", torch.float32, (1,))
-    st = lib().policy_loss(_ptr(logits), ldz, _ptr(targets), _ptr(weights), _ptr(advantages), _ptr(old_logp), _ptr(ref_logp),
-                           _ptr(loss), _ptr(logp), _ptr(dlogits), T, V, float(clip_lo), float(clip_hi), float(kl_coef), dt,
-                           _ptr(ws), ws_bytes, _stream(stream))
+    T, ldz = logits.shape
+    V, dt, f32 = ldz if vocab is None else vocab, _dtype_code(logits), torch.float32
+    args = (_arg(logits, "logits", logits.dtype, (T, ldz)), ldz, _arg(targets, "targets", torch.int32, (T,)),
+            _opt(weights, "weights", f32, (T,)), _arg(advantages, "advantages", f32, (T,)), _arg(old_logp, "old_logp", f32, (T,)),
+            _opt(ref_logp, "ref_logp", f32, (T,)), _arg(loss, "loss", f32, (1,)), _arg(logp, "logp", f32, (T,)),
+            _opt(dlogits, "dlogits", logits.dtype, (T, ldz)))
+    wp, wn, ws = _ws_for(ws, lambda: token_loss_workspace_bytes(TOKEN_LOSS_OP_POLICY, T, V, ldz, 0, dt), logits, stream)
+    st = lib().policy_loss(*args, T, V, clip_lo, clip_hi, kl_coef, dt, wp, wn, _stream(stream))
     _check(st, "policy_loss")
     return loss
 
@@ -596,14 +600,15 @@ def preference_loss(logits, targets, weights, ref_logp, seq, loss, margins, logp
     the header): fills loss [1], margins [pairs], logp [T] and, when given, dlogits."""
     import torch
 
-    npairs = margins.shape[0]
-    T, V, ldz, dt, ws, ws_bytes = _loss_inputs(TOKEN_LOSS_OP_PREFERENCE, logits, targets, weights, logp, dlogits, vocab, npairs,
-                                               ws, stream, {"ref_logp": ref_logp})
-    _want(loss, "loss", torch.float32, (1,)), _want(margins, "margins", torch.float32, (npairs,))
-    _want(seq, "seq", torch.int32, (2 * npairs + 1,))
-    st = lib().preference_loss(_ptr(logits), ldz, _ptr(targets), _ptr(weights), _ptr(ref_logp), _ptr(seq), npairs, _ptr(loss),
-                               _ptr(margins), _ptr(logp), _ptr(dlogits), T, V, float(beta), float(label_smoothing), dt,
-                               _ptr(ws), ws_bytes, _stream(stream))
+    (T, ldz), npairs = logits.shape, margins.shape[0]
+    V, dt, f32 = ldz if vocab is None else vocab, _dtype_code(logits), torch.float32
+    args = (_arg(logits, "logits", logits.dtype, (T, ldz)), ldz, _arg(targets, "targets", torch.int32, (T,)),
+            _opt(weights, "weights", f32, (T,)), _opt(ref_logp, "ref_logp", f32, (T,)),
+            _arg(seq, "seq", torch.int32, (2 * npairs + 1,)), npairs, _arg(loss, "loss", f32, (1,)),
+            _arg(margins, "margins", f32, (npairs,)), _arg(logp, "logp", f32, (T,)),
+            _opt(dlogits, "dlogits", logits.dtype, (T, ldz)))
+    wp, wn, ws = _ws_for(ws, lambda: token_loss_workspace_bytes(TOKEN_LOSS_OP_PREFERENCE, T, V, ldz, npairs, dt), logits, stream)
+    st = lib().preference_loss(*args, T, V, beta, label_smoothing, dt, wp, wn, _stream(stream))
     _check(st, "preference_loss")
     return loss
 
@@ -621,12 +626,10 @@ class GradList:
             raise ValueError("as many outputs as gradients are required")
         arr = (_Grad * max(len(grads), 1))()
         for i, (g, o) in enumerate(zip(grads, out)):
-            for name, t in (("a gradient", g), ("an output", o)):
-                _want(t, name, t.dtype)
-                _ptr(t)
             if o.numel() != g.numel():
                 raise ValueError("an output has another size than its gradient")
-            arr[i] = _Grad(g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(g), _dtype_code(o))
+            arr[i] = _Grad(_arg(g, "a gradient", g.dtype, g.shape), _arg(o, "an output", o.dtype, o.shape), g.numel(),
+                           _dtype_code(g), _dtype_code(o))
         n = lib().grad_list_bytes(arr, len(grads))
         if n == ctypes.c_size_t(-1).value:
             raise LoraError(LORA_EINVAL, "grad_list_bytes", lib().lora_last_error().decode())
@@ -647,8 +650,7 @@ def grad_norm(grads: GradList, norm, stream=None):
     """norm [1] = global norm of the listed gradients."""
     import torch
 
-    _want(norm, "norm", torch.float32, (1,))
-    _check(lib().grad_norm(ctypes.byref(grads.list), _ptr(norm), _stream(stream)), "grad_norm")
+    _check(lib().grad_norm(ctypes.byref(grads.list), _arg(norm, "norm", torch.float32, (1,)), _stream(stream)), "grad_norm")
     return norm
 
 
@@ -657,8 +659,8 @@ def grad_clip(grads: GradList, max_norm: float, norm, stream=None):
     norm [2] receives the norm before and the factor."""
     import torch
 
-    _want(norm, "norm", torch.float32, (2,))
-    _check(lib().grad_clip(ctypes.byref(grads.list), float(max_norm), _ptr(norm), _stream(stream)), "grad_clip")
+    _check(lib().grad_clip(ctypes.byref(grads.list), max_norm, _arg(norm, "norm", torch.float32, (2,)), _stream(stream)),
+           "grad_clip")
     return norm
 
 
