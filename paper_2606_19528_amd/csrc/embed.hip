@@ -3,13 +3,20 @@
 //   dE[v]   = scale sum over t with ids[t] = v of dout[t], ascending t
 // An id outside [0, V) has a zero output row and no gradient.
 //
-// The gradient's positions are sorted by token (stable radix sort, so equal
-// tokens keep ascending t) and cut into chunks of equally many sorted
-// positions: a chunk's work does not depend on how often a token occurs.  A
-// chunk sums its tokens' rows one after another in registers.  What it holds
-// of a token that began in an earlier chunk goes to its partial sum, and the
-// join launch adds a token's partial sums in chunk order: no atomics, one
-// order of summation.
+// The gradient of many positions (EmbedPlan::scan false): they are sorted by
+// token (stable radix sort, so equal tokens keep ascending t) and cut into
+// chunks of equally many sorted positions: a chunk's work does not depend on
+// how often a token occurs.  A chunk sums its tokens' rows one after another in
+// registers.  What it holds of a token that began in an earlier chunk goes to
+// its partial sum, and the join launch adds a token's partial sums in chunk
+// order: no atomics on values, one order of summation.
+//
+// The gradient of few positions: six to nine launches of a sort would take
+// longer than the sums.  A workgroup instead looks for its positions' tokens
+// among all of them: see embed_scan_kernel.
+#include <algorithm>
+#include <type_traits>
+
 #include "kernels.hpp"
 #include "launch.hpp"
 
@@ -41,9 +48,11 @@ __global__ __launch_bounds__(EF_NT) void embed_fwd_kernel(const typename E::T *t
 
 // ---- stable radix sort of (token, position) ------------------------------------
 // Keys are tokens, V for an id outside [0, V) so that those sort last.  One pass
-// per digit of up to 9 bits over tiles of 2048 keys: the tiles' digit counts
-// (digit-major), their prefix along the tiles, the scatter.
-constexpr int RS_NT = 256, RS_R = 8, RS_TILE = RS_NT * RS_R, RS_BINS = 512, RS_WAVES = RS_NT / 64;
+// per digit of up to 9 bits over tiles of 1024 keys: the tiles' digit counts
+// (digit-major), their prefix along the tiles, the scatter.  Up to RS_DIRECT
+// tiles the scatter sums the counts itself and the prefix launch is spared.
+constexpr int RS_DIRECT = 64;
+constexpr int RS_NT = 256, RS_R = 4, RS_TILE = RS_NT * RS_R, RS_BINS = 512, RS_WAVES = RS_NT / 64;
 
 __device__ __forceinline__ uint32_t embed_key(int32_t id, int V) { return id >= 0 && id < V ? (uint32_t)id : (uint32_t)V; }
 
@@ -107,12 +116,12 @@ __global__ __launch_bounds__(RS_NT) void radix_prefix_kernel(int *count, int nti
   if (threadIdx.x == 0) total[blockIdx.x] = base;
 }
 
-// A wave owns 512 consecutive keys, 64 a round; lanes with equal digits find
+// A wave owns 64 RS_R consecutive keys, 64 a round; lanes with equal digits find
 // each other by ballots, so a key's rank among its wave's equal digits is the
 // count of the earlier rounds plus the lower lanes of its own.
 __global__ __launch_bounds__(RS_NT) void radix_scatter_kernel(const uint32_t *key, const int32_t *pos, bool ids, int n, int V,
                                                               int shift, int bits, int ntile, const int *count, const int *total,
-                                                              uint32_t *key_out, int32_t *pos_out) {
+                                                              bool direct, uint32_t *key_out, int32_t *pos_out) {
   __shared__ int cnt[RS_WAVES][RS_BINS];
   __shared__ int base[RS_BINS];
   __shared__ int part[RS_WAVES];
@@ -121,10 +130,22 @@ __global__ __launch_bounds__(RS_NT) void radix_scatter_kernel(const uint32_t *ke
   int run = 0;
   for (int d0 = 0; d0 < bins; d0 += RS_NT) {  // keys of smaller digits, and of this digit in earlier tiles
     const int d = d0 + threadIdx.x;
-    int all;
-    const int x = d < bins ? total[d] : 0;
+    int all, x = 0, before = 0;
+    if (d < bins) {
+      const int *row = count + (int64_t)d * ntile;
+      if (direct) {
+#pragma unroll 8
+        for (int t = 0; t < ntile; ++t) {
+          x += row[t];
+          before += t < (int)blockIdx.x ? row[t] : 0;
+        }
+      } else {
+        x = total[d];
+        before = row[blockIdx.x];
+      }
+    }
     const int e = block_scan<RS_NT>(x, part, &all);
-    if (d < bins) base[d] = run + e + count[(int64_t)d * ntile + blockIdx.x];
+    if (d < bins) base[d] = run + e + before;
     run += all;
   }
   __syncthreads();
@@ -179,39 +200,84 @@ __global__ __launch_bounds__(RS_NT) void radix_scatter_kernel(const uint32_t *ke
 // A sorted place is a head when its token is in range and differs from the one
 // before; seg[i] = number of the place's token among the distinct ones.
 constexpr int SG_NT = 256, SG_R = 8, SG_TILE = SG_NT * SG_R;
+constexpr int SG_OWN = 16;  // tiles up to which each counts the heads before it itself
 
-__device__ __forceinline__ bool is_head(const uint32_t *sid, int64_t i, int n, int V) {
-  return i < n && sid[i] != (uint32_t)V && (i == 0 || sid[i - 1] != sid[i]);
+// Heads among the places i .. i + 7 (i a multiple of 8), as bits.
+__device__ __forceinline__ uint32_t heads8(const uint32_t *sid, int64_t i, int n, int V, uint32_t *k) {
+  if (i >= n) return 0;
+  uint32_t last = i > 0 ? sid[i - 1] : (uint32_t)V;
+  if (i + 8 <= n) {
+    const u32x4 lo = ld16(sid + i), hi = ld16(sid + i + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      k[e] = lo[e];
+      k[4 + e] = hi[e];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) k[e] = i + e < n ? sid[i + e] : (uint32_t)V;
+  }
+  uint32_t h = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    h |= (uint32_t)(k[e] != (uint32_t)V && k[e] != last) << e;
+    last = k[e];
+  }
+  return h;
 }
 __global__ __launch_bounds__(SG_NT) void seg_count_kernel(const uint32_t *sid, int n, int V, int *count) {
   __shared__ int part[SG_NT / 64];
-  int c = 0;
-  for (int r = 0; r < SG_R; ++r)
-    c += is_head(sid, (int64_t)blockIdx.x * SG_TILE + r * SG_NT + threadIdx.x, n, V);
+  uint32_t k[SG_R];
   int all;
-  block_scan<SG_NT>(c, part, &all);
+  block_scan<SG_NT>(__popc(heads8(sid, (int64_t)blockIdx.x * SG_TILE + threadIdx.x * SG_R, n, V, k)), part, &all);
   if (threadIdx.x == 0) count[blockIdx.x] = all;
 }
-// count becomes its exclusive prefix, total[0] the number of distinct tokens.
-__global__ __launch_bounds__(SG_NT) void seg_kernel(const uint32_t *sid, int n, int V, const int *before, int *seg, int32_t *tokens) {
+// before: heads ahead of each tile (and behind them the number of heads in all); null:
+// each workgroup counts them itself, and the last one leaves the number in nseg.
+__global__ __launch_bounds__(SG_NT) void seg_kernel(const uint32_t *sid, int n, int V, const int *before, int *nseg, int *seg,
+                                                    int32_t *tokens) {
   __shared__ int part[SG_NT / 64];
-  int run = before[blockIdx.x] - 1;
-  for (int r = 0; r < SG_R; ++r) {
-    const int64_t i = (int64_t)blockIdx.x * SG_TILE + r * SG_NT + threadIdx.x;
-    const bool h = is_head(sid, i, n, V);
-    int all;
-    const int e = block_scan<SG_NT>(h, part, &all);
-    if (i < n) {
-      const int s = run + e + (h ? 1 : 0);
-      seg[i] = s;
-      if (h) tokens[s] = (int32_t)sid[i];
-    }
+  uint32_t k[SG_R];
+  const int64_t i0 = (int64_t)blockIdx.x * SG_TILE + threadIdx.x * SG_R;
+  int run = -1, all;
+  if (before) {
+    run += before[blockIdx.x];
+  } else {
+    int c = 0;
+#pragma unroll 4
+    for (int b = 0; b < (int)blockIdx.x; ++b) c += __popc(heads8(sid, (int64_t)b * SG_TILE + threadIdx.x * SG_R, n, V, k));
+    block_scan<SG_NT>(c, part, &all);
     run += all;
   }
+  const uint32_t h = heads8(sid, i0, n, V, k);
+  run += block_scan<SG_NT>(__popc(h), part, &all);
+#pragma unroll
+  for (int e = 0; e < SG_R; ++e) {
+    if (i0 + e >= n) break;
+    if ((h >> e) & 1u) tokens[++run] = (int32_t)k[e];
+    seg[i0 + e] = run;
+  }
+  if (!before && blockIdx.x == gridDim.x - 1 && threadIdx.x == SG_NT - 1) nseg[0] = run + 1;
+}
+
+// ---- clearing ------------------------------------------------------------------------
+// One vector a thread: 1.2 GB at 6.8 TB/s.  (Four a thread 6.1; loops of 256 workgroups of
+// 256 threads side by side 6.5, and 5.2 with a look at a bitmap of the tokens present, so that
+// no row is written twice; 64 rows a workgroup 5.3.)
+constexpr int CL_NT = 256;
+__global__ __launch_bounds__(CL_NT) void clear_kernel(f32x4 *out, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * CL_NT + threadIdx.x;
+  if (i < n) out[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+}
+static void clear(float *out, int64_t rows, int64_t D, hipStream_t st) {
+  constexpr int64_t most = (int64_t)1 << 30;  // vectors a launch
+  for (int64_t v0 = 0, n = rows * (D / 4); v0 < n; v0 += most)
+    hipLaunchKernelGGL(clear_kernel, dim3((unsigned)((std::min(most, n - v0) + CL_NT - 1) / CL_NT)), dim3(CL_NT), 0, st,
+                       (f32x4 *)out + v0, std::min(most, n - v0));
 }
 
 // ---- sums ---------------------------------------------------------------------------
-constexpr int EG_NT = 128, EG_U = 8;
+constexpr int EG_NT = 256, EG_COL = 128, EG_U = 8;  // a workgroup: two chunks by EG_COL vectors
 
 struct EmbedGrad {
   const uint32_t *sid;   // [T] sorted tokens (V: none)
@@ -241,40 +307,22 @@ __device__ __forceinline__ void put_grad(const EmbedGrad &a, int64_t row, int v,
   }
 }
 
-// Workgroups [0, nchunk * ncol): a chunk and a block of EG_NT vectors of its
-// columns each.  The rest clear what no token reaches: 64 rows each.
+// Workgroups [0, nwork): two chunks and a block of EG_COL vectors of their columns
+// each.  Compact form: the rest clear 64 rows each of those that no token reaches.
 template <typename E>
-__global__ __launch_bounds__(EG_NT) void embed_grad_kernel(EmbedGrad a) {
+__global__ __launch_bounds__(EG_NT) void embed_grad_kernel(EmbedGrad a, unsigned nwork) {
   const int vpr = a.D / E::VEC;
-  const unsigned work = (unsigned)a.nchunk * a.ncol;
-  if (blockIdx.x >= work) {
-    const int64_t r0 = (int64_t)(blockIdx.x - work) * 64;
-    const int lane = threadIdx.x & 63;
-    const int64_t rows = a.tokens ? a.cap : a.V;
-    const int64_t r = r0 + lane;
-    bool used = r >= rows;
-    if (a.tokens) used = used || r < a.nseg[0];
-    else if (!used) {  // lower bound of token r among the sorted ones
-      int lo = 0, hi = a.T;
-      while (lo < hi) {
-        const int mid = (int)(((unsigned)lo + (unsigned)hi) >> 1);
-        if (a.sid[mid] < (uint32_t)r) lo = mid + 1;
-        else hi = mid;
-      }
-      used = lo < a.T && a.sid[lo] == (uint32_t)r;
-    }
-    uint64_t clear = ~__ballot(used);
-    if (a.tokens && threadIdx.x < 64 && !used) a.tokens[r] = -1;
-    while (clear) {
-      const int l = __ffsll((unsigned long long)clear) - 1;
-      clear &= clear - 1;
-      f32x4 *o = (f32x4 *)(a.out + (r0 + l) * a.D);
+  if (blockIdx.x >= nwork) {
+    const int64_t r0 = (int64_t)(blockIdx.x - nwork) * 64, r1 = min(r0 + 64, (int64_t)a.cap);
+    for (int64_t r = max(r0, (int64_t)a.nseg[0]); r < r1; ++r) {
+      if (threadIdx.x == 0) a.tokens[r] = -1;
+      f32x4 *o = (f32x4 *)(a.out + r * a.D);
       for (int v = threadIdx.x; v < a.D / 4; v += EG_NT) o[v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
     return;
   }
-  const int chunk = blockIdx.x / a.ncol, v = (blockIdx.x % a.ncol) * EG_NT + threadIdx.x;
-  if (v >= vpr) return;
+  const int chunk = blockIdx.x / a.ncol * 2 + threadIdx.x / EG_COL, v = (blockIdx.x % a.ncol) * EG_COL + threadIdx.x % EG_COL;
+  if (v >= vpr || chunk >= a.nchunk) return;
   const int64_t c0 = (int64_t)chunk * a.chunk, c1 = min((int64_t)a.T, c0 + a.chunk);
   uint32_t cur = a.sid[c0];
   bool later = c0 > 0 && a.sid[c0 - 1] == cur;  // the token began in an earlier chunk
@@ -321,9 +369,9 @@ __global__ __launch_bounds__(EG_NT) void embed_grad_kernel(EmbedGrad a) {
 // A token's partial sums, added to its row in chunk order by the workgroups of
 // the first chunk that the token runs into.
 template <typename E>
-__global__ __launch_bounds__(EG_NT) void embed_join_kernel(EmbedGrad a) {
+__global__ __launch_bounds__(EG_COL) void embed_join_kernel(EmbedGrad a) {
   const int vpr = a.D / E::VEC;
-  const int chunk = blockIdx.x / a.ncol + 1, v = (blockIdx.x % a.ncol) * EG_NT + threadIdx.x;
+  const int chunk = blockIdx.x / a.ncol + 1, v = (blockIdx.x % a.ncol) * EG_COL + threadIdx.x;
   if (v >= vpr) return;
   const int64_t c0 = (int64_t)chunk * a.chunk;
   const uint32_t tok = a.sid[c0];
@@ -341,6 +389,347 @@ __global__ __launch_bounds__(EG_NT) void embed_join_kernel(EmbedGrad a) {
   put_grad<E>(a, grad_row(a, c0), v, acc, true);
 }
 
+// ---- few positions: no sort ------------------------------------------------------------
+// The occurrences of a token, in ascending t, are cut into runs of RUN, and the
+// rows of a run are summed by the workgroup of the position that starts it.  The
+// first run's sum is the token's row; a later run's goes to a slot of its own,
+// and the join launch adds the slots of a token.
+// A workgroup of W waves takes W positions.  Each wave holds a W-th of all T tokens
+// in registers and compares it with the workgroup's W tokens (ballots): how
+// many equal ones lie before a position, and which are the next after it.
+// Slots: with L smaller tokens among the positions, run i of a token takes slot
+// (L + RUN i) / RUN, i > 0: in sorted order RUN positions of the same token lie
+// before it, so no other run's quotient is the same.
+// The compact form's row of a token is its rank in a bitmap of all tokens
+// present, which every workgroup builds in LDS.
+constexpr int ES_RUN = 8, ES_COLS = 256;  // columns of an item of the join launch
+constexpr int ES_U = 4;                   // a lane holds 4 ES_U tokens: T <= 16 NT
+
+struct EmbedScan {
+  const int32_t *ids;
+  const void *dout;
+  float *out;
+  int32_t *tokens;  // compact form; else null
+  // workspace: slots [T / RUN + 1][D]; per workgroup the number of its tokens with
+  // more than one run, and for each its row, first slot and number of slots
+  float *slots;
+  int32_t *nhot, *hot;
+  int T, V, D, cap, nwg, accumulate;
+  float scale;
+};
+
+// Four elements of a row.
+__device__ __forceinline__ f32x4 row4(BF16, const void *row, int v) {
+  const uint2 x = ((const uint2 *)row)[v];
+  return f32x4{__builtin_bit_cast(float, x.x << 16), __builtin_bit_cast(float, x.x & 0xffff0000u),
+               __builtin_bit_cast(float, x.y << 16), __builtin_bit_cast(float, x.y & 0xffff0000u)};
+}
+__device__ __forceinline__ f32x4 row4(F32, const void *row, int v) { return ((const f32x4 *)row)[v]; }
+
+// Positions base + 4 lane .. + 3 of the ids; -1 past the end.
+__device__ __forceinline__ int4 ids4(const int32_t *ids, int base, int lane, int T) {
+  const int i = base + 4 * lane;
+  if (i + 4 <= T) return *(const int4 *)(ids + i);
+  int4 k;
+  k.x = i < T ? ids[i] : -1;
+  k.y = i + 1 < T ? ids[i + 1] : -1;
+  k.z = i + 2 < T ? ids[i + 2] : -1;
+  k.w = -1;
+  return k;
+}
+// Lanes whose position base + 4 lane + c is below t.
+__device__ __forceinline__ uint64_t lanes_below(int t, int base, int c) {
+  const int n = (t - base - c + 3) >> 2;
+  return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull;
+}
+__device__ __forceinline__ int below_lane(uint64_t m) {  // bits of m below this lane
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+
+// Sum of the rows of positions t, list[0 .. n), n < R, into the row `dst`, by NT
+// threads.  All R rows are loaded, so that no branch stands between the loads
+// of several columns; those past n are the first row again.
+template <typename E, int NT, int R>
+__device__ __forceinline__ void sum_rows(const EmbedScan &a, int t, const int *list, int n, float *dst, float scale, bool add) {
+  const int64_t bytes = (int64_t)a.D * sizeof(typename E::T);
+  const char *x = (const char *)a.dout;
+  const int nv = a.D / 4;
+  const char *row[R];
+  row[0] = x + t * bytes;
+#pragma unroll
+  for (int u = 1; u < R; ++u) row[u] = x + (int64_t)(u <= n ? __builtin_amdgcn_readfirstlane(list[u - 1]) : t) * bytes;
+#pragma unroll(R == 8 ? 3 : R == 4 ? 4 : 8)
+  for (int v = threadIdx.x & (NT - 1); v < nv; v += NT) {
+    f32x4 f[R];
+#pragma unroll
+    for (int u = 0; u < R; ++u) f[u] = row4(E(), row[u], v);
+#pragma unroll
+    for (int u = 1; u < R; ++u) f[0] += u <= n ? f[u] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 s = f[0] * scale, *o = (f32x4 *)dst + v;
+    *o = add ? s + *o : s;
+  }
+}
+template <typename E, int NT>
+__device__ __forceinline__ void sum_run(const EmbedScan &a, int t, const int *list, int n, float *dst, float scale, bool add) {
+  if (n == 0) sum_rows<E, NT, 1>(a, t, list, n, dst, scale, add);
+  else if (n == 1) sum_rows<E, NT, 2>(a, t, list, n, dst, scale, add);
+  else if (n < 4) sum_rows<E, NT, 4>(a, t, list, n, dst, scale, add);
+  else sum_rows<E, NT, 8>(a, t, list, n, dst, scale, add);
+}
+
+template <typename E, int NT>
+__global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
+  constexpr int W = NT / 64;
+  extern __shared__ uint32_t lds[];  // compact form: bitmap words, then the marks before each word
+  __shared__ int near[W][W][ES_RUN];  // of position q, as wave w sees it: the next occurrences in its part,
+  __shared__ int nnear[W][W], nbefore[W][W];  // how many of them, how many before q
+  __shared__ int nless[W][W], nequal[W][W];
+  __shared__ int list[W][ES_RUN];
+  __shared__ int run[W][3];  // 1: the token's row, 2: a slot, 0: none; its number; rows after the first
+  __shared__ int hot[W][3], again[W];
+  __shared__ int part[W];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if ((int)blockIdx.x >= a.nwg) {  // dense form, not cleared ahead: the rows of 64 tokens that do not occur
+    const int64_t r0 = (int64_t)(blockIdx.x - a.nwg) * 64;
+    uint32_t *mask = lds;
+    if (threadIdx.x < 2) mask[threadIdx.x] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x * 4; i < a.T; i += NT * 4) {
+      const int4 k = ids4(a.ids, i - 4 * lane, lane, a.T);
+      const int kk[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int64_t d = (int64_t)kk[c] - r0;
+        if (d >= 0 && d < 64) atomicOr(&mask[d >> 5], 1u << (d & 31));
+      }
+    }
+    __syncthreads();
+    const int rows = (int)min((int64_t)64, a.V - r0);
+    for (int r = wave; r < rows; r += W) {
+      if ((mask[r >> 5] >> (r & 31)) & 1u) continue;
+      f32x4 *o = (f32x4 *)(a.out + (r0 + r) * a.D);
+      for (int v = lane; v < a.D / 4; v += 64) o[v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    return;
+  }
+  // This wave's part of the tokens: ES_U groups of 256 positions from p0 on.
+  const int groups = ((a.T + 255) / 256 + W - 1) / W, p0 = wave * groups * 256;
+  int4 x[ES_U];
+#pragma unroll
+  for (int u = 0; u < ES_U; ++u) x[u] = u < groups ? ids4(a.ids, p0 + u * 256, lane, a.T) : int4{-1, -1, -1, -1};
+  const int t0 = blockIdx.x * W;
+  int k[W];  // the workgroup's tokens, -1: none
+#pragma unroll
+  for (int q = 0; q < W; ++q) {
+    k[q] = t0 + q < a.T ? __builtin_amdgcn_readfirstlane(a.ids[t0 + q]) : -1;
+    if (k[q] >= a.V) k[q] = -1;
+  }
+  const int words = (a.V + 31) / 32;
+  uint32_t *before = lds + words;
+  int nseg = 0;
+  if (a.tokens) {
+    for (int i = threadIdx.x; i < words; i += NT) lds[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < ES_U; ++u) {
+      const int kk[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (kk[c] >= 0 && kk[c] < a.V) {  // (most of a frequent token's marks find it marked)
+          const uint32_t bit = 1u << (kk[c] & 31);
+          if (!(*(volatile uint32_t *)&lds[kk[c] >> 5] & bit)) atomicOr(&lds[kk[c] >> 5], bit);
+        }
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < W; ++q) {
+    const int t = t0 + q;
+    int nb = 0, na = 0;
+#pragma unroll
+    for (int u = 0; u < ES_U; ++u) {
+      if (k[q] < 0) break;
+      const int base = p0 + u * 256;
+      const uint64_t m[4] = {__ballot(x[u].x == k[q]), __ballot(x[u].y == k[q]), __ballot(x[u].z == k[q]),
+                             __ballot(x[u].w == k[q])};
+      if ((m[0] | m[1] | m[2] | m[3]) == 0) continue;
+      if (base + 256 <= t) {  // all before t
+        nb += __popcll(m[0]) + __popcll(m[1]) + __popcll(m[2]) + __popcll(m[3]);
+        continue;
+      }
+      if (na >= ES_RUN) continue;
+      uint64_t after[4];
+      int all = 0, mine = na;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        nb += __popcll(m[c] & lanes_below(t, base, c));
+        after[c] = m[c] & ~lanes_below(t + 1, base, c);
+        all += __popcll(after[c]);
+        mine += below_lane(after[c]);
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if ((after[c] >> lane) & 1ull) {
+          if (mine < ES_RUN) near[q][wave][mine] = base + 4 * lane + c;
+          ++mine;
+        }
+      na += all;
+    }
+    if (lane == 0) {
+      nbefore[q][wave] = nb;
+      nnear[q][wave] = min(na, ES_RUN);
+    }
+  }
+  __syncthreads();
+  if (a.tokens) {
+    // (an odd stretch a thread: its words lie in banks of their own)
+    const int per = ((words + NT - 1) / NT) | 1, w0 = min(words, per * (int)threadIdx.x), w1 = min(words, w0 + per);
+    int c = 0;
+    for (int i = w0; i < w1; ++i) c += __popc(lds[i]);
+    int b = block_scan<NT>(c, part, &nseg);
+    for (int i = w0; i < w1; ++i) {
+      before[i] = b;
+      b += __popc(lds[i]);
+    }
+  }
+  // Wave q joins what the waves saw of position q: its number among its token's
+  // occurrences, and the next RUN (one more than a run holds: whether another run follows).
+  const int t = t0 + wave;
+  int kt = t < a.T ? __builtin_amdgcn_readfirstlane(a.ids[t]) : -1;
+  if (kt >= a.V) kt = -1;
+  int j = 0, found = 0;
+  {
+    const int c = lane < W ? nnear[wave][lane] : 0, inc = wave_scan(c, lane);
+    int jb = lane < W ? nbefore[wave][lane] : 0;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) jb += __shfl_xor(jb, off);
+    j = __builtin_amdgcn_readfirstlane(jb);
+    found = __builtin_amdgcn_readlane(inc, 63);
+    for (int i = 0; i < c; ++i)
+      if (inc - c + i < ES_RUN) list[wave][inc - c + i] = near[wave][lane][i];
+  }
+  const bool starts = kt >= 0 && j % ES_RUN == 0, first = j == 0, more = found >= ES_RUN;
+  if (lane == 0) again[wave] = starts && (!first || more);
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < W; ++q) {
+    if (!__builtin_amdgcn_readfirstlane(again[q])) continue;
+    int less = 0, equal = 0;
+#pragma unroll
+    for (int u = 0; u < ES_U; ++u) {
+      const int xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        less += __popcll(__ballot((unsigned)xs[c] < (unsigned)k[q]));
+        equal += __popcll(__ballot(xs[c] == k[q]));
+      }
+    }
+    if (lane == 0) {
+      nless[q][wave] = less;
+      nequal[q][wave] = equal;
+    }
+  }
+  __syncthreads();
+  int kind = 0, row = 0;
+  if (lane < 3) hot[wave][lane] = 0;
+  if (starts) {
+    int less = 0, equal = 0;
+    if (!first || more)
+      for (int w = 0; w < W; ++w) {
+        less += nless[wave][w];
+        equal += nequal[wave][w];
+      }
+    kind = first ? 1 : 2;
+    row = first ? kt : (less + j) / ES_RUN;
+    if (a.tokens && first) {
+      row = before[kt >> 5] + __popc(lds[kt >> 5] & ((1u << (kt & 31)) - 1u));
+      if (lane == 0) a.tokens[row] = kt;
+    }
+    if (first && more && lane == 0) {
+      hot[wave][0] = row;
+      hot[wave][1] = (less + ES_RUN) / ES_RUN;
+      hot[wave][2] = (equal - 1) / ES_RUN;
+    }
+  }
+  const int n = min(found, ES_RUN - 1);
+  // Runs of one or two rows: each wave its own.  Longer ones: all waves, a part of the
+  // columns each (a wave alone took 12 rounds of eight loads for 3072 columns).
+  if (lane == 0) {
+    run[wave][0] = n > 1 ? kind : 0;
+    run[wave][1] = row;
+    run[wave][2] = n;
+  }
+  __syncthreads();
+  auto sum = [&](auto nt, int tt, const int *l, int m, int kd, int64_t r) {
+    sum_run<E, decltype(nt)::value>(a, tt, l, m, kd == 1 ? a.out + r * a.D : a.slots + r * a.D, kd == 1 ? a.scale : 1.0f,
+                                    kd == 1 && a.accumulate);
+  };
+  row = __builtin_amdgcn_readfirstlane(row);
+  if (kind != 0 && n <= 1) sum(std::integral_constant<int, 64>(), t, list[wave], n, kind, row);
+  if (a.tokens && t < a.cap && t >= nseg) {  // what no token reaches
+    if (lane == 0) a.tokens[t] = -1;
+    f32x4 *o = (f32x4 *)(a.out + (int64_t)t * a.D);
+    for (int v = lane; v < a.D / 4; v += 64) o[v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  for (int q = 0; q < W; ++q) {
+    const int kd = __builtin_amdgcn_readfirstlane(run[q][0]);
+    if (kd != 0)
+      sum(std::integral_constant<int, NT>(), t0 + q, list[q], __builtin_amdgcn_readfirstlane(run[q][2]), kd,
+          __builtin_amdgcn_readfirstlane(run[q][1]));
+  }
+  if (threadIdx.x == 0) {
+    int m = 0;
+    for (int q = 0; q < W; ++q) {
+      if (hot[q][2] == 0) continue;
+      int32_t *e = a.hot + 3 * ((int64_t)t0 + m++);
+      e[0] = hot[q][0];
+      e[1] = hot[q][1];
+      e[2] = hot[q][2];
+    }
+    a.nhot[blockIdx.x] = m;
+  }
+}
+
+// Adds the slots of the tokens with more than one run to their rows.  An item is
+// a token and ES_COLS columns; the waves take consecutive ranges of its slots,
+// whose sums are added in their order.
+constexpr int EJ_NT = 1024, EJ_WAVES = EJ_NT / 64, EJ_GRID = 512;
+__global__ __launch_bounds__(EJ_NT) void embed_slots_kernel(EmbedScan a, int per_wg) {
+  __shared__ int first[EJ_NT];  // number of the workgroup's first item
+  __shared__ int part[EJ_WAVES];
+  __shared__ f32x4 red[EJ_WAVES][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int total;
+  first[threadIdx.x] = block_scan<EJ_NT>((int)threadIdx.x < a.nwg ? a.nhot[threadIdx.x] : 0, part, &total);
+  __syncthreads();
+  const int ncol = (a.D + ES_COLS - 1) / ES_COLS;
+  for (int64_t it = blockIdx.x; it < (int64_t)total * ncol; it += gridDim.x) {
+    const int h = (int)(it / ncol), v = (int)(it % ncol) * 64 + lane;
+    int lo = 0, hi = a.nwg - 1;  // the last workgroup whose first item is at most h (it has one: empty ones repeat the next's)
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (first[mid] <= h) lo = mid;
+      else hi = mid - 1;
+    }
+    const int32_t *e = a.hot + 3 * ((int64_t)lo * per_wg + (h - first[lo]));
+    const int row = e[0], slot = e[1], n = e[2];
+    const int per = (n + EJ_WAVES - 1) / EJ_WAVES, s0 = min(n, wave * per), s1 = min(n, s0 + per);
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (v < a.D / 4) {
+      const f32x4 *x = (const f32x4 *)(a.slots + (int64_t)(slot + s0) * a.D) + v;
+#pragma unroll 8
+      for (int i = s0; i < s1; ++i, x += a.D / 4) s += *x;
+    }
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && v < a.D / 4) {
+      for (int w = 1; w < EJ_WAVES; ++w) s += red[w][lane];
+      f32x4 *o = (f32x4 *)(a.out + (int64_t)row * a.D) + v;
+      *o += s * a.scale;
+    }
+    __syncthreads();
+  }
+}
+
 hipError_t launch_embed_fwd(const void *table, const int32_t *ids, void *out, int T, int V, int D, float scale, Dtype d,
                             hipStream_t st) {
   const dim3 grid((T + EF_NT / 64 - 1) / (EF_NT / 64));
@@ -353,19 +742,34 @@ hipError_t launch_embed_fwd(const void *table, const int32_t *ids, void *out, in
   return hipGetLastError();
 }
 
+constexpr int64_t EMBED_SCAN_T = 6144, EMBED_SCAN_V = 196608;
+
 static size_t up256(size_t b) { return (b + 255) & ~size_t(255); }
 
 EmbedPlan embed_plan(int64_t T, int64_t V, int64_t D) {
   EmbedPlan p{};
+  size_t off = 0;
+  p.scan = T <= EMBED_SCAN_T && V <= EMBED_SCAN_V;
+  if (p.scan) {
+    p.per_wg = T <= 4096 ? 4 : 8;
+    p.nwg = (int)((T + p.per_wg - 1) / p.per_wg);
+    p.nhot = off;
+    off += up256((size_t)p.nwg * 4);
+    p.hot = off;
+    off += up256((size_t)p.nwg * p.per_wg * 12);
+    p.partial = off;
+    off += up256((size_t)(T / ES_RUN + 1) * D * 4);
+    p.total = off;
+    return p;
+  }
   int bits = 1;
   while (((int64_t)1 << bits) <= V) ++bits;  // keys 0 .. V
   p.passes = (bits + 8) / 9;
   p.digit = (bits + p.passes - 1) / p.passes;
   p.ntile = (int)((T + RS_TILE - 1) / RS_TILE);
-  p.chunk = T <= 8192 ? EG_U : 4 * EG_U;
+  p.chunk = 4 * EG_U;
   p.nchunk = (int)((T + p.chunk - 1) / p.chunk);
   const int64_t nsg = (T + SG_TILE - 1) / SG_TILE;
-  size_t off = 0;
   for (int i = 0; i < 2; ++i) {
     p.key[i] = off;
     off += up256((size_t)T * 4);
@@ -386,6 +790,7 @@ EmbedPlan embed_plan(int64_t T, int64_t V, int64_t D) {
 
 hipError_t launch_embed_sort(const int32_t *ids, int T, int V, const EmbedPlan &p, char *ws, int32_t *tokens, hipStream_t st) {
   const int bins = 1 << p.digit;
+  const bool direct = p.ntile <= RS_DIRECT;
   int *count = (int *)(ws + p.count), *total = count + (int64_t)RS_BINS * p.ntile;
   const uint32_t *key = (const uint32_t *)ids;
   const int32_t *pos = nullptr;
@@ -394,19 +799,60 @@ hipError_t launch_embed_sort(const int32_t *ids, int T, int V, const EmbedPlan &
     const bool first = s == 0;
     hipLaunchKernelGGL(radix_count_kernel, dim3(p.ntile), dim3(RS_NT), 0, st, key, first, T, V, s * p.digit, bins, p.ntile,
                        count);
-    hipLaunchKernelGGL(radix_prefix_kernel, dim3(bins), dim3(RS_NT), 0, st, count, p.ntile, total);
+    if (!direct) hipLaunchKernelGGL(radix_prefix_kernel, dim3(bins), dim3(RS_NT), 0, st, count, p.ntile, total);
     hipLaunchKernelGGL(radix_scatter_kernel, dim3(p.ntile), dim3(RS_NT), 0, st, key, pos, first, T, V, s * p.digit, p.digit,
-                       p.ntile, count, total, (uint32_t *)(ws + p.key[o]), (int32_t *)(ws + p.pos[o]));
+                       p.ntile, count, total, direct, (uint32_t *)(ws + p.key[o]), (int32_t *)(ws + p.pos[o]));
     key = (const uint32_t *)(ws + p.key[o]);
     pos = (const int32_t *)(ws + p.pos[o]);
   }
   if (tokens) {
     const int nsg = (T + SG_TILE - 1) / SG_TILE;
-    int *sc = (int *)(ws + p.segcount);
-    hipLaunchKernelGGL(seg_count_kernel, dim3(nsg), dim3(SG_NT), 0, st, key, T, V, sc);
-    hipLaunchKernelGGL(radix_prefix_kernel, dim3(1), dim3(RS_NT), 0, st, sc, nsg, sc + nsg);
-    hipLaunchKernelGGL(seg_kernel, dim3(nsg), dim3(SG_NT), 0, st, key, T, V, sc, (int *)(ws + p.seg), tokens);
+    int *sc = (int *)(ws + p.segcount), *seg = (int *)(ws + p.seg);
+    const bool own = nsg <= SG_OWN;
+    if (!own) {
+      hipLaunchKernelGGL(seg_count_kernel, dim3(nsg), dim3(SG_NT), 0, st, key, T, V, sc);
+      hipLaunchKernelGGL(radix_prefix_kernel, dim3(1), dim3(RS_NT), 0, st, sc, nsg, sc + nsg);
+    }
+    hipLaunchKernelGGL(seg_kernel, dim3(nsg), dim3(SG_NT), 0, st, key, T, V, own ? nullptr : sc, sc + nsg, seg, tokens);
   }
+  return hipGetLastError();
+}
+
+template <typename E>
+static void embed_scan(const EmbedScan &a, const EmbedPlan &p, int own, size_t lds, hipStream_t st) {
+  const dim3 grid((unsigned)(p.nwg + own));
+  if (p.per_wg == 4) hipLaunchKernelGGL((embed_scan_kernel<E, 256>), grid, dim3(256), lds, st, a);
+  else hipLaunchKernelGGL((embed_scan_kernel<E, 512>), grid, dim3(512), lds, st, a);
+}
+
+hipError_t launch_embed_scan(const int32_t *ids, const void *dout, float *out, int32_t *tokens, int T, int V, int D, float scale,
+                             bool accumulate, Dtype d, const EmbedPlan &p, char *ws, hipStream_t st) {
+  EmbedScan a{};
+  a.ids = ids;
+  a.dout = dout;
+  a.out = out;
+  a.tokens = tokens;
+  a.slots = (float *)(ws + p.partial);
+  a.nhot = (int32_t *)(ws + p.nhot);
+  a.hot = (int32_t *)(ws + p.hot);
+  a.T = T;
+  a.V = V;
+  a.D = D;
+  a.cap = T < V ? T : V;
+  a.nwg = p.nwg;
+  a.accumulate = accumulate;
+  a.scale = scale;
+  // A dense gradient below 64 MB is cleared beside the sums, which spares a launch (3 us);
+  // a larger one ahead of them, at the higher rate.
+  int own = 0;
+  if (!accumulate && !tokens) {
+    if ((int64_t)V * D < (16 << 20)) own = (V + 63) / 64;
+    else clear(out, V, D, st);
+  }
+  const size_t lds = tokens ? (size_t)((V + 31) / 32) * 8 : 8;
+  if (d == DT_BF16) embed_scan<BF16>(a, p, own, lds, st);
+  else embed_scan<F32>(a, p, own, lds, st);
+  if (T > ES_RUN) hipLaunchKernelGGL(embed_slots_kernel, dim3(EJ_GRID), dim3(EJ_NT), 0, st, a, p.per_wg);
   return hipGetLastError();
 }
 
@@ -430,15 +876,16 @@ hipError_t launch_embed_grad(const void *dout, float *out, int32_t *tokens, int 
   a.accumulate = accumulate;
   a.scale = scale;
   const int vec = d == DT_BF16 ? 8 : 4;
-  a.ncol = (D / vec + EG_NT - 1) / EG_NT;
-  const int64_t clear = accumulate ? 0 : ((tokens ? (int64_t)a.cap : (int64_t)V) + 63) / 64;
-  const dim3 grid((unsigned)((int64_t)a.nchunk * a.ncol + clear)), join((unsigned)((int64_t)(a.nchunk - 1) * a.ncol));
+  a.ncol = (D / vec + EG_COL - 1) / EG_COL;
+  const unsigned nwork = (unsigned)((int64_t)((a.nchunk + 1) / 2) * a.ncol);
+  if (!tokens && !accumulate) clear(out, V, D, st);
+  const dim3 grid(nwork + (tokens ? (unsigned)((a.cap + 63) / 64) : 0u)), join((unsigned)((int64_t)(a.nchunk - 1) * a.ncol));
   if (d == DT_BF16) {
-    hipLaunchKernelGGL(embed_grad_kernel<BF16>, grid, dim3(EG_NT), 0, st, a);
-    if (a.nchunk > 1) hipLaunchKernelGGL(embed_join_kernel<BF16>, join, dim3(EG_NT), 0, st, a);
+    hipLaunchKernelGGL(embed_grad_kernel<BF16>, grid, dim3(EG_NT), 0, st, a, nwork);
+    if (a.nchunk > 1) hipLaunchKernelGGL(embed_join_kernel<BF16>, join, dim3(EG_COL), 0, st, a);
   } else {
-    hipLaunchKernelGGL(embed_grad_kernel<F32>, grid, dim3(EG_NT), 0, st, a);
-    if (a.nchunk > 1) hipLaunchKernelGGL(embed_join_kernel<F32>, join, dim3(EG_NT), 0, st, a);
+    hipLaunchKernelGGL(embed_grad_kernel<F32>, grid, dim3(EG_NT), 0, st, a, nwork);
+    if (a.nchunk > 1) hipLaunchKernelGGL(embed_join_kernel<F32>, join, dim3(EG_COL), 0, st, a);
   }
   return hipGetLastError();
 }

@@ -380,14 +380,19 @@ RowSplit row_split(int64_t T, int64_t L, int r, Dtype dt);
 // ---- embedding lookup and its gradient (embed.hip) ----
 hipError_t launch_embed_fwd(const void *table, const int32_t *ids, void *out, int T, int V, int D, float scale, Dtype d,
                             hipStream_t st);
-// Sort and workspace (byte offsets) of an embedding gradient: `passes` digits
-// of `digit` bits over `ntile` tiles; the sums over `nchunk` chunks of `chunk`
-// sorted positions.
+// Workspace (byte offsets) of an embedding gradient and how it runs.  scan:
+// without a sort, `per_wg` positions a workgroup (launch_embed_scan).  Else a
+// sort by `passes` digits of `digit` bits over `ntile` tiles, and the sums over
+// `nchunk` chunks of `chunk` sorted positions.
 struct EmbedPlan {
+  bool scan;
+  int per_wg, nwg;
   int passes, digit, ntile, chunk, nchunk;
-  size_t key[2], pos[2], seg, segcount, count, partial, total;
+  size_t nhot, hot, key[2], pos[2], seg, segcount, count, partial, total;
 };
 EmbedPlan embed_plan(int64_t T, int64_t V, int64_t D);
+hipError_t launch_embed_scan(const int32_t *ids, const void *dout, float *out, int32_t *tokens, int T, int V, int D, float scale,
+                             bool accumulate, Dtype d, const EmbedPlan &p, char *ws, hipStream_t st);
 // Sorts the positions by token; with `tokens` also numbers the distinct tokens
 // and lists them there.
 hipError_t launch_embed_sort(const int32_t *ids, int T, int V, const EmbedPlan &p, char *ws, int32_t *tokens, hipStream_t st);

@@ -59,6 +59,13 @@ lora_status_t embed_grad(const int32_t *ids, const void *dout, float *out, int32
   const Range outs[] = {rng(out, rows * D * 4), rng(tokens, rows * 4), rng(ws, (int64_t)p.total)};
   if (clash(outs, ins)) return fail(LORA_EINVAL, "an output overlaps an input or another output");
   hipStream_t st = (hipStream_t)hip_stream;
+  if (p.scan) {
+    Timed t(K_EMBED_GRAD, st);
+    const hipError_t e = launch_embed_scan(ids, dout, out, tokens, (int)T, (int)V, (int)D, scale, accumulate != 0, dtype(dt), p,
+                                           (char *)ws, st);
+    t.done();
+    return e == hipSuccess ? LORA_OK : hip_fail(e, "embed_grad launch");
+  }
   {
     Timed t(K_EMBED_SORT, st);
     const hipError_t e = launch_embed_sort(ids, (int)T, (int)V, p, (char *)ws, tokens, st);
