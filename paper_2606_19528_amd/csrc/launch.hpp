@@ -455,7 +455,10 @@ struct GradEntries {
   GradEntry e[GRAD_ENTRIES];
 };
 constexpr int GRAD_PARTS = 1024;  // workgroups of the norm, one partial sum each
+constexpr int GRAD_FEW = 8;  // chunks of 4096 elements that one workgroup takes (launch_grad_few)
 hipError_t launch_grad_layout(const GradEntries &e, int count, int chunk, GradChunk *out, hipStream_t st);
+// norm[0], and with `clip` norm[1] and the outputs, in one launch.
+hipError_t launch_grad_few(const GradChunk *c, int nchunk, bool clip, float max_norm, float *norm, hipStream_t st);
 hipError_t launch_grad_norm(const GradChunk *c, int nchunk, double *part, float *norm, hipStream_t st);
 hipError_t launch_grad_clip(const GradChunk *c, int nchunk, double *part, float max_norm, float *norm, hipStream_t st);
 
