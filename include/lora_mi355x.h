@@ -319,8 +319,8 @@ lora_status_t lora_ckpt_backward(const lora_node_t *nodes, int n, int64_t T, con
  * ids are int32 device values; one outside [0, V) gives a zero row of out and
  * no gradient (a padding position, say).  table, out and dout have type dt; out is
  * rounded once.  Sums are fp32, over ascending t in groups whose size depends on T
- * alone.  D a multiple of 8 (LORA_EUNSUPPORTED).  T and V up to 2^30, matrices up
- * to 2^40 elements. */
+ * and V alone.  D a multiple of 8 up to 2^20, T up to 2^25, T D up to 2^37, V up to
+ * 2^30, the table up to 2^40 elements (LORA_EUNSUPPORTED). */
 lora_status_t embed_fwd(const void *table, const int32_t *ids, void *out, int64_t T, int64_t V,
                         int64_t D, float scale, lora_dtype_t dt, void *hip_stream);
 size_t embed_bwd_workspace_bytes(int64_t T, int64_t V, int64_t D);
@@ -359,8 +359,8 @@ lora_status_t embed_bwd_rows(const int32_t *ids, const void *dout, int32_t *toke
  *
  * A target outside [0, V) at a position of weight != 0 gives NaN (logp, the loss and
  * that row); logits of -inf are forbidden tokens of probability 0.  Rows of logits
- * must be whole 16-byte vectors (ldz a multiple of 8 bf16, 4 fp32;
- * LORA_EUNSUPPORTED); V is any.  loss is one fp32, margins [npairs] and logp [T]
+ * must be whole 16-byte vectors (ldz a multiple of 8 bf16, 4 fp32); V is any.  T up
+ * to 2^23, ldz to 2^30, npairs to 2^22, logits to 2^40 elements (LORA_EUNSUPPORTED).  loss is one fp32, margins [npairs] and logp [T]
  * fp32.  Statistics are fp32, the sums over positions 64-bit.  Workspace:
  * token_loss_workspace_bytes ((size_t)-1 for rejected sizes; npairs counts for
  * TOKEN_LOSS_OP_PREFERENCE only). */

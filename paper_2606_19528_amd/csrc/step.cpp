@@ -17,7 +17,11 @@ using namespace lora;
 namespace {
 
 constexpr int64_t kMaxMatrix = int64_t(1) << 40;  // elements; offsets are 64-bit
-constexpr int64_t kMaxRows = int64_t(1) << 30;
+constexpr int64_t kMaxRows = int64_t(1) << 30;    // a vocabulary, a row
+// A launch has fewer than 2^32 threads: positions of an embedding (64 threads each, and in
+// the gradient 4 for each 512 columns of each), of a loss (256 each), pairs (512 each).
+constexpr int64_t kMaxEmbedT = int64_t(1) << 25, kMaxEmbedElems = int64_t(1) << 37;
+constexpr int64_t kMaxLossT = int64_t(1) << 23, kMaxPairs = int64_t(1) << 22;
 
 bool bad_dtype(lora_dtype_t dt) { return dt != LORA_BF16 && dt != LORA_F32; }
 Dtype dtype(lora_dtype_t dt) { return dt == LORA_BF16 ? DT_BF16 : DT_F32; }
@@ -39,8 +43,8 @@ lora_status_t check_embed(int64_t T, int64_t V, int64_t D, lora_dtype_t dt) {
   if (T < 1 || V < 1 || D < 1) return fail(LORA_EINVAL, "T, V and D must be >= 1");
   if (D % 8) return fail(LORA_EUNSUPPORTED, "D must be a multiple of 8");
   if (D > kMaxDim) return fail(LORA_EUNSUPPORTED, "D must be at most 2^20");
-  if (T > kMaxRows || V > kMaxRows || T > kMaxMatrix / D || V > kMaxMatrix / D)
-    return fail(LORA_EUNSUPPORTED, "T and V at most 2^30, matrices at most 2^40 elements");
+  if (T > kMaxEmbedT || T > kMaxEmbedElems / D) return fail(LORA_EUNSUPPORTED, "T at most 2^25, T times D at most 2^37");
+  if (V > kMaxRows || V > kMaxMatrix / D) return fail(LORA_EUNSUPPORTED, "V at most 2^30, the table at most 2^40 elements");
   return LORA_OK;
 }
 lora_status_t embed_grad(const int32_t *ids, const void *dout, float *out, int32_t *tokens, bool compact, int64_t T,
@@ -108,8 +112,8 @@ lora_status_t check_loss_sizes(int op, int64_t T, int64_t V, int64_t ldz, int64_
   if (T < 1 || V < 1 || ldz < V) return fail(LORA_EINVAL, "need T >= 1, V >= 1 and ldz >= V");
   if (op == TOKEN_LOSS_OP_PREFERENCE && pairs < 1) return fail(LORA_EINVAL, "need at least one pair");
   if (ldz % (dt == LORA_BF16 ? 8 : 4)) return fail(LORA_EUNSUPPORTED, "rows of logits must be whole 16-byte vectors");
-  if (T > kMaxRows || ldz > kMaxRows || T > kMaxMatrix / ldz || (op == TOKEN_LOSS_OP_PREFERENCE && pairs > kMaxRows))
-    return fail(LORA_EUNSUPPORTED, "T, ldz and pairs at most 2^30, logits at most 2^40 elements");
+  if (T > kMaxLossT || ldz > kMaxRows || T > kMaxMatrix / ldz || (op == TOKEN_LOSS_OP_PREFERENCE && pairs > kMaxPairs))
+    return fail(LORA_EUNSUPPORTED, "T at most 2^23, ldz 2^30, pairs 2^22, logits 2^40 elements");
   return LORA_OK;
 }
 

@@ -364,7 +364,7 @@ __global__ __launch_bounds__(NT, 4) void policy_rows_kernel(TokenLoss a, PolicyA
   constexpr int SPAN = NT * E::VEC;  // elements of one vector of every thread
   u32x4 x[NV];
   auto buffer = [&](const void *q, int vecs) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(q), 0, vecs * 16, 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(q), 0, min(vecs, NV * NT) * 16, 0x00020000);
   };
   // The next row from t on of this workgroup with a weight, the others' dz cleared.
   auto next_row = [&](int64_t t) {

@@ -61,7 +61,7 @@ NAN, INF = float("nan"), math.inf
     (embed_fwd, dict(T=0), EINVAL), (embed_fwd, dict(V=0), EINVAL), (embed_fwd, dict(D=0), EINVAL),
     (embed_fwd, dict(D=12), EUNSUP), (embed_fwd, dict(D=1 << 21), EUNSUP), (embed_fwd, dict(dt=5), EINVAL),
     (embed_fwd, dict(scale=NAN), EINVAL), (embed_fwd, dict(out=P(3, 8)), EINVAL), (embed_fwd, dict(out=P(1, 64)), EINVAL),
-    (embed_fwd, dict(T=1 << 31), EUNSUP), (embed_fwd, dict(V=1 << 40), EUNSUP),
+    (embed_fwd, dict(T=(1 << 25) + 1, D=8), EUNSUP), (embed_fwd, dict(T=1 << 25, D=1 << 13), EUNSUP), (embed_fwd, dict(V=1 << 40), EUNSUP),
     (embed_bwd, dict(ids=None), EINVAL), (embed_bwd, dict(dout=None), EINVAL), (embed_bwd, dict(dtable=None), EINVAL),
     (embed_bwd, dict(ws=None), EWS), (embed_bwd, dict(wsb=64), EWS), (embed_bwd, dict(ws=P(5, 4)), EINVAL),
     (embed_bwd, dict(scale=INF), EINVAL), (embed_bwd, dict(dtable=P(3, 16)), EINVAL), (embed_bwd, dict(ws=P(4, 16)), EINVAL),
@@ -69,7 +69,7 @@ NAN, INF = float("nan"), math.inf
     (embed_rows, dict(tokens=None), EINVAL), (embed_rows, dict(tokens=P(4)), EINVAL), (embed_rows, dict(rows=P(5)), EINVAL),
     (logp, dict(z=None), EINVAL), (logp, dict(y=None), EINVAL), (logp, dict(logp=None), EINVAL), (logp, dict(V=0), EINVAL),
     (logp, dict(T=-1), EINVAL), (logp, dict(V=105), EINVAL), (logp, dict(ld=100), EUNSUP), (logp, dict(ld=102, dt=1), EUNSUP),
-    (logp, dict(dt=2), EINVAL), (logp, dict(z=P(1, 2)), EINVAL), (logp, dict(logp=P(3)), EINVAL), (logp, dict(T=1 << 31), EUNSUP),
+    (logp, dict(dt=2), EINVAL), (logp, dict(z=P(1, 2)), EINVAL), (logp, dict(logp=P(3)), EINVAL), (logp, dict(T=(1 << 23) + 1), EUNSUP),
     (policy, dict(adv=None), EINVAL), (policy, dict(old=None), EINVAL), (policy, dict(loss=None), EINVAL),
     (policy, dict(ref=None), EINVAL), (policy, dict(lo=-0.1), EINVAL), (policy, dict(hi=NAN), EINVAL),
     (policy, dict(kl=INF), EINVAL), (policy, dict(ws=None), EWS), (policy, dict(wsb=8), EWS), (policy, dict(dz=P(1, 16)), EINVAL),
@@ -77,7 +77,7 @@ NAN, INF = float("nan"), math.inf
     (policy, dict(T=1 << 62), EUNSUP),
     (pref, dict(seq=None), EINVAL), (pref, dict(margins=None), EINVAL), (pref, dict(pairs=0), EINVAL), (pref, dict(beta=NAN), EINVAL),
     (pref, dict(eps=-0.1), EINVAL), (pref, dict(eps=1.1), EINVAL), (pref, dict(ws=None), EWS), (pref, dict(margins=P(9)), EINVAL),
-    (pref, dict(dz=P(2)), EINVAL), (pref, dict(pairs=1 << 31), EUNSUP), (pref, dict(ld=100), EUNSUP),
+    (pref, dict(dz=P(2)), EINVAL), (pref, dict(pairs=(1 << 22) + 1), EUNSUP), (pref, dict(ld=100), EUNSUP),
 ])
 def test_refusals(fn, kw, code):
     assert fn(**kw) == code
