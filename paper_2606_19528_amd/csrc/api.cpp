@@ -44,6 +44,11 @@ std::vector<EventPair> g_prof[K_COUNT];
 
 }  // namespace
 
+lora::meet_word lora::next_tag() {
+  static MeetTags tags;
+  return tags.take();
+}
+
 lora::Timed::Timed(int id_, hipStream_t st_) : id(id_), st(st_) {
   std::lock_guard<std::mutex> lk(g_prof_mu);
   if (!g_prof_on) return;
@@ -102,11 +107,6 @@ unsigned int next_gen() {
     v = ++g;
   } while (v == 0);
   return v;
-}
-// Tag of a few-token launch's meetings.
-meet_word next_tag() {
-  static MeetTags tags;
-  return tags.take();
 }
 // Test hook (lora_debug_set_handover): 1 makes every tile's hand-over wait
 // of the following fused launches give up.

@@ -52,6 +52,9 @@ enum KernelId {
   K_COUNT
 };
 
+// Tag of a launch's meetings (meet.hpp).
+meet_word next_tag();
+
 // Brackets the launches of one kernel with events while the hook is enabled.
 struct Timed {
   int id;

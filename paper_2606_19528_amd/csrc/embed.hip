@@ -458,7 +458,7 @@ __device__ __forceinline__ void sum_rows(const EmbedScan &a, int t, const int *l
   row[0] = x + t * bytes;
 #pragma unroll
   for (int u = 1; u < R; ++u) row[u] = x + (int64_t)(u <= n ? __builtin_amdgcn_readfirstlane(list[u - 1]) : t) * bytes;
-#pragma unroll(R == 8 ? 3 : R == 4 ? 4 : 8)
+#pragma unroll(R == 8 ? 2 : R == 4 ? 2 : 4)
   for (int v = threadIdx.x & (NT - 1); v < nv; v += NT) {
     f32x4 f[R];
 #pragma unroll

@@ -416,6 +416,8 @@ struct TokenLoss {
   // them of each row (preference); the targets' logits; w dL/dlogp (preference);
   // w L (policy) or a pair's loss
   float *stat, *ztgt, *coef, *rows;
+  // token_logp of rows in parts: the flags of the parts' meetings, this launch's tag
+  meet_word *sync, gen;
 };
 // Parts of a row, a workgroup each, in the launches for few rows, and their
 // length in 16-byte vectors.

@@ -25,7 +25,7 @@
 
 #include "kernels.hpp"
 #include "launch.hpp"
-#include "meet.hpp"
+#include "meet_flags.hpp"
 
 namespace lora {
 
@@ -37,28 +37,6 @@ constexpr int NW_BKE = 64;  // k per stage
 template <int V>
 struct NwIC {
   static constexpr int value = V;
-};
-
-// The flags of a meeting of n <= 64 workgroups (meet.hpp) as one wave reads and
-// writes them, a word a lane.  (A counter instead of flags serialised the
-// arrivals, 1.1 us each; only those that see all flags up meet in the exchange.)
-struct NwFlags {
-  meet_word *w;
-  int lane;
-  __device__ void raise(int i, meet_word tag) {
-    if (lane == 0) __hip_atomic_store(w + i, tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __device__ void settle() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-  __device__ bool all_up(int n, meet_word tag) {
-    const meet_word f = lane < n ? __hip_atomic_load(w + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : tag;
-    return __ballot(f != tag) == 0;
-  }
-  // (the return value is lane 0's)
-  __device__ meet_word lower(int n) {
-    if (lane == 0) return __hip_atomic_exchange(w, meet_word(0), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (lane < n) __hip_atomic_store(w + lane, meet_word(0), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return 0;
-  }
 };
 
 // 16 bytes at device scope (sc1: past the caches that other XCDs do not see).
@@ -400,7 +378,7 @@ __global__ __launch_bounds__(256) void narrow_kernel(NarrowArgs a) {
   if (a.parts > 1) {
     __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0): this wave's stores have completed
     __syncthreads();
-    NwFlags flags{a.sync + tile_id * a.parts, lane};
+    MeetFlags flags{a.sync + tile_id * a.parts, lane};
     if (wv == 0) {
       const bool all = meet_arrive(flags, part, a.parts, a.gen);
       if (lane == 0) *s_all = all;
@@ -506,7 +484,7 @@ __global__ __launch_bounds__(256) void narrow_kernel(NarrowArgs a) {
       __syncthreads();
       // (Two may see all: they store the same sums, and raise nothing after.)
       if (wv == 0) {
-        NwFlags flags{a.sync + (int64_t)a.tiles_n * a.tiles_m * a.parts + nt * a.tiles_m, lane};
+        MeetFlags flags{a.sync + (int64_t)a.tiles_n * a.tiles_m * a.parts + nt * a.tiles_m, lane};
         const bool all = meet_arrive(flags, mt, a.tiles_m, a.gen);
         if (all) meet_lower(flags, a.tiles_m);
         if (lane == 0) *s_all = all;

@@ -86,7 +86,7 @@ lora_status_t embed_grad(const int32_t *ids, const void *dout, float *out, int32
 // ----- losses over the targets' log-probabilities ---------------------------------
 struct LossLayout {
   LossPlan plan;
-  size_t stat, ztgt, coef, rows, total;
+  size_t stat, ztgt, coef, rows, sync, total;
 };
 LossLayout loss_layout(int op, int64_t T, int64_t V, int64_t ldz, int64_t pairs, lora_dtype_t dt) {
   LossLayout L{};
@@ -101,6 +101,8 @@ LossLayout loss_layout(int op, int64_t T, int64_t V, int64_t ldz, int64_t pairs,
   off += pref ? round256((size_t)T * 4) : 0;
   L.rows = off;
   off += op == TOKEN_LOSS_OP_LOGP ? 0 : round256((size_t)(pref ? pairs : T) * 4);
+  L.sync = off;
+  off += op == TOKEN_LOSS_OP_LOGP && L.plan.parts > 1 ? round256((size_t)T * L.plan.parts * sizeof(meet_word)) : 0;
   L.total = off;
   return L;
 }
@@ -164,6 +166,7 @@ TokenLoss loss_args(const void *logits, int64_t ldz, const int32_t *targets, con
   a.ztgt = (float *)(wsb + L.ztgt);
   a.coef = L.coef == L.rows ? nullptr : (float *)(wsb + L.coef);
   a.rows = (float *)(wsb + L.rows);
+  a.sync = (meet_word *)(wsb + L.sync);
   return a;
 }
 
@@ -306,7 +309,8 @@ lora_status_t token_logp(const void *logits, int64_t ldz, const int32_t *targets
   s = check_loss(TOKEN_LOSS_OP_LOGP, logits, ldz, targets, weights, logp, nullptr, T, V, 0, dt, nullptr, 0, nullptr, 0, ws,
                  ws_bytes, &L);
   if (s != LORA_OK) return s;
-  const TokenLoss a = loss_args(logits, ldz, targets, weights, logp, nullptr, nullptr, T, V, L, ws);
+  TokenLoss a = loss_args(logits, ldz, targets, weights, logp, nullptr, nullptr, T, V, L, ws);
+  a.gen = next_tag();
   hipStream_t st = (hipStream_t)hip_stream;
   Timed t(K_TOKEN_LOGP, st);
   const hipError_t e = launch_token_logp(a, dtype(dt), st);

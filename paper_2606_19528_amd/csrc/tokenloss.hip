@@ -12,6 +12,7 @@
 // Rows of weight 0 are not read; their logp is 0 and their gradient a row of zeros.
 #include "kernels.hpp"
 #include "launch.hpp"
+#include "meet_flags.hpp"
 
 namespace lora {
 
@@ -151,7 +152,21 @@ __device__ __forceinline__ void policy_terms(const PolicyArgs &p, int64_t t, dou
 // ---- statistics of rows, or of parts of rows -------------------------------------
 constexpr int TL_NT = 256;
 
-// Part p of a row: vectors [p, p + 1) * part_vecs.
+// Part p of row t, vectors [p, p + 1) part_vecs, for the whole workgroup.
+template <typename E>
+__device__ __forceinline__ Stat part_stat(const TokenLoss &a, int64_t t, int p, Stat *red) {
+  const u32x4 *row = row_ptr<E>(a, t);
+  const int nv = (a.V + E::VEC - 1) / E::VEC, end = min(nv, (p + 1) * a.part_vecs);
+  Stat st{-INFINITY, 0.0f};
+  for (int i = p * a.part_vecs + threadIdx.x; i < end; i += TL_NT) {
+    u32x4 x = row[i];
+    if ((i + 1) * E::VEC > a.V) x = cut_row(E(), x, i, a.V, neg_inf_bits(E()));
+    stat_vec<E>(st, x);
+  }
+  return block_stat<TL_NT>(st, red);
+}
+
+// stat: for the launches that follow; null: whole rows, logp.
 template <typename E>
 __global__ __launch_bounds__(TL_NT) void token_stat_kernel(TokenLoss a, Stat *stat) {
   __shared__ Stat red[TL_NT / 64];
@@ -162,15 +177,7 @@ __global__ __launch_bounds__(TL_NT) void token_stat_kernel(TokenLoss a, Stat *st
     if (!stat && threadIdx.x == 0) a.logp[t] = 0.0f;
     return;
   }
-  const u32x4 *row = row_ptr<E>(a, t);
-  const int nv = (a.V + E::VEC - 1) / E::VEC, end = min(nv, (p + 1) * a.part_vecs);
-  Stat st{-INFINITY, 0.0f};
-  for (int i = p * a.part_vecs + threadIdx.x; i < end; i += TL_NT) {
-    u32x4 x = row[i];
-    if ((i + 1) * E::VEC > a.V) x = cut_row(E(), x, i, a.V, neg_inf_bits(E()));
-    stat_vec<E>(st, x);
-  }
-  st = block_stat<TL_NT>(st, red);
+  const Stat st = part_stat<E>(a, t, p, red);
   if (threadIdx.x) return;
   if (stat) stat[blockIdx.x] = st;
   else a.logp[t] = (float)logp_of(target_logit<E>(a, t), st);
@@ -185,17 +192,44 @@ __device__ __forceinline__ Stat joined_stat(const TokenLoss &a, const Stat *stat
   return wave_stat(lane < a.parts ? stat[t * a.parts + lane] : Stat{-INFINITY, 0.0f});
 }
 __device__ __forceinline__ Stat thread_stat(const TokenLoss &a, const Stat *stat, int64_t t) {
-  Stat st = stat[t * a.parts];
-  for (int p = 1; p < a.parts; ++p) st = stat_join(st, stat[t * a.parts + p]);
+  constexpr int U = 8;  // loads in flight
+  Stat st{-INFINITY, 0.0f};
+  for (int p = 0; p < a.parts; p += U) {
+    Stat x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = stat[t * a.parts + min(p + u, a.parts - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (p + u < a.parts) st = stat_join(st, x[u]);
+  }
   return st;
 }
 
-__global__ __launch_bounds__(TL_NT) void logp_join_kernel(TokenLoss a, const Stat *stat) {
-  const int64_t t = (int64_t)blockIdx.x * (TL_NT / 64) + (threadIdx.x >> 6);
-  if (t >= a.T) return;
-  float logp = 0.0f;
-  if (weight(a, t) != 0.0f) logp = (float)logp_of(a.ztgt[t], joined_stat(a, stat, t));
-  if ((threadIdx.x & 63) == 0) a.logp[t] = logp;
+// token_logp of few rows in one launch: the parts of a row meet (meet.hpp), and the
+// one that comes last joins them.  Statistics and flags are written and read at
+// device scope, by the first wave.
+template <typename E>
+__global__ __launch_bounds__(TL_NT) void logp_parts_kernel(TokenLoss a) {
+  __shared__ Stat red[TL_NT / 64];
+  const int64_t t = blockIdx.x / a.parts;
+  const int p = blockIdx.x % a.parts, lane = threadIdx.x & 63;
+  if (weight(a, t) == 0.0f) {
+    if (p == 0 && threadIdx.x == 0) a.logp[t] = 0.0f;
+    return;
+  }
+  const Stat st = part_stat<E>(a, t, p, red);
+  if (threadIdx.x >= 64) return;
+  uint64_t *slot = (uint64_t *)a.stat + t * a.parts;
+  if (lane == 0) __hip_atomic_store(slot + p, __builtin_bit_cast(uint64_t, st), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  MeetFlags flags{a.sync + t * a.parts, lane};
+  flags.settle();  // the part is in memory before its flag rises
+  if (!meet_arrive(flags, p, a.parts, a.gen)) return;
+  Stat all{-INFINITY, 0.0f};
+  if (lane < a.parts)
+    all = __builtin_bit_cast(Stat, __hip_atomic_load(slot + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+  all = wave_stat(all);
+  const float logp = (float)logp_of(target_logit<E>(a, t), all);
+  if (meet_lower(flags, a.parts) == a.gen && lane == 0) a.logp[t] = logp;
 }
 
 // ---- sums over positions -----------------------------------------------------------
@@ -454,11 +488,12 @@ __global__ __launch_bounds__(NT, 4) void policy_rows_kernel(TokenLoss a, PolicyA
 }
 
 // Parts of a row in the launches that take few rows: enough for about 8192
-// workgroups, none under 8 KB, at most a wave's lanes.
+// workgroups, none under 16 KB (of 4, 8, 16 and 32 KB the best over a pair, a short answer and a
+// short rollout), at most a wave's lanes.
 LossPlan loss_plan(int64_t T, int64_t V, int64_t ld, Dtype d) {
   const int64_t vec = d == DT_BF16 ? 8 : 4, nz = (V + vec - 1) / vec;
   LossPlan p{};
-  const int64_t most = nz / 512, want = (8192 + T - 1) / T;
+  const int64_t most = nz / 1024, want = (8192 + T - 1) / T;
   p.parts = (int)(most < 1 ? 1 : most < want ? most : want);
   if (p.parts > 64) p.parts = 64;
   p.part_vecs = (int)((nz + p.parts - 1) / p.parts);
@@ -466,15 +501,15 @@ LossPlan loss_plan(int64_t T, int64_t V, int64_t ld, Dtype d) {
   return p;
 }
 
+template <typename E>
+static void logp_launch(const TokenLoss &a, hipStream_t st) {
+  const dim3 grid((unsigned)((int64_t)a.T * a.parts));
+  if (a.parts > 1) hipLaunchKernelGGL(logp_parts_kernel<E>, grid, dim3(TL_NT), 0, st, a);
+  else hipLaunchKernelGGL(token_stat_kernel<E>, grid, dim3(TL_NT), 0, st, a, (Stat *)nullptr);
+}
 hipError_t launch_token_logp(const TokenLoss &a, Dtype d, hipStream_t st) {
-  Stat *stat = a.parts > 1 ? (Stat *)a.stat : nullptr;
-  const dim3 grid((unsigned)((int64_t)a.T * a.parts)), join((a.T + TL_NT / 64 - 1) / (TL_NT / 64));
-  if (d == DT_BF16) {
-    hipLaunchKernelGGL(token_stat_kernel<BF16>, grid, dim3(TL_NT), 0, st, a, stat);
-  } else {
-    hipLaunchKernelGGL(token_stat_kernel<F32>, grid, dim3(TL_NT), 0, st, a, stat);
-  }
-  if (stat) hipLaunchKernelGGL(logp_join_kernel, join, dim3(TL_NT), 0, st, a, stat);
+  if (d == DT_BF16) logp_launch<BF16>(a, st);
+  else logp_launch<F32>(a, st);
   return hipGetLastError();
 }
 

@@ -376,6 +376,35 @@ def test_graph_replays_and_other_stream():
         assert all(torch.equal(a, b) for a, b in zip(want, (L, lp, dz)))
 
 
+def test_logp_in_parts_replays():
+    """Rows in parts that meet within the launch: a captured call replayed, with eager
+    calls on the same workspace in between, and a workspace of arbitrary contents."""
+    _announce("logp parts graph")
+    T, V = 24, 128256
+    g = torch.Generator().manual_seed(3)
+    n = lm.token_loss_workspace_bytes(lm.TOKEN_LOSS_OP_LOGP, T, V, V)
+    ws = torch.randint(0, 256, (n,), dtype=torch.uint8, device="cuda")
+    y = torch.randint(0, V, (T,), generator=g, dtype=torch.int32).cuda()
+    z, lp, want = torch.empty(T, V, dtype=BF16, device="cuda"), torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    z.normal_()
+    lm.token_logp(z, y, lp, ws=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lm.token_logp(z, y, lp, ws=ws)
+    for seed in range(6):
+        z.normal_(std=1.0 + seed)
+        lp.fill_(5.0)
+        graph.replay()
+        lm.token_logp(z, y, want, ws=ws if seed % 2 else None)
+        torch.cuda.synchronize()
+        assert torch.equal(lp, want)
+        if seed == 3:
+            ws.random_(0, 256)
+    ref = R.logp(z.cpu(), y.cpu(), V)[0]
+    _close(lp.cpu(), ref, R.logp_bound(z.cpu(), y.cpu(), V), "logp")
+
+
 def test_python_refusals():
     T, V = 4, 16
     z = torch.zeros(T, V, device="cuda")
