@@ -22,27 +22,32 @@
 
 namespace lora {
 
-// One wave a token.
-constexpr int EF_NT = 256;
+// A wave takes up to 4 vectors a lane of one token's row, all loads before the first
+// store.  Bound by memory: 16384 rows of 2048 bf16 18 us (67 MB written, 30 MB of distinct
+// rows read: 5.4 TB/s); 24 rows of 3072 2.8 us, 3.5 with a wave a row and a load at a time.
+constexpr int EF_NT = 256, EF_U = 4;
 template <typename E>
 __global__ __launch_bounds__(EF_NT) void embed_fwd_kernel(const typename E::T *table, const int32_t *ids,
-                                                          typename E::T *out, int T, int V, int vpr, float scale) {
-  const int t = blockIdx.x * (EF_NT / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (t >= T) return;
+                                                          typename E::T *out, int T, int V, int vpr, unsigned per_row,
+                                                          float scale) {
+  const unsigned w = blockIdx.x * (EF_NT / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const unsigned t = w / per_row;
+  if (t >= (unsigned)T) return;
+  const int v0 = (w % per_row) * 64 * EF_U + lane;
   const int id = __builtin_amdgcn_readfirstlane(ids[t]);
   const bool ok = id >= 0 && id < V;
   const u32x4 *src = (const u32x4 *)table + (int64_t)(ok ? id : 0) * vpr;
-  u32x4 *dst = (u32x4 *)out + (int64_t)t * vpr;
-  for (int v = lane; v < vpr; v += 64) {
-    u32x4 x = zero16();
-    if (ok) {
-      float f[E::VEC];
-      unpack_vec(E(), src[v], f);
+  u32x4 *dst = (u32x4 *)out + (int64_t)t * vpr, x[EF_U];
 #pragma unroll
-      for (int e = 0; e < E::VEC; ++e) f[e] *= scale;
-      x = pack_vec(E(), f);
-    }
-    dst[v] = x;
+  for (int u = 0; u < EF_U; ++u) x[u] = ok && v0 + u * 64 < vpr ? src[v0 + u * 64] : zero16();
+#pragma unroll
+  for (int u = 0; u < EF_U; ++u) {
+    if (v0 + u * 64 >= vpr) break;
+    float f[E::VEC];
+    unpack_vec(E(), x[u], f);
+#pragma unroll
+    for (int e = 0; e < E::VEC; ++e) f[e] *= scale;
+    dst[v0 + u * 64] = ok ? pack_vec(E(), f) : zero16();
   }
 }
 
@@ -277,6 +282,8 @@ static void clear(float *out, int64_t rows, int64_t D, hipStream_t st) {
 }
 
 // ---- sums ---------------------------------------------------------------------------
+// 16384 positions of 151936 x 2048: sort and numbers 22 us, sums 40, join 5 (201 MB, 39 us at a
+// copy's rate); of 128256 x 3072 the sums alone take 81 (300 MB, 59).
 constexpr int EG_NT = 256, EG_COL = 128, EG_U = 8;  // a workgroup: two chunks by EG_COL vectors
 
 struct EmbedGrad {
@@ -402,6 +409,10 @@ __global__ __launch_bounds__(EG_COL) void embed_join_kernel(EmbedGrad a) {
 // before it, so no other run's quotient is the same.
 // The compact form's row of a token is its rank in a bitmap of all tokens
 // present, which every workgroup builds in LDS.
+// 4096 positions of 128256 x 3072, frequencies of a text: 29 us and 7 for the join (75 MB, 15 us
+// at a copy's rate); 23 with all tokens different, 14 of which remain at 64 columns: the chain
+// load, compare, meet in LDS, load rows.  More positions a workgroup (8 instead of 4: 37 us in
+// all for 36, and 24 against 20 at 512 positions) lengthen it.
 constexpr int ES_RUN = 8, ES_COLS = 256;  // columns of an item of the join launch
 constexpr int ES_U = 4;                   // a lane holds 4 ES_U tokens: T <= 16 NT
 
@@ -689,7 +700,8 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
   }
 }
 
-// Adds the slots of the tokens with more than one run to their rows.  An item is
+// Adds the slots of the tokens with more than one run to their rows (half as many
+// workgroups: 38 us for both launches of the case above, instead of 36).  An item is
 // a token and ES_COLS columns; the waves take consecutive ranges of its slots,
 // whose sums are added in their order.
 constexpr int EJ_NT = 1024, EJ_WAVES = EJ_NT / 64, EJ_GRID = 512;
@@ -732,16 +744,21 @@ __global__ __launch_bounds__(EJ_NT) void embed_slots_kernel(EmbedScan a, int per
 
 hipError_t launch_embed_fwd(const void *table, const int32_t *ids, void *out, int T, int V, int D, float scale, Dtype d,
                             hipStream_t st) {
-  const dim3 grid((T + EF_NT / 64 - 1) / (EF_NT / 64));
+  const int vpr = D / (d == DT_BF16 ? 8 : 4);
+  const unsigned per_row = (vpr + 64 * EF_U - 1) / (64 * EF_U);
+  const dim3 grid((unsigned)(((int64_t)T * per_row + EF_NT / 64 - 1) / (EF_NT / 64)));
   if (d == DT_BF16)
     hipLaunchKernelGGL(embed_fwd_kernel<BF16>, grid, dim3(EF_NT), 0, st, (const uint16_t *)table, ids, (uint16_t *)out, T, V,
-                       D / 8, scale);
+                       vpr, per_row, scale);
   else
-    hipLaunchKernelGGL(embed_fwd_kernel<F32>, grid, dim3(EF_NT), 0, st, (const float *)table, ids, (float *)out, T, V, D / 4,
-                       scale);
+    hipLaunchKernelGGL(embed_fwd_kernel<F32>, grid, dim3(EF_NT), 0, st, (const float *)table, ids, (float *)out, T, V, vpr,
+                       per_row, scale);
   return hipGetLastError();
 }
 
+// Without a sort, compact form over 128256 x 3072 / 8192 x 512: 4096 positions 36 / 24 us (with
+// one 57 / 42), 6000 58 / 44 (61 / 44), 8192 74 / 54 (65 / 47).  The bitmap of up to 196608
+// tokens and its counts take 48 KB of LDS.
 constexpr int64_t EMBED_SCAN_T = 6144, EMBED_SCAN_V = 196608;
 
 static size_t up256(size_t b) { return (b + 255) & ~size_t(255); }
@@ -842,17 +859,20 @@ hipError_t launch_embed_scan(const int32_t *ids, const void *dout, float *out, i
   a.nwg = p.nwg;
   a.accumulate = accumulate;
   a.scale = scale;
-  // A dense gradient below 64 MB is cleared beside the sums, which spares a launch (3 us);
-  // a larger one ahead of them, at the higher rate.
+  // A dense gradient below 256 MB is cleared beside the sums, which spares a launch (3 us) and
+  // hides the search for the tokens; a larger one ahead of them, at the higher rate.
   int own = 0;
   if (!accumulate && !tokens) {
-    if ((int64_t)V * D < (16 << 20)) own = (V + 63) / 64;
+    if ((int64_t)V * D < (64 << 20)) own = (V + 63) / 64;
     else clear(out, V, D, st);
   }
   const size_t lds = tokens ? (size_t)((V + 31) / 32) * 8 : 8;
   if (d == DT_BF16) embed_scan<BF16>(a, p, own, lds, st);
   else embed_scan<F32>(a, p, own, lds, st);
-  if (T > ES_RUN) hipLaunchKernelGGL(embed_slots_kernel, dim3(EJ_GRID), dim3(EJ_NT), 0, st, a, p.per_wg);
+  if (T > ES_RUN) {  // (at most T / (RUN + 1) tokens have a second run)
+    const int64_t items = (int64_t)(T / (ES_RUN + 1)) * ((D + ES_COLS - 1) / ES_COLS);
+    hipLaunchKernelGGL(embed_slots_kernel, dim3((unsigned)std::min<int64_t>(EJ_GRID, items)), dim3(EJ_NT), 0, st, a, p.per_wg);
+  }
   return hipGetLastError();
 }
 

@@ -424,7 +424,7 @@ struct TokenLoss {
 struct LossPlan {
   int parts, part_vecs;
 };
-LossPlan loss_plan(int64_t T, int64_t V, int64_t ld, Dtype d);
+LossPlan loss_plan(int64_t T, int64_t V, Dtype d, bool logp_only);
 struct PolicyArgs {
   const float *adv, *old_logp, *ref;  // ref null: no KL term
   float lo, hi, kl;                   // ratio bounds 1 - clip_lo, 1 + clip_hi

@@ -18,9 +18,9 @@ namespace {
 
 constexpr int64_t kMaxMatrix = int64_t(1) << 40;  // elements; offsets are 64-bit
 constexpr int64_t kMaxRows = int64_t(1) << 30;    // a vocabulary, a row
-// A launch has fewer than 2^32 threads: positions of an embedding (64 threads each, and in
-// the gradient 4 for each 512 columns of each), of a loss (256 each), pairs (512 each).
-constexpr int64_t kMaxEmbedT = int64_t(1) << 25, kMaxEmbedElems = int64_t(1) << 37;
+// A launch has fewer than 2^32 threads: positions of an embedding (64 threads each for 4 KB of
+// row, and in the gradient 4 for each 512 columns), of a loss (256 each), pairs (512 each).
+constexpr int64_t kMaxEmbedT = int64_t(1) << 25, kMaxEmbedElems = int64_t(1) << 35;
 constexpr int64_t kMaxLossT = int64_t(1) << 23, kMaxPairs = int64_t(1) << 22;
 
 bool bad_dtype(lora_dtype_t dt) { return dt != LORA_BF16 && dt != LORA_F32; }
@@ -43,7 +43,7 @@ lora_status_t check_embed(int64_t T, int64_t V, int64_t D, lora_dtype_t dt) {
   if (T < 1 || V < 1 || D < 1) return fail(LORA_EINVAL, "T, V and D must be >= 1");
   if (D % 8) return fail(LORA_EUNSUPPORTED, "D must be a multiple of 8");
   if (D > kMaxDim) return fail(LORA_EUNSUPPORTED, "D must be at most 2^20");
-  if (T > kMaxEmbedT || T > kMaxEmbedElems / D) return fail(LORA_EUNSUPPORTED, "T at most 2^25, T times D at most 2^37");
+  if (T > kMaxEmbedT || T > kMaxEmbedElems / D) return fail(LORA_EUNSUPPORTED, "T at most 2^25, T times D at most 2^35");
   if (V > kMaxRows || V > kMaxMatrix / D) return fail(LORA_EUNSUPPORTED, "V at most 2^30, the table at most 2^40 elements");
   return LORA_OK;
 }
@@ -88,9 +88,9 @@ struct LossLayout {
   LossPlan plan;
   size_t stat, ztgt, coef, rows, sync, total;
 };
-LossLayout loss_layout(int op, int64_t T, int64_t V, int64_t ldz, int64_t pairs, lora_dtype_t dt) {
+LossLayout loss_layout(int op, int64_t T, int64_t V, int64_t pairs, lora_dtype_t dt) {
   LossLayout L{};
-  L.plan = loss_plan(T, V, ldz, dtype(dt));
+  L.plan = loss_plan(T, V, dtype(dt), op == TOKEN_LOSS_OP_LOGP);
   const bool pref = op == TOKEN_LOSS_OP_PREFERENCE;
   size_t off = 0;
   L.stat = off;  // of the parts, and of the rows
@@ -129,7 +129,7 @@ lora_status_t check_loss(int op, const void *logits, int64_t ldz, const int32_t 
   if (!logits || !targets || !logp) return fail(LORA_EINVAL, "logits, targets and logp are required");
   const void *ptrs[] = {logits, targets, weights, logp, dlogits};
   if (misaligned(ptrs)) return fail(LORA_EINVAL, "pointers must be 16-byte aligned");
-  *L = loss_layout(op, T, V, ldz, pairs, dt);
+  *L = loss_layout(op, T, V, pairs, dt);
   if ((s = check_ws(ws, ws_bytes, L->total)) != LORA_OK) return s;
   const int64_t zb = T * ldz * (int64_t)esize(dt);
   Range ins[8], outs[8];
@@ -298,7 +298,7 @@ lora_status_t embed_bwd_rows(const int32_t *ids, const void *dout, int32_t *toke
 
 size_t token_loss_workspace_bytes(token_loss_op_t op, int64_t T, int64_t V, int64_t ldz, int64_t npairs, lora_dtype_t dt) {
   if (check_loss_sizes(op, T, V, ldz, npairs, dt) != LORA_OK) return (size_t)-1;
-  return loss_layout(op, T, V, ldz, npairs, dt).total;
+  return loss_layout(op, T, V, npairs, dt).total;
 }
 
 lora_status_t token_logp(const void *logits, int64_t ldz, const int32_t *targets, const float *weights, float *logp,

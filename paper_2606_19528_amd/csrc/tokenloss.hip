@@ -10,6 +10,8 @@
 // logp is held in 64 bits until it is rounded for the output: in 32 bits the rounding of
 // log s and logp would be most of the error of a margin, a difference of sums of logp.
 // Rows of weight 0 are not read; their logp is 0 and their gradient a row of zeros.
+#include <algorithm>
+
 #include "kernels.hpp"
 #include "launch.hpp"
 #include "meet_flags.hpp"
@@ -487,16 +489,19 @@ __global__ __launch_bounds__(NT, 4) void policy_rows_kernel(TokenLoss a, PolicyA
   }
 }
 
-// Parts of a row in the launches that take few rows: enough for about 8192
-// workgroups, none under 16 KB (of 4, 8, 16 and 32 KB the best over a pair, a short answer and a
-// short rollout), at most a wave's lanes.
-LossPlan loss_plan(int64_t T, int64_t V, int64_t ld, Dtype d) {
+// Parts of a row in the launches that take few rows: at most a wave's lanes, none under
+// 16 KB (of 4, 8, 16 and 32 KB the best over a pair, a short answer and a short rollout).
+// Before a gradient: enough for about 8192 workgroups (2048 x 151936 bf16 in pairs 326 us,
+// whole rows 370).  Log-probabilities alone, whose parts meet: 2048 workgroups, and rows up to
+// 64 KB whole (1024 x 32000 bf16 12.9 us, 16 in parts for 2048 workgroups; 512 x 151936 28.7,
+// whole rows 36.5, 33.3 in parts for 8192).
+LossPlan loss_plan(int64_t T, int64_t V, Dtype d, bool logp_only) {
   const int64_t vec = d == DT_BF16 ? 8 : 4, nz = (V + vec - 1) / vec;
+  const int64_t want = ((logp_only ? 2048 : 8192) + T - 1) / T;
+  int64_t parts = std::min<int64_t>(std::min(want, nz / 1024), 64);
+  if (parts < 1 || (logp_only && nz <= 4096)) parts = 1;
   LossPlan p{};
-  const int64_t most = nz / 1024, want = (8192 + T - 1) / T;
-  p.parts = (int)(most < 1 ? 1 : most < want ? most : want);
-  if (p.parts > 64) p.parts = 64;
-  p.part_vecs = (int)((nz + p.parts - 1) / p.parts);
+  p.part_vecs = (int)((nz + parts - 1) / parts);
   p.parts = (int)((nz + p.part_vecs - 1) / p.part_vecs);
   return p;
 }

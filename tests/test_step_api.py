@@ -61,7 +61,7 @@ NAN, INF = float("nan"), math.inf
     (embed_fwd, dict(T=0), EINVAL), (embed_fwd, dict(V=0), EINVAL), (embed_fwd, dict(D=0), EINVAL),
     (embed_fwd, dict(D=12), EUNSUP), (embed_fwd, dict(D=1 << 21), EUNSUP), (embed_fwd, dict(dt=5), EINVAL),
     (embed_fwd, dict(scale=NAN), EINVAL), (embed_fwd, dict(out=P(3, 8)), EINVAL), (embed_fwd, dict(out=P(1, 64)), EINVAL),
-    (embed_fwd, dict(T=(1 << 25) + 1, D=8), EUNSUP), (embed_fwd, dict(T=1 << 25, D=1 << 13), EUNSUP), (embed_fwd, dict(V=1 << 40), EUNSUP),
+    (embed_fwd, dict(T=(1 << 25) + 1, D=8), EUNSUP), (embed_fwd, dict(T=1 << 25, D=1 << 11), EUNSUP), (embed_fwd, dict(V=1 << 40), EUNSUP),
     (embed_bwd, dict(ids=None), EINVAL), (embed_bwd, dict(dout=None), EINVAL), (embed_bwd, dict(dtable=None), EINVAL),
     (embed_bwd, dict(ws=None), EWS), (embed_bwd, dict(wsb=64), EWS), (embed_bwd, dict(ws=P(5, 4)), EINVAL),
     (embed_bwd, dict(scale=INF), EINVAL), (embed_bwd, dict(dtable=P(3, 16)), EINVAL), (embed_bwd, dict(ws=P(4, 16)), EINVAL),
