@@ -282,8 +282,8 @@ static void clear(float *out, int64_t rows, int64_t D, hipStream_t st) {
 }
 
 // ---- sums ---------------------------------------------------------------------------
-// 16384 positions of 151936 x 2048: sort and numbers 22 us, sums 40, join 5 (201 MB, 39 us at a
-// copy's rate); of 128256 x 3072 the sums alone take 81 (300 MB, 59).
+// 16384 positions of 151936 x 2048: sort 24 us, numbers 7, sums 37, join 9 (201 MB, 39 us at a
+// copy's rate, and in the last-level cache); of 128256 x 3072 the sums alone take 78 (300 MB, 59).
 constexpr int EG_NT = 256, EG_COL = 128, EG_U = 8;  // a workgroup: two chunks by EG_COL vectors
 
 struct EmbedGrad {
