@@ -60,7 +60,8 @@
  * order work; see lora_handover_giveups); the part counts of the dA / dB
  * token reductions that run as token parts (they pick the part that adds
  * the parts' tiles, which it adds in ascending part order); the exchange that
- * picks it in the few-token kernel; and, in the top-k table build, the
+ * picks it in the few-token kernel and in token_logp of few rows; the counts and
+ * marks of tokens in the embedding gradient; and, in the top-k table build, the
  * reservation of candidate-list slots, whose order is normalised by the
  * selection (ties go to the smaller index).
  *

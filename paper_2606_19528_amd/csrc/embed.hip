@@ -15,7 +15,6 @@
 // longer than the sums.  A workgroup instead looks for its positions' tokens
 // among all of them: see embed_scan_kernel.
 #include <algorithm>
-#include <type_traits>
 
 #include "kernels.hpp"
 #include "launch.hpp"
@@ -409,10 +408,10 @@ __global__ __launch_bounds__(EG_COL) void embed_join_kernel(EmbedGrad a) {
 // before it, so no other run's quotient is the same.
 // The compact form's row of a token is its rank in a bitmap of all tokens
 // present, which every workgroup builds in LDS.
-// 4096 positions of 128256 x 3072, frequencies of a text: 29 us and 7 for the join (75 MB, 15 us
-// at a copy's rate); 23 with all tokens different, 14 of which remain at 64 columns: the chain
-// load, compare, meet in LDS, load rows.  More positions a workgroup (8 instead of 4: 37 us in
-// all for 36, and 24 against 20 at 512 positions) lengthen it.
+// 4096 positions of 128256 x 3072, frequencies of a text: 27 us and 7 for the join (75 MB, 15 us
+// at a copy's rate).  At 64 columns 18 remain, a chain in each workgroup: loads 0.6, bitmap and
+// its counts 4, comparisons 3, joins 2, rows 3.  More positions a workgroup (8 instead of 4: 37
+// us in all for 36, and 24 against 20 at 512 positions) lengthen it.
 constexpr int ES_RUN = 8, ES_COLS = 256;  // columns of an item of the join launch
 constexpr int ES_U = 4;                   // a lane holds 4 ES_U tokens: T <= 16 NT
 
@@ -469,7 +468,7 @@ __device__ __forceinline__ void sum_rows(const EmbedScan &a, int t, const int *l
   row[0] = x + t * bytes;
 #pragma unroll
   for (int u = 1; u < R; ++u) row[u] = x + (int64_t)(u <= n ? __builtin_amdgcn_readfirstlane(list[u - 1]) : t) * bytes;
-#pragma unroll(R == 8 ? 2 : R == 4 ? 2 : 4)
+#pragma unroll(R < 4 ? 8 : 2)
   for (int v = threadIdx.x & (NT - 1); v < nv; v += NT) {
     f32x4 f[R];
 #pragma unroll
@@ -481,17 +480,10 @@ __device__ __forceinline__ void sum_rows(const EmbedScan &a, int t, const int *l
   }
 }
 template <typename E, int NT>
-__device__ __forceinline__ void sum_run(const EmbedScan &a, int t, const int *list, int n, float *dst, float scale, bool add) {
-  if (n == 0) sum_rows<E, NT, 1>(a, t, list, n, dst, scale, add);
-  else if (n == 1) sum_rows<E, NT, 2>(a, t, list, n, dst, scale, add);
-  else if (n < 4) sum_rows<E, NT, 4>(a, t, list, n, dst, scale, add);
-  else sum_rows<E, NT, 8>(a, t, list, n, dst, scale, add);
-}
-
-template <typename E, int NT>
 __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
   constexpr int W = NT / 64;
-  extern __shared__ uint32_t lds[];  // compact form: bitmap words, then the marks before each word
+  extern __shared__ uint32_t lds[];  // compact form: bitmap words
+  __shared__ int stretch[NT];        // and the marks before each thread's
   __shared__ int near[W][W][ES_RUN];  // of position q, as wave w sees it: the next occurrences in its part,
   __shared__ int nnear[W][W], nbefore[W][W];  // how many of them, how many before q
   __shared__ int nless[W][W], nequal[W][W];
@@ -529,91 +521,93 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
 #pragma unroll
   for (int u = 0; u < ES_U; ++u) x[u] = u < groups ? ids4(a.ids, p0 + u * 256, lane, a.T) : int4{-1, -1, -1, -1};
   const int t0 = blockIdx.x * W;
-  int k[W];  // the workgroup's tokens, -1: none
-#pragma unroll
-  for (int q = 0; q < W; ++q) {
-    k[q] = t0 + q < a.T ? __builtin_amdgcn_readfirstlane(a.ids[t0 + q]) : -1;
-    if (k[q] >= a.V) k[q] = -1;
-  }
+  int ks = lane < W && t0 + lane < a.T ? a.ids[t0 + lane] : -1;  // lane q: the workgroup's token q, -1: none
+  if (ks >= a.V || ks < 0) ks = -1;
   const int words = (a.V + 31) / 32;
-  uint32_t *before = lds + words;
-  int nseg = 0;
   if (a.tokens) {
     for (int i = threadIdx.x; i < words; i += NT) lds[i] = 0;
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < ES_U; ++u) {
       const int kk[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+      uint32_t seen[4];  // (most of a frequent token's marks find it marked)
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        if (kk[c] >= 0 && kk[c] < a.V) {  // (most of a frequent token's marks find it marked)
-          const uint32_t bit = 1u << (kk[c] & 31);
-          if (!(*(volatile uint32_t *)&lds[kk[c] >> 5] & bit)) atomicOr(&lds[kk[c] >> 5], bit);
-        }
+        seen[c] = kk[c] >= 0 && kk[c] < a.V ? ((volatile uint32_t *)lds)[kk[c] >> 5] >> (kk[c] & 31) & 1u : 1u;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (!seen[c]) atomicOr(&lds[kk[c] >> 5], 1u << (kk[c] & 31));
     }
   }
-#pragma unroll
+  // Occurrences before each position, in this wave's part.  (The loops over positions are
+  // not unrolled: a launch runs the code once, so its length is time.)
+#pragma unroll 1
   for (int q = 0; q < W; ++q) {
-    const int t = t0 + q;
-    int nb = 0, na = 0;
+    const int t = t0 + q, k = __builtin_amdgcn_readlane(ks, q);
+    int nb = 0;
 #pragma unroll
     for (int u = 0; u < ES_U; ++u) {
-      if (k[q] < 0) break;
       const int base = p0 + u * 256;
-      const uint64_t m[4] = {__ballot(x[u].x == k[q]), __ballot(x[u].y == k[q]), __ballot(x[u].z == k[q]),
-                             __ballot(x[u].w == k[q])};
+      if (k < 0 || base >= t) break;
+      uint64_t m[4] = {__ballot(x[u].x == k), __ballot(x[u].y == k), __ballot(x[u].z == k), __ballot(x[u].w == k)};
       if ((m[0] | m[1] | m[2] | m[3]) == 0) continue;
-      if (base + 256 <= t) {  // all before t
-        nb += __popcll(m[0]) + __popcll(m[1]) + __popcll(m[2]) + __popcll(m[3]);
-        continue;
-      }
-      if (na >= ES_RUN) continue;
-      uint64_t after[4];
-      int all = 0, mine = na;
+      if (base + 256 > t)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        nb += __popcll(m[c] & lanes_below(t, base, c));
-        after[c] = m[c] & ~lanes_below(t + 1, base, c);
-        all += __popcll(after[c]);
-        mine += below_lane(after[c]);
-      }
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if ((after[c] >> lane) & 1ull) {
-          if (mine < ES_RUN) near[q][wave][mine] = base + 4 * lane + c;
-          ++mine;
-        }
-      na += all;
+        for (int c = 0; c < 4; ++c) m[c] &= lanes_below(t, base, c);
+      nb += __popcll(m[0]) + __popcll(m[1]) + __popcll(m[2]) + __popcll(m[3]);
     }
-    if (lane == 0) {
-      nbefore[q][wave] = nb;
-      nnear[q][wave] = min(na, ES_RUN);
-    }
+    if (lane == 0) nbefore[q][wave] = nb;
   }
   __syncthreads();
+  // Lane q W + w: what wave w saw before position q; every lane of q W .. the sum.
+  int jq = lane < W * W ? nbefore[lane / W][lane % W] : 0;
+#pragma unroll
+  for (int off = 1; off < W; off <<= 1) jq += __shfl_xor(jq, off);
+  // The next occurrences after each position that starts a run.
+#pragma unroll 1
+  for (int q = 0; q < W; ++q) {
+    const int t = t0 + q, k = __builtin_amdgcn_readlane(ks, q);
+    int na = 0;
+    if (k >= 0 && __builtin_amdgcn_readlane(jq, q * W) % ES_RUN == 0) {
+#pragma unroll
+      for (int u = 0; u < ES_U; ++u) {
+        const int base = p0 + u * 256;
+        if (base + 256 <= t || na >= ES_RUN) continue;
+        uint64_t m[4] = {__ballot(x[u].x == k), __ballot(x[u].y == k), __ballot(x[u].z == k), __ballot(x[u].w == k)};
+        if ((m[0] | m[1] | m[2] | m[3]) == 0) continue;
+        if (base <= t)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) m[c] &= ~lanes_below(t + 1, base, c);
+        int mine = na + below_lane(m[0]) + below_lane(m[1]) + below_lane(m[2]) + below_lane(m[3]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if ((m[c] >> lane) & 1ull) {
+            if (mine < ES_RUN) near[q][wave][mine] = base + 4 * lane + c;
+            ++mine;
+          }
+        na += __popcll(m[0]) + __popcll(m[1]) + __popcll(m[2]) + __popcll(m[3]);
+      }
+    }
+    if (lane == 0) nnear[q][wave] = min(na, ES_RUN);
+  }
+  // Marks before each thread's stretch of the bitmap (an odd stretch: its words lie in
+  // banks of their own).
+  const int per = ((words + NT - 1) / NT) | 1;
+  int nseg = 0;
   if (a.tokens) {
-    // (an odd stretch a thread: its words lie in banks of their own)
-    const int per = ((words + NT - 1) / NT) | 1, w0 = min(words, per * (int)threadIdx.x), w1 = min(words, w0 + per);
+    const int w0 = min(words, per * (int)threadIdx.x), w1 = min(words, w0 + per);
     int c = 0;
     for (int i = w0; i < w1; ++i) c += __popc(lds[i]);
-    int b = block_scan<NT>(c, part, &nseg);
-    for (int i = w0; i < w1; ++i) {
-      before[i] = b;
-      b += __popc(lds[i]);
-    }
+    stretch[threadIdx.x] = block_scan<NT>(c, part, &nseg);
   }
+  __syncthreads();
   // Wave q joins what the waves saw of position q: its number among its token's
   // occurrences, and the next RUN (one more than a run holds: whether another run follows).
   const int t = t0 + wave;
-  int kt = t < a.T ? __builtin_amdgcn_readfirstlane(a.ids[t]) : -1;
-  if (kt >= a.V) kt = -1;
-  int j = 0, found = 0;
+  const int kt = __builtin_amdgcn_readfirstlane(__shfl(ks, wave)), j = __builtin_amdgcn_readfirstlane(__shfl(jq, wave * W));
+  int found = 0;
   {
     const int c = lane < W ? nnear[wave][lane] : 0, inc = wave_scan(c, lane);
-    int jb = lane < W ? nbefore[wave][lane] : 0;
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) jb += __shfl_xor(jb, off);
-    j = __builtin_amdgcn_readfirstlane(jb);
     found = __builtin_amdgcn_readlane(inc, 63);
     for (int i = 0; i < c; ++i)
       if (inc - c + i < ES_RUN) list[wave][inc - c + i] = near[wave][lane][i];
@@ -621,17 +615,18 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
   const bool starts = kt >= 0 && j % ES_RUN == 0, first = j == 0, more = found >= ES_RUN;
   if (lane == 0) again[wave] = starts && (!first || more);
   __syncthreads();
-#pragma unroll
+#pragma unroll 1
   for (int q = 0; q < W; ++q) {
     if (!__builtin_amdgcn_readfirstlane(again[q])) continue;
+    const int k = __builtin_amdgcn_readlane(ks, q);
     int less = 0, equal = 0;
 #pragma unroll
     for (int u = 0; u < ES_U; ++u) {
       const int xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        less += __popcll(__ballot((unsigned)xs[c] < (unsigned)k[q]));
-        equal += __popcll(__ballot(xs[c] == k[q]));
+        less += __popcll(__ballot((unsigned)xs[c] < (unsigned)k));
+        equal += __popcll(__ballot(xs[c] == k));
       }
     }
     if (lane == 0) {
@@ -652,7 +647,14 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
     kind = first ? 1 : 2;
     row = first ? kt : (less + j) / ES_RUN;
     if (a.tokens && first) {
-      row = before[kt >> 5] + __popc(lds[kt >> 5] & ((1u << (kt & 31)) - 1u));
+      // (its stretch's marks before it, a word a lane)
+      const int word = kt >> 5, first_word = word / per * per;
+      int c = 0;
+      for (int i = first_word + lane; i <= word; i += 64)
+        c += __popc(i < word ? lds[i] : lds[i] & ((1u << (kt & 31)) - 1u));
+#pragma unroll
+      for (int off = 32; off >= 1; off >>= 1) c += __shfl_xor(c, off);
+      row = stretch[word / per] + c;
       if (lane == 0) a.tokens[row] = kt;
     }
     if (first && more && lane == 0) {
@@ -670,22 +672,24 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
     run[wave][2] = n;
   }
   __syncthreads();
-  auto sum = [&](auto nt, int tt, const int *l, int m, int kd, int64_t r) {
-    sum_run<E, decltype(nt)::value>(a, tt, l, m, kd == 1 ? a.out + r * a.D : a.slots + r * a.D, kd == 1 ? a.scale : 1.0f,
-                                    kd == 1 && a.accumulate);
-  };
+  auto dest = [&](int kd, int64_t r) { return kd == 1 ? a.out + r * a.D : a.slots + r * a.D; };
   row = __builtin_amdgcn_readfirstlane(row);
-  if (kind != 0 && n <= 1) sum(std::integral_constant<int, 64>(), t, list[wave], n, kind, row);
+  if (kind != 0 && n == 0)
+    sum_rows<E, 64, 1>(a, t, list[wave], n, dest(kind, row), kind == 1 ? a.scale : 1.0f, kind == 1 && a.accumulate);
+  if (kind != 0 && n == 1)
+    sum_rows<E, 64, 2>(a, t, list[wave], n, dest(kind, row), kind == 1 ? a.scale : 1.0f, kind == 1 && a.accumulate);
   if (a.tokens && t < a.cap && t >= nseg) {  // what no token reaches
     if (lane == 0) a.tokens[t] = -1;
     f32x4 *o = (f32x4 *)(a.out + (int64_t)t * a.D);
     for (int v = lane; v < a.D / 4; v += 64) o[v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
+#pragma unroll 1
   for (int q = 0; q < W; ++q) {
     const int kd = __builtin_amdgcn_readfirstlane(run[q][0]);
     if (kd != 0)
-      sum(std::integral_constant<int, NT>(), t0 + q, list[q], __builtin_amdgcn_readfirstlane(run[q][2]), kd,
-          __builtin_amdgcn_readfirstlane(run[q][1]));
+      sum_rows<E, NT, ES_RUN>(a, t0 + q, list[q], __builtin_amdgcn_readfirstlane(run[q][2]),
+                              dest(kd, __builtin_amdgcn_readfirstlane(run[q][1])), kd == 1 ? a.scale : 1.0f,
+                              kd == 1 && a.accumulate);
   }
   if (threadIdx.x == 0) {
     int m = 0;
@@ -757,9 +761,9 @@ hipError_t launch_embed_fwd(const void *table, const int32_t *ids, void *out, in
 }
 
 // Without a sort, compact form over 128256 x 3072 / 8192 x 512: 4096 positions 36 / 24 us (with
-// one 57 / 42), 6000 58 / 44 (61 / 44), 8192 74 / 54 (65 / 47).  The bitmap of up to 196608
-// tokens and its counts take 48 KB of LDS.
-constexpr int64_t EMBED_SCAN_T = 6144, EMBED_SCAN_V = 196608;
+// one 57 / 42), 6000 58 / 44 (61 / 44), 8192 74 / 54 (65 / 47).  The bitmap of up to 262144
+// tokens takes 32 KB of LDS.
+constexpr int64_t EMBED_SCAN_T = 6144, EMBED_SCAN_V = 262144;
 
 static size_t up256(size_t b) { return (b + 255) & ~size_t(255); }
 
@@ -866,7 +870,7 @@ hipError_t launch_embed_scan(const int32_t *ids, const void *dout, float *out, i
     if ((int64_t)V * D < (64 << 20)) own = (V + 63) / 64;
     else clear(out, V, D, st);
   }
-  const size_t lds = tokens ? (size_t)((V + 31) / 32) * 8 : 8;
+  const size_t lds = tokens ? (size_t)((V + 31) / 32) * 4 : 8;
   if (d == DT_BF16) embed_scan<BF16>(a, p, own, lds, st);
   else embed_scan<F32>(a, p, own, lds, st);
   if (T > ES_RUN) {  // (at most T / (RUN + 1) tokens have a second run)

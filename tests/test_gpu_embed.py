@@ -64,7 +64,7 @@ def _check_grad(got, ids, dout, V, scale, base=None):
 
 
 CASES = [(1, 1, 8), (1, 1000, 64), (2, 3, 24), (8, 50, 136), (9, 50, 136), (64, 40, 1032), (65, 700, 2048), (257, 513, 72),
-         (1023, 1000, 64), (2048, 511, 40), (2049, 512, 40), (4100, 30000, 72), (6144, 700, 16), (6145, 5000, 16), (8193, 300000, 16), (300, 196609, 24),
+         (1023, 1000, 64), (2048, 511, 40), (2049, 512, 40), (4100, 30000, 72), (6144, 700, 16), (6145, 5000, 16), (8193, 300000, 16), (300, 262145, 24), (300, 262144, 24),
          (20011, 130001, 16), (32769, 600, 8), (70001, 900, 8)]
 
 
@@ -136,6 +136,39 @@ def test_repeatable_and_ordered_on_its_stream():
     lm.embed_bwd(ids, dout, b, stream=st)
     torch.cuda.current_stream().wait_stream(st)
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T", [300, 9000])  # without and with a sort
+def test_graph_replays(T):
+    """A captured lookup and its gradients replay on changed tokens."""
+    _announce(f"embed graph T={T}")
+    g = torch.Generator().manual_seed(T)
+    V, D = 800, 40
+    table, dout = torch.randn(V, D, generator=g).cuda(), torch.randn(T, D, generator=g).cuda()
+    ids, out = torch.zeros(T, dtype=torch.int32, device="cuda"), torch.empty(T, D, device="cuda")
+    n = min(T, V)
+    dense, rows, tokens = torch.empty(V, D, device="cuda"), torch.empty(n, D, device="cuda"), torch.empty(n, dtype=torch.int32, device="cuda")
+    ws = torch.empty(lm.embed_bwd_workspace_bytes(T, V, D), dtype=torch.uint8, device="cuda")
+
+    def call():
+        lm.embed_fwd(table, ids, out)
+        lm.embed_bwd(ids, dout, dense, ws=ws)
+        lm.embed_bwd_rows(ids, dout, V, tokens, rows, ws=ws)
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for kind in ("uniform", "text", "same", "outside", "uniform"):
+        ids.copy_(_ids(T, V, kind, g))
+        call()
+        want = [t.clone() for t in (out, dense, rows, tokens)]
+        for t in (out, dense, rows, tokens):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (out, dense, rows, tokens)))
 
 
 def test_infinities_stay_in_their_row():

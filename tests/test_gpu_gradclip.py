@@ -122,6 +122,25 @@ def test_list_follows_the_buffers_and_repeats():
     assert not torch.equal(seen[0][0], seen[1][0])
 
 
+@pytest.mark.parametrize("n", [5000, 500001])  # one launch and two
+def test_graph_replays(n):
+    _announce(f"clip graph {n}")
+    buf, out, res = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty(2, device="cuda")
+    gl = lm.grad_list([buf], [out])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lm.grad_clip(gl, 1.0, res)
+    for seed in range(4):
+        buf.normal_(std=10.0 ** (seed - 4))
+        lm.grad_clip(gl, 1.0, res)
+        want = out.clone(), res.clone()
+        out.zero_(), res.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(res, want[1])
+
+
 def test_python_refusals():
     a = torch.ones(8, device="cuda")
     with pytest.raises(lm.LoraError):
