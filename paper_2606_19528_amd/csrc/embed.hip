@@ -29,7 +29,7 @@ template <typename E>
 __global__ __launch_bounds__(EF_NT) void embed_fwd_kernel(const typename E::T *table, const int32_t *ids,
                                                           typename E::T *out, int T, int V, int vpr, unsigned per_row,
                                                           float scale) {
-  const unsigned w = blockIdx.x * (EF_NT / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const unsigned w = blockIdx.x * (EF_NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const unsigned t = w / per_row;
   if (t >= (unsigned)T) return;
   const int v0 = (w % per_row) * 64 * EF_U + lane;
@@ -491,7 +491,8 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
   __shared__ int run[W][3];  // 1: the token's row, 2: a slot, 0: none; its number; rows after the first
   __shared__ int hot[W][3], again[W];
   __shared__ int part[W];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // (the wave's number is read into a scalar, so that what hangs on it stays in scalar registers)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x >= a.nwg) {  // dense form, not cleared ahead: the rows of 64 tokens that do not occur
     const int64_t r0 = (int64_t)(blockIdx.x - a.nwg) * 64;
     uint32_t *mask = lds;
@@ -713,7 +714,7 @@ __global__ __launch_bounds__(EJ_NT) void embed_slots_kernel(EmbedScan a, int per
   __shared__ int first[EJ_NT];  // number of the workgroup's first item
   __shared__ int part[EJ_WAVES];
   __shared__ f32x4 red[EJ_WAVES][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int total;
   first[threadIdx.x] = block_scan<EJ_NT>((int)threadIdx.x < a.nwg ? a.nhot[threadIdx.x] : 0, part, &total);
   __syncthreads();
@@ -760,10 +761,10 @@ hipError_t launch_embed_fwd(const void *table, const int32_t *ids, void *out, in
   return hipGetLastError();
 }
 
-// Without a sort, compact form over 128256 x 3072 / 8192 x 512: 4096 positions 36 / 24 us (with
-// one 57 / 42), 6000 58 / 44 (61 / 44), 8192 74 / 54 (65 / 47).  The bitmap of up to 262144
-// tokens takes 32 KB of LDS.
-constexpr int64_t EMBED_SCAN_T = 6144, EMBED_SCAN_V = 262144;
+// Without a sort, compact form over 128256 x 3072 / 8192 x 512: 4096 positions 34 / 23 us (with
+// one 57 / 42), 6000 45 / 32 (61 / 44), 8192 59 / 44 (66 / 50); a lane holds 16
+// tokens of a workgroup of 512.  The bitmap of up to 262144 tokens takes 32 KB of LDS.
+constexpr int64_t EMBED_SCAN_T = 8192, EMBED_SCAN_V = 262144;
 
 static size_t up256(size_t b) { return (b + 255) & ~size_t(255); }
 
