@@ -396,7 +396,7 @@ __global__ __launch_bounds__(EG_COL) void embed_join_kernel(EmbedGrad a) {
 }
 
 // ---- few positions: no sort ------------------------------------------------------------
-// The occurrences of a token, in ascending t, are cut into runs of RUN, and the
+// The occurrences of a token, in ascending t, are cut into runs of RUN = 8, and the
 // rows of a run are summed by the workgroup of the position that starts it.  The
 // first run's sum is the token's row; a later run's goes to a slot of its own,
 // and the join launch adds the slots of a token.
@@ -412,8 +412,15 @@ __global__ __launch_bounds__(EG_COL) void embed_join_kernel(EmbedGrad a) {
 // at a copy's rate).  At 64 columns 18 remain, a chain in each workgroup: loads 0.6, bitmap and
 // its counts 4, comparisons 3, joins 2, rows 3.  More positions a workgroup (8 instead of 4: 37
 // us in all for 36, and 24 against 20 at 512 positions) lengthen it.
-constexpr int ES_RUN = 8, ES_COLS = 256;  // columns of an item of the join launch
-constexpr int ES_U = 4;                   // a lane holds 4 ES_U tokens: T <= 16 NT
+constexpr int ES_RUN = 8, ES_BATCH = 8;  // rows of a run, and of those that a thread loads at once
+constexpr int ES_COLS = 256;  // columns of an item of the join launch
+// Up to this many positions a run holds all of a token's, and one launch does.  32 distinct
+// tokens: 11.9 us for 14.6 with the second launch (3072 columns), 15.4 for 18.0 (8192); four
+// tokens 8 times each 16.5 for 19.2 and 23.7 for 26.5.  One token 32 times, in a workgroup
+// alone, loses: 17.6 for 15.4 and 30.8 for 17.7.  At 64 the repeated ones lose more (four
+// tokens 16 times 54.7 for 30.4) than distinct ones gain.
+constexpr int ES_FEW = 32;
+constexpr int ES_U = 4;  // a lane holds 4 ES_U tokens: T <= 16 NT
 
 struct EmbedScan {
   const int32_t *ids;
@@ -479,15 +486,37 @@ __device__ __forceinline__ void sum_rows(const EmbedScan &a, int t, const int *l
     *o = add ? s + *o : s;
   }
 }
+// The same for more rows, ES_BATCH at a time.
 template <typename E, int NT>
+__device__ __forceinline__ void sum_long(const EmbedScan &a, int t, const int *list, int n, float *dst, float scale, bool add) {
+  const int64_t bytes = (int64_t)a.D * sizeof(typename E::T);
+  const char *x = (const char *)a.dout;
+  for (int v = threadIdx.x & (NT - 1); v < a.D / 4; v += NT) {
+    f32x4 s = row4(E(), x + t * bytes, v);
+    for (int b = 0; b < n; b += ES_BATCH) {
+      f32x4 f[ES_BATCH];
+#pragma unroll
+      for (int u = 0; u < ES_BATCH; ++u)
+        f[u] = row4(E(), x + (int64_t)__builtin_amdgcn_readfirstlane(list[min(b + u, n - 1)]) * bytes, v);
+#pragma unroll
+      for (int u = 0; u < ES_BATCH; ++u) s += b + u < n ? f[u] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    s *= scale;
+    f32x4 *o = (f32x4 *)dst + v;
+    *o = add ? s + *o : s;
+  }
+}
+
+// RUN is ES_RUN, or ES_FEW for T <= ES_FEW, where no token has a second run.
+template <typename E, int NT, int RUN>
 __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
   constexpr int W = NT / 64;
   extern __shared__ uint32_t lds[];  // compact form: bitmap words
   __shared__ int stretch[NT];        // and the marks before each thread's
-  __shared__ int near[W][W][ES_RUN];  // of position q, as wave w sees it: the next occurrences in its part,
+  __shared__ int near[W][W][RUN];  // of position q, as wave w sees it: the next occurrences in its part,
   __shared__ int nnear[W][W], nbefore[W][W];  // how many of them, how many before q
   __shared__ int nless[W][W], nequal[W][W];
-  __shared__ int list[W][ES_RUN];
+  __shared__ int list[W][RUN];
   __shared__ int run[W][3];  // 1: the token's row, 2: a slot, 0: none; its number; rows after the first
   __shared__ int hot[W][3], again[W];
   __shared__ int part[W];
@@ -569,11 +598,11 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
   for (int q = 0; q < W; ++q) {
     const int t = t0 + q, k = __builtin_amdgcn_readlane(ks, q);
     int na = 0;
-    if (k >= 0 && __builtin_amdgcn_readlane(jq, q * W) % ES_RUN == 0) {
+    if (k >= 0 && __builtin_amdgcn_readlane(jq, q * W) % RUN == 0) {
 #pragma unroll
       for (int u = 0; u < ES_U; ++u) {
         const int base = p0 + u * 256;
-        if (base + 256 <= t || na >= ES_RUN) continue;
+        if (base + 256 <= t || na >= RUN) continue;
         uint64_t m[4] = {__ballot(x[u].x == k), __ballot(x[u].y == k), __ballot(x[u].z == k), __ballot(x[u].w == k)};
         if ((m[0] | m[1] | m[2] | m[3]) == 0) continue;
         if (base <= t)
@@ -583,13 +612,13 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
           if ((m[c] >> lane) & 1ull) {
-            if (mine < ES_RUN) near[q][wave][mine] = base + 4 * lane + c;
+            if (mine < RUN) near[q][wave][mine] = base + 4 * lane + c;
             ++mine;
           }
         na += __popcll(m[0]) + __popcll(m[1]) + __popcll(m[2]) + __popcll(m[3]);
       }
     }
-    if (lane == 0) nnear[q][wave] = min(na, ES_RUN);
+    if (lane == 0) nnear[q][wave] = min(na, RUN);
   }
   // Marks before each thread's stretch of the bitmap (an odd stretch: its words lie in
   // banks of their own).
@@ -611,9 +640,9 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
     const int c = lane < W ? nnear[wave][lane] : 0, inc = wave_scan(c, lane);
     found = __builtin_amdgcn_readlane(inc, 63);
     for (int i = 0; i < c; ++i)
-      if (inc - c + i < ES_RUN) list[wave][inc - c + i] = near[wave][lane][i];
+      if (inc - c + i < RUN) list[wave][inc - c + i] = near[wave][lane][i];
   }
-  const bool starts = kt >= 0 && j % ES_RUN == 0, first = j == 0, more = found >= ES_RUN;
+  const bool starts = kt >= 0 && j % RUN == 0, first = j == 0, more = found >= RUN;
   if (lane == 0) again[wave] = starts && (!first || more);
   __syncthreads();
 #pragma unroll 1
@@ -646,7 +675,7 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
         equal += nequal[wave][w];
       }
     kind = first ? 1 : 2;
-    row = first ? kt : (less + j) / ES_RUN;
+    row = first ? kt : (less + j) / RUN;
     if (a.tokens && first) {
       // (its stretch's marks before it, a word a lane)
       const int word = kt >> 5, first_word = word / per * per;
@@ -660,11 +689,11 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
     }
     if (first && more && lane == 0) {
       hot[wave][0] = row;
-      hot[wave][1] = (less + ES_RUN) / ES_RUN;
-      hot[wave][2] = (equal - 1) / ES_RUN;
+      hot[wave][1] = (less + RUN) / RUN;
+      hot[wave][2] = (equal - 1) / RUN;
     }
   }
-  const int n = min(found, ES_RUN - 1);
+  const int n = min(found, RUN - 1);
   // Runs of one or two rows: each wave its own.  Longer ones: all waves, a part of the
   // columns each (a wave alone took 12 rounds of eight loads for 3072 columns).
   if (lane == 0) {
@@ -687,10 +716,13 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
 #pragma unroll 1
   for (int q = 0; q < W; ++q) {
     const int kd = __builtin_amdgcn_readfirstlane(run[q][0]);
-    if (kd != 0)
-      sum_rows<E, NT, ES_RUN>(a, t0 + q, list[q], __builtin_amdgcn_readfirstlane(run[q][2]),
-                              dest(kd, __builtin_amdgcn_readfirstlane(run[q][1])), kd == 1 ? a.scale : 1.0f,
-                              kd == 1 && a.accumulate);
+    if (kd == 0) continue;
+    const int m = __builtin_amdgcn_readfirstlane(run[q][2]);
+    float *dst = dest(kd, __builtin_amdgcn_readfirstlane(run[q][1]));
+    const float f = kd == 1 ? a.scale : 1.0f;
+    const bool add = kd == 1 && a.accumulate;
+    if (RUN <= ES_BATCH || m < ES_BATCH) sum_rows<E, NT, ES_BATCH>(a, t0 + q, list[q], m, dst, f, add);
+    else sum_long<E, NT>(a, t0 + q, list[q], m, dst, f, add);
   }
   if (threadIdx.x == 0) {
     int m = 0;
@@ -843,8 +875,9 @@ hipError_t launch_embed_sort(const int32_t *ids, int T, int V, const EmbedPlan &
 template <typename E>
 static void embed_scan(const EmbedScan &a, const EmbedPlan &p, int own, size_t lds, hipStream_t st) {
   const dim3 grid((unsigned)(p.nwg + own));
-  if (p.per_wg == 4) hipLaunchKernelGGL((embed_scan_kernel<E, 256>), grid, dim3(256), lds, st, a);
-  else hipLaunchKernelGGL((embed_scan_kernel<E, 512>), grid, dim3(512), lds, st, a);
+  if (a.T <= ES_FEW) hipLaunchKernelGGL((embed_scan_kernel<E, 256, ES_FEW>), grid, dim3(256), lds, st, a);
+  else if (p.per_wg == 4) hipLaunchKernelGGL((embed_scan_kernel<E, 256, ES_RUN>), grid, dim3(256), lds, st, a);
+  else hipLaunchKernelGGL((embed_scan_kernel<E, 512, ES_RUN>), grid, dim3(512), lds, st, a);
 }
 
 hipError_t launch_embed_scan(const int32_t *ids, const void *dout, float *out, int32_t *tokens, int T, int V, int D, float scale,
@@ -874,7 +907,7 @@ hipError_t launch_embed_scan(const int32_t *ids, const void *dout, float *out, i
   const size_t lds = tokens ? (size_t)((V + 31) / 32) * 4 : 8;
   if (d == DT_BF16) embed_scan<BF16>(a, p, own, lds, st);
   else embed_scan<F32>(a, p, own, lds, st);
-  if (T > ES_RUN) {  // (at most T / (RUN + 1) tokens have a second run)
+  if (T > ES_FEW) {  // (at most T / (RUN + 1) tokens have a second run)
     const int64_t items = (int64_t)(T / (ES_RUN + 1)) * ((D + ES_COLS - 1) / ES_COLS);
     hipLaunchKernelGGL(embed_slots_kernel, dim3((unsigned)std::min<int64_t>(EJ_GRID, items)), dim3(EJ_NT), 0, st, a, p.per_wg);
   }
