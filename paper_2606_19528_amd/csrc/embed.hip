@@ -396,7 +396,7 @@ __global__ __launch_bounds__(EG_COL) void embed_join_kernel(EmbedGrad a) {
 }
 
 // ---- few positions: no sort ------------------------------------------------------------
-// The occurrences of a token, in ascending t, are cut into runs of RUN = 8, and the
+// The occurrences of a token, in ascending t, are cut into runs of RUN, and the
 // rows of a run are summed by the workgroup of the position that starts it.  The
 // first run's sum is the token's row; a later run's goes to a slot of its own,
 // and the join launch adds the slots of a token.
@@ -420,6 +420,9 @@ constexpr int ES_COLS = 256;  // columns of an item of the join launch
 // alone, loses: 17.6 for 15.4 and 30.8 for 17.7.  At 64 the repeated ones lose more (four
 // tokens 16 times 54.7 for 30.4) than distinct ones gain.
 constexpr int ES_FEW = 32;
+// Rows that a workgroup of the dense form clears, a bit each: 14913 x 1392 15.5 us, 64 rows 18.0;
+// 16 and 8 alike, but 8192 positions of 50257 x 768 take 39.9, 41.5 and 49.4.
+constexpr int ES_CLEAR = 32;
 constexpr int ES_U = 4;  // a lane holds 4 ES_U tokens: T <= 16 NT
 
 struct EmbedScan {
@@ -522,25 +525,23 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
   __shared__ int part[W];
   // (the wave's number is read into a scalar, so that what hangs on it stays in scalar registers)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if ((int)blockIdx.x >= a.nwg) {  // dense form, not cleared ahead: the rows of 64 tokens that do not occur
-    const int64_t r0 = (int64_t)(blockIdx.x - a.nwg) * 64;
-    uint32_t *mask = lds;
-    if (threadIdx.x < 2) mask[threadIdx.x] = 0;
+  if ((int)blockIdx.x >= a.nwg) {  // dense form, not cleared ahead: the rows of ES_CLEAR tokens that do not occur
+    const int r0 = (int)(blockIdx.x - a.nwg) * ES_CLEAR;
+    if (threadIdx.x == 0) lds[0] = 0;
     __syncthreads();
     for (int i = threadIdx.x * 4; i < a.T; i += NT * 4) {
       const int4 k = ids4(a.ids, i - 4 * lane, lane, a.T);
       const int kk[4] = {k.x, k.y, k.z, k.w};
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int64_t d = (int64_t)kk[c] - r0;
-        if (d >= 0 && d < 64) atomicOr(&mask[d >> 5], 1u << (d & 31));
-      }
+      for (int c = 0; c < 4; ++c)
+        if (kk[c] >= r0 && kk[c] - r0 < ES_CLEAR) atomicOr(&lds[0], 1u << (kk[c] - r0));
     }
     __syncthreads();
-    const int rows = (int)min((int64_t)64, a.V - r0);
+    const uint32_t mask = lds[0];
+    const int rows = min(ES_CLEAR, a.V - r0);
     for (int r = wave; r < rows; r += W) {
-      if ((mask[r >> 5] >> (r & 31)) & 1u) continue;
-      f32x4 *o = (f32x4 *)(a.out + (r0 + r) * a.D);
+      if ((mask >> r) & 1u) continue;
+      f32x4 *o = (f32x4 *)(a.out + (int64_t)(r0 + r) * a.D);
       for (int v = lane; v < a.D / 4; v += 64) o[v] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
     return;
@@ -901,10 +902,10 @@ hipError_t launch_embed_scan(const int32_t *ids, const void *dout, float *out, i
   // hides the search for the tokens; a larger one ahead of them, at the higher rate.
   int own = 0;
   if (!accumulate && !tokens) {
-    if ((int64_t)V * D < (64 << 20)) own = (V + 63) / 64;
+    if ((int64_t)V * D < (64 << 20)) own = (V + ES_CLEAR - 1) / ES_CLEAR;
     else clear(out, V, D, st);
   }
-  const size_t lds = tokens ? (size_t)((V + 31) / 32) * 4 : 8;
+  const size_t lds = tokens ? (size_t)((V + 31) / 32) * 4 : 4;
   if (d == DT_BF16) embed_scan<BF16>(a, p, own, lds, st);
   else embed_scan<F32>(a, p, own, lds, st);
   if (T > ES_FEW) {  // (at most T / (RUN + 1) tokens have a second run)

@@ -64,7 +64,7 @@ def _check_grad(got, ids, dout, V, scale, base=None):
 
 
 CASES = [(1, 1, 8), (1, 1000, 64), (2, 3, 24), (8, 50, 136), (9, 50, 136), (64, 40, 1032), (32, 1, 2048), (31, 3, 24), (33, 2, 1032), (65, 700, 2048), (257, 513, 72),
-         (1023, 1000, 64), (2048, 511, 40), (2049, 512, 40), (4100, 30000, 72), (6144, 700, 16), (6145, 5000, 16), (8193, 300000, 16), (300, 262145, 24), (300, 262144, 24),
+         (1023, 1000, 64), (2048, 511, 40), (2049, 512, 40), (4100, 30000, 72), (6144, 700, 16), (6145, 5000, 16), (8200, 1024, 16), (8193, 300000, 16), (8300, 262144, 8), (300, 262145, 24), (300, 262144, 24),
          (20011, 130001, 16), (32769, 600, 8), (70001, 900, 8)]
 
 
