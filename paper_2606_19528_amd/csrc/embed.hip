@@ -411,7 +411,7 @@ __global__ __launch_bounds__(EG_COL) void embed_join_kernel(EmbedGrad a) {
 // 4096 positions of 128256 x 3072, frequencies of a text: 27 us and 7 for the join (75 MB, 15 us
 // at a copy's rate).  At 64 columns 18 remain, a chain in each workgroup: loads 0.6, bitmap and
 // its counts 4, comparisons 3, joins 2, rows 3.  More positions a workgroup (8 instead of 4: 37
-// us in all for 36, and 24 against 20 at 512 positions) lengthen it.
+// us in all for 34, and 24 against 20 at 512 positions) lengthen it.
 constexpr int ES_RUN = 8, ES_BATCH = 8;  // rows of a run, and of those that a thread loads at once
 constexpr int ES_COLS = 256;  // columns of an item of the join launch
 // Up to this many positions a run holds all of a token's, and one launch does.  32 distinct
@@ -739,7 +739,7 @@ __global__ __launch_bounds__(NT) void embed_scan_kernel(EmbedScan a) {
 }
 
 // Adds the slots of the tokens with more than one run to their rows (half as many
-// workgroups: 38 us for both launches of the case above, instead of 36).  An item is
+// workgroups: 36 us for both launches of the case above, instead of 34).  An item is
 // a token and ES_COLS columns; the waves take consecutive ranges of its slots,
 // whose sums are added in their order.
 constexpr int EJ_NT = 1024, EJ_WAVES = EJ_NT / 64, EJ_GRID = 512;
