@@ -19,6 +19,7 @@
 namespace lora {
 
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2eRest = 1.925963033500011e-8f;  // log2 e - kLog2e
 
 // Running maximum and sum of exp(z - m).  A lane that has seen nothing (or only
 // -inf) has m = -inf and s = 0 (exponents are taken from 0 then).
@@ -26,7 +27,15 @@ struct Stat {
   float m, s;
 };
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
-__device__ __forceinline__ float exp_diff(float z, float m) { return __builtin_amdgcn_exp2f((z - m) * kLog2e); }
+// exp(z - m).  Scaled by kLog2e alone every term would be high by 1.3e-8 (m - z) of itself, and
+// log s by that times the mean of m - z: about 6e-8 in every row of a decoder's logits, which
+// a margin, a difference of sums over rows, adds up instead of averaging.
+__device__ __forceinline__ float exp_diff(float z, float m) {
+  const float d = z - m;
+  return __builtin_amdgcn_exp2f(fmaf(d, kLog2e, d * kLog2eRest));
+}
+// The same where it is one element's factor (dz): the offset is below the rounding of the product.
+__device__ __forceinline__ float exp_diff_fast(float z, float m) { return __builtin_amdgcn_exp2f((z - m) * kLog2e); }
 __device__ __forceinline__ Stat stat_join(Stat a, Stat b) {
   const float m = fmaxf(a.m, b.m), r = finite_max(m);
   return {m, a.s * exp_diff(a.m, r) + b.s * exp_diff(b.m, r)};
@@ -100,7 +109,7 @@ __device__ __forceinline__ u32x4 dz_vec(u32x4 x, int i, float m, float k, float 
   float f[E::VEC];
   unpack_vec(E(), x, f);
 #pragma unroll
-  for (int e = 0; e < E::VEC; ++e) f[e] = k * exp_diff(f[e], m);
+  for (int e = 0; e < E::VEC; ++e) f[e] = k * exp_diff_fast(f[e], m);
   const int ye = y - i * E::VEC;
   if ((unsigned)ye < (unsigned)E::VEC) {
 #pragma unroll
@@ -405,7 +414,8 @@ template <typename E, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void policy_rows_kernel(TokenLoss a, PolicyArgs p) {
   __shared__ Stat red[NT / 64 < 1 ? 1 : NT / 64];
   const int nz = (a.V + E::VEC - 1) / E::VEC, nv = (int)(a.ld / E::VEC);
-  const int tid = threadIdx.x, off = tid * 16;
+  int tid = threadIdx.x;
+  const int off = tid * 16;
   constexpr int LAG = NV < 5 ? NV : 5;
   constexpr int SPAN = NT * E::VEC;  // elements of one vector of every thread
   u32x4 x[NV];
@@ -444,7 +454,8 @@ __global__ __launch_bounds__(NT, 4) void policy_rows_kernel(TokenLoss a, PolicyA
 #pragma unroll
   for (int v = 0; v < NV; ++v) take(v);
   while (t < a.T) {
-    asm volatile("" : "+s"(V));  // (what depends on V is recomputed for each row, not kept in registers)
+    // (what depends on V and on the thread's columns is recomputed for each row, not kept in registers)
+    asm volatile("" : "+s"(V), "+v"(tid));
     const u32x4 *zrow = row_ptr<E>(a, t);
 #pragma unroll 4
     for (int i = NV * NT + tid; i < nz; i += NT) {
