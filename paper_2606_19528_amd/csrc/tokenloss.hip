@@ -11,6 +11,7 @@
 // log s and logp would be most of the error of a margin, a difference of sums of logp.
 // Rows of weight 0 are not read; their logp is 0 and their gradient a row of zeros.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.hpp"
 #include "launch.hpp"
@@ -40,10 +41,29 @@ __device__ __forceinline__ Stat stat_join(Stat a, Stat b) {
   const float m = fmaxf(a.m, b.m), r = finite_max(m);
   return {m, a.s * exp_diff(a.m, r) + b.s * exp_diff(b.m, r)};
 }
-__device__ __forceinline__ Stat wave_stat(Stat a) {
+// U statistics, each joined over groups of `width` lanes (a power of two).  First to the common
+// maximum, then plain sums: both give every lane the same bits, since a + b = b + a.  (A
+// multiply-add of the lane's own product and its partner's rounded one rounds differently in the
+// two lanes, and lanes that take different sides of a clip leave a row of dz partly zero.)
+template <int U>
+__device__ __forceinline__ void group_stats(Stat (&x)[U], int width) {
+#pragma clang fp contract(off)
+  float m[U];
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) a = stat_join(a, Stat{__shfl_xor(a.m, off), __shfl_xor(a.s, off)});
-  return a;
+  for (int u = 0; u < U; ++u) m[u] = x[u].m;
+  for (int off = width >> 1; off >= 1; off >>= 1)
+#pragma unroll
+    for (int u = 0; u < U; ++u) m[u] = fmaxf(m[u], __shfl_xor(m[u], off));
+#pragma unroll
+  for (int u = 0; u < U; ++u) x[u] = {m[u], x[u].s * exp_diff(x[u].m, finite_max(m[u]))};
+  for (int off = width >> 1; off >= 1; off >>= 1)
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u].s += __shfl_xor(x[u].s, off);
+}
+__device__ __forceinline__ Stat wave_stat(Stat a) {
+  Stat x[1] = {a};
+  group_stats<1>(x, 64);
+  return x[0];
 }
 template <int N>
 __device__ __forceinline__ float max_of(const float *f) {
@@ -200,7 +220,7 @@ __global__ __launch_bounds__(TL_NT) void token_stat_kernel(TokenLoss a, Stat *st
 }
 
 // A row's statistics from those of its parts (at most 64): in every lane of a
-// wave, or by one thread.
+// wave, the same bits, or by one thread.
 __device__ __forceinline__ Stat joined_stat(const TokenLoss &a, const Stat *stat, int64_t t) {
   const int lane = threadIdx.x & 63;
   return wave_stat(lane < a.parts ? stat[t * a.parts + lane] : Stat{-INFINITY, 0.0f});
@@ -301,22 +321,55 @@ __device__ __forceinline__ void write_dz(const TokenLoss &a, int64_t t, int p, S
   for (; i < end; i += TL_NT) put_dz<NTS>(zero16(), out + i);
 }
 
+// From this many rows on, rows in registers; fewer in parts (128256 bf16: 256 rows 36 and 48 us,
+// 128 rows 31 and 30; 32000 and shorter rows alike).
+constexpr int POLICY_ROWS = 192;
+static_assert(POLICY_ROWS <= TL_NT, "a thread a row");
+
 // Bound by launches and latency: 97 x 8192 fp32 3.8 + 4.6 us on the GPU, 12 a call.
 // Policy loss of few rows, after token_stat_kernel: each workgroup writes one
-// part of a row of dz; the last one sums the loss, a thread a row.
+// part of a row of dz; ahead of them the first one sums the loss, and LOSS_WGS - 1 end at once:
+// a part is read again on the XCD, one of 8 in turn, whose cache has it from the statistics (60 x
+// 151936 fp32 20.3 us a call, 21.9 with one workgroup ahead).
+constexpr int LOSS_WGS = 8;
 template <typename E>
 __global__ __launch_bounds__(TL_NT) void policy_parts_kernel(TokenLoss a, PolicyArgs p, const Stat *stat) {
   __shared__ double red[TL_NT / 64];
-  if (blockIdx.x == gridDim.x - 1) {
+  __shared__ Stat rows[POLICY_ROWS];
+  if (blockIdx.x == 0) {
+    // Statistics of the rows, `width` lanes each, joined as joined_stat does (empty lanes change
+    // no bits), so that the loss takes the same side of the clip as dz; then a thread a row.
+    constexpr int WAVES = TL_NT / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int width = a.parts > 1 ? 1 << (32 - __clz(a.parts - 1)) : 1, per = 64 / width, part = lane % width;
+    int t0 = wave * per + lane / width;
+    auto join = [&](auto n) {  // n rows of each group of lanes at once
+      constexpr int U = decltype(n)::value;
+      Stat x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = stat[min(t0 + u * WAVES * per, a.T - 1) * a.parts + min(part, a.parts - 1)];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (part >= a.parts) x[u] = Stat{-INFINITY, 0.0f};
+      group_stats<U>(x, width);
+#pragma unroll
+      for (int u = 0; u < U; ++u, t0 += WAVES * per)
+        if (part == 0 && t0 < a.T) rows[t0] = x[u];
+    };
+    int left = (a.T + WAVES * per - 1) / (WAVES * per);
+    for (; left > 2; left -= 8) join(std::integral_constant<int, 8>());
+    if (left > 0) join(std::integral_constant<int, 2>());
+    __syncthreads();
     double sum = 0.0;
-    for (int64_t t = threadIdx.x; t < a.T; t += TL_NT) {
+    const int t = threadIdx.x;
+    if (t < a.T) {
       const float w = weight(a, t);
       double logp = 0.0;
       if (w != 0.0f) {
         float l, g;
-        logp = logp_of(a.ztgt[t], thread_stat(a, stat, t));
+        logp = logp_of(a.ztgt[t], rows[t]);
         policy_terms(p, t, logp, &l, &g);
-        sum += w * l;
+        sum = w * l;
       }
       a.logp[t] = (float)logp;
     }
@@ -324,7 +377,9 @@ __global__ __launch_bounds__(TL_NT) void policy_parts_kernel(TokenLoss a, Policy
     if (threadIdx.x == 0) a.loss[0] = (float)sum;
     return;
   }
-  const int64_t t = blockIdx.x / a.parts;
+  if (blockIdx.x < LOSS_WGS) return;
+  const unsigned b = blockIdx.x - LOSS_WGS;
+  const int64_t t = b / a.parts;
   const float w = weight(a, t);
   Stat st{0.0f, 1.0f};
   float c = 0.0f;
@@ -336,7 +391,7 @@ __global__ __launch_bounds__(TL_NT) void policy_parts_kernel(TokenLoss a, Policy
     c = w * g;
     y = a.y[t];
   }
-  write_dz<E, false>(a, t, blockIdx.x % a.parts, st, c, y);
+  write_dz<E, false>(a, t, b % a.parts, st, c, y);
 }
 
 // softplus(x) = log(1 + exp x)
@@ -545,16 +600,13 @@ static void policy_rows(const TokenLoss &a, const PolicyArgs &p, int per_cu, hip
   hipLaunchKernelGGL((policy_rows_kernel<E, NT, NV>), dim3(grid), dim3(NT), 0, st, a, p);
 }
 
-// From this many rows on, rows in registers; fewer in parts (128256 bf16: 256 rows 36 and 48 us,
-// 128 rows 31 and 30; 32000 and shorter rows alike).
-constexpr int POLICY_ROWS = 192;
 template <typename E>
 static void policy_launches(const TokenLoss &a, const PolicyArgs &p, hipStream_t st) {
   if (a.T < POLICY_ROWS && a.parts > 1) {
     Stat *stat = (Stat *)a.stat;
     hipLaunchKernelGGL(token_stat_kernel<E>, dim3((unsigned)((int64_t)a.T * a.parts)), dim3(TL_NT), 0, st, a, stat);
-    hipLaunchKernelGGL(policy_parts_kernel<E>, dim3((unsigned)(a.dz ? (int64_t)a.T * a.parts + 1 : 1)), dim3(TL_NT), 0, st, a,
-                       p, stat);
+    hipLaunchKernelGGL(policy_parts_kernel<E>, dim3((unsigned)(a.dz ? (int64_t)a.T * a.parts + LOSS_WGS : 1)), dim3(TL_NT), 0,
+                       st, a, p, stat);
     return;
   }
   const int nz = (a.V + E::VEC - 1) / E::VEC;

@@ -1,5 +1,5 @@
 """Token losses where an error of one rounding decides or adds up: margins over many
-rows."""
+rows, positions at the edge of the clip."""
 import sys
 
 import pytest
@@ -52,3 +52,46 @@ def test_margin_has_no_common_offset(V, dt):
     want = beta * float(d[:chosen].sum() - d[chosen:].sum())
     tol = beta * R.U * (0.2 * (2 * chosen - n) + 6 * 1.5 * n ** 0.5) + 2 * R.U * abs(want)
     assert abs(float(M[0]) - want) <= tol, (float(M[0]) - want, tol)
+
+
+def _at_the_edge(T, V, dt, sign, seed):
+    """A policy loss with clip_lo = clip_hi = 0 right after the rollout: old_logp is the current
+    logp rounded to fp32, so every ratio is 1 within a few roundings and the branch of every
+    position hangs on them."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    z = (torch.randn(T, V, generator=g, device="cuda") * 2.0).to(dt)
+    y = torch.randint(0, V, (T,), generator=g, dtype=torch.int32, device="cuda")
+    adv, old = torch.full((T,), sign, device="cuda"), torch.empty(T, device="cuda")
+    L, dz = torch.empty(1, device="cuda"), torch.empty_like(z)
+    lm.policy_loss(z, y, None, adv, torch.zeros(T, device="cuda"), None, L, old)  # (old: logp)
+    lm.policy_loss(z, y, None, adv, old, None, L, torch.empty(T, device="cuda"), dz, clip_lo=0.0, clip_hi=0.0)
+    return float(L[0]), dz
+
+
+# rows in one wave's registers, in a workgroup's, and in parts
+@pytest.mark.parametrize("T,V", [(1500, 512), (1500, 2048), (300, 9000), (150, 32768), (60, 128256)])
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_gradient_rows_at_the_clips_edge_are_whole(T, V, dt):
+    """A position is clipped or it is not: its row of dlogits is zero, or no element of it
+    is (c softmax is above 1e-12 everywhere)."""
+    _announce(f"clip edge T={T} V={V} {dt}")
+    for sign in (1.0, -1.0):
+        _, dz = _at_the_edge(T, V, dt, sign, T + V)
+        n = (dz != 0).sum(1)
+        some = (n != 0) & (n != V)
+        assert not some.any(), f"{int(some.sum())} of {T} rows are partly zero"
+        assert 0 < int((n == 0).sum()) < T  # both sides occur
+
+
+def test_loss_and_gradient_take_one_side_of_the_clip():
+    """One position, its row in parts: where the gradient is that of a clipped position, the
+    loss is that of the bound, exactly -1 times the advantage."""
+    _announce("clip edge, loss and gradient")
+    clipped = 0
+    for seed in range(60):
+        for sign in (1.0, -1.0):
+            loss, dz = _at_the_edge(1, 65536, F32, sign, seed)
+            if not dz.any():
+                clipped += 1
+                assert loss == -sign, (seed, sign, loss)
+    assert clipped
