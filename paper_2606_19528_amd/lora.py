@@ -196,8 +196,12 @@ def _stream(stream):
     import torch
 
     if stream is None:
-        # (the current stream's handle; building torch's Stream object for it takes 3 us)
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+        # (the current stream's handle; building torch's Stream object for it takes 3 us, so that
+        # is left to a torch without this function, which is not public)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return ctypes.c_void_p(raw(torch.cuda.current_device()))
+        stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
 
 
