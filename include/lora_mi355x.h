@@ -401,8 +401,12 @@ lora_status_t preference_loss(const void *logits, int64_t ldz, const int32_t *ta
  *   g    n elements of type dt; n = 0 entries are skipped
  *   out  n elements of type out_dt that grad_clip writes: g itself (same type), a
  *        buffer of its own, or NULL in a list used for grad_norm alone
- * Errors: LORA_EINVAL (NULL or misaligned pointers, negative n, an output that
- * overlaps another range, a list not laid out, max_norm negative or NaN),
+ * norm has to lie outside of all of them: it is written while they are read.  The
+ * calls check it against the list's memory alone, since the gradients' addresses
+ * are in there, on the device.
+ * Errors: LORA_EINVAL (NULL or misaligned pointers, negative n, an out that
+ * overlaps another range of the list or its memory, norm in the list's memory, a
+ * list not laid out, max_norm negative or NaN),
  * LORA_EUNSUPPORTED (over 2^20 gradients or 2^40 elements), LORA_EWORKSPACE, LORA_EHIP. */
 typedef struct {
   const void *g;

@@ -7,6 +7,7 @@ binding raises -- there is no fallback path.
 """
 from __future__ import annotations
 
+import bisect
 import ctypes
 import os
 
@@ -640,8 +641,25 @@ class GradList:
         self.mem, nbytes = _ws(None, int(n), grads[0], stream)
         self.list = _GradList()
         self.tensors = (grads, out)
+        # Where the listed tensors lie, as disjoint ranges in ascending order (_apart).
+        self.starts, self.ends = [], []
+        for lo, hi in sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in (*grads, *out) if t.numel()):
+            if self.ends and lo <= self.ends[-1]:
+                self.ends[-1] = max(self.ends[-1], hi)
+            else:
+                self.starts.append(lo)
+                self.ends.append(hi)
         _check(lib().grad_list_init(ctypes.byref(self.list), arr, len(grads), _ptr(self.mem), nbytes, _stream(stream)),
                "grad_list_init")
+
+
+def _apart(grads: GradList, address: int, nbytes: int, where: str):
+    """Refuses a norm that lies in a listed tensor: it is written while others read there.
+    (The C entry points cannot: the list's addresses are in device memory.)"""
+    i = bisect.bisect_right(grads.ends, address)  # the first range that ends after `address`
+    if i < len(grads.starts) and grads.starts[i] < address + nbytes:
+        raise LoraError(LORA_EINVAL, where, "norm overlaps a listed gradient or output")
+    return address
 
 
 def grad_list(grads, out=None, stream=None) -> GradList:
@@ -654,7 +672,8 @@ def grad_norm(grads: GradList, norm, stream=None):
     """norm [1] = global norm of the listed gradients."""
     import torch
 
-    _check(lib().grad_norm(ctypes.byref(grads.list), _arg(norm, "norm", torch.float32, (1,)), _stream(stream)), "grad_norm")
+    at = _apart(grads, _arg(norm, "norm", torch.float32, (1,)), 4, "grad_norm")
+    _check(lib().grad_norm(ctypes.byref(grads.list), at, _stream(stream)), "grad_norm")
     return norm
 
 
@@ -663,8 +682,8 @@ def grad_clip(grads: GradList, max_norm: float, norm, stream=None):
     norm [2] receives the norm before and the factor."""
     import torch
 
-    _check(lib().grad_clip(ctypes.byref(grads.list), max_norm, _arg(norm, "norm", torch.float32, (2,)), _stream(stream)),
-           "grad_clip")
+    at = _apart(grads, _arg(norm, "norm", torch.float32, (2,)), 8, "grad_clip")
+    _check(lib().grad_clip(ctypes.byref(grads.list), max_norm, at, _stream(stream)), "grad_clip")
     return norm
 
 
