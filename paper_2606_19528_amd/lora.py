@@ -649,8 +649,9 @@ class GradList:
             else:
                 self.starts.append(lo)
                 self.ends.append(hi)
-        _check(lib().grad_list_init(ctypes.byref(self.list), arr, len(grads), _ptr(self.mem), nbytes, _stream(stream)),
-               "grad_list_init")
+        st = _stream(stream)
+        self.stream = st.value
+        _check(lib().grad_list_init(ctypes.byref(self.list), arr, len(grads), _ptr(self.mem), nbytes, st), "grad_list_init")
 
 
 def _apart(grads: GradList, address: int, nbytes: int, where: str):
@@ -660,6 +661,17 @@ def _apart(grads: GradList, address: int, nbytes: int, where: str):
     if i < len(grads.starts) and grads.starts[i] < address + nbytes:
         raise LoraError(LORA_EINVAL, where, "norm overlaps a listed gradient or output")
     return address
+
+
+def _list_stream(grads: GradList, stream):
+    """The stream's handle.  The list's memory was allocated on the stream that laid it out; where
+    another one uses it, the allocator keeps it until that one is done."""
+    import torch
+
+    st = _stream(stream)
+    if st.value != grads.stream:
+        grads.mem.record_stream(torch.cuda.current_stream() if stream is None else stream)
+    return st
 
 
 def grad_list(grads, out=None, stream=None) -> GradList:
@@ -673,7 +685,7 @@ def grad_norm(grads: GradList, norm, stream=None):
     import torch
 
     at = _apart(grads, _arg(norm, "norm", torch.float32, (1,)), 4, "grad_norm")
-    _check(lib().grad_norm(ctypes.byref(grads.list), at, _stream(stream)), "grad_norm")
+    _check(lib().grad_norm(ctypes.byref(grads.list), at, _list_stream(grads, stream)), "grad_norm")
     return norm
 
 
@@ -683,7 +695,7 @@ def grad_clip(grads: GradList, max_norm: float, norm, stream=None):
     import torch
 
     at = _apart(grads, _arg(norm, "norm", torch.float32, (2,)), 8, "grad_clip")
-    _check(lib().grad_clip(ctypes.byref(grads.list), max_norm, at, _stream(stream)), "grad_clip")
+    _check(lib().grad_clip(ctypes.byref(grads.list), max_norm, at, _list_stream(grads, stream)), "grad_clip")
     return norm
 
 

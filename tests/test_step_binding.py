@@ -98,3 +98,19 @@ def test_norm_apart_from_the_listed_gradients(launches, at, n, fits):
         with pytest.raises(lm.LoraError):
             call()
         assert not launches
+
+
+def test_list_memory_stays_while_another_stream_uses_it(launches):
+    """The list's own memory is allocated on the stream that lays it out.  A call on another
+    stream has to tell the allocator, or the memory of a list that is dropped goes to
+    another tensor while that stream's kernels still read addresses from it."""
+    gl = lm.grad_list([_Buffer(0x100000, 1024)], stream=_Stream(0x10))
+    lm.grad_clip(gl, 1.0, _Buffer(0x800000, 2))
+    lm.grad_norm(gl, _Buffer(0x800000, 1), stream=_Stream(0x10))
+    assert gl.mem.recorded == []  # its own stream
+    lm.grad_clip(gl, 1.0, _Buffer(0x800000, 2), stream=_Stream(0x20))
+    lm.grad_norm(gl, _Buffer(0x800000, 1), stream=_Stream(0x30))
+    assert gl.mem.recorded == [0x20, 0x30]
+    other = lm.grad_list([_Buffer(0x100000, 1024)], stream=_Stream(0x20))
+    lm.grad_clip(other, 1.0, _Buffer(0x800000, 2))  # the current stream
+    assert other.mem.recorded == [0x10]
