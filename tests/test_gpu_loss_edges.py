@@ -95,3 +95,62 @@ def test_loss_and_gradient_take_one_side_of_the_clip():
                 clipped += 1
                 assert loss == -sign, (seed, sign, loss)
     assert clipped
+
+
+def _along(f, z, X, h):
+    """(central difference of f along X, bound of its truncation): the third derivative from
+    the five points of f in 64 bits, twice for what it changes in between."""
+    v = [float(f(z + k * h * X)) for k in (-2, -1, 1, 2)]
+    return (v[2] - v[1]) / (2 * h), 2 * h * h / 6 * abs(v[3] - 2 * v[2] + 2 * v[1] - v[0]) / (2 * h ** 3)
+
+
+@pytest.mark.parametrize("which", ["policy", "preference"])
+def test_kernel_gradients_along_themselves(which):
+    """The kernels' gradients against central differences of the kernels' own losses, in
+    the gradient's direction, where the derivative is its norm.  A loss in 32 bits is off
+    by its positions' c times what their log-probabilities are off by, and its rounding;
+    what is allowed in all has to be under 3 % of the derivative."""
+    _announce(f"{which} gradient along itself")
+    T, V, h, kl, beta, eps = 24, 64, 1.0 / 32, 0.2, 0.8, 0.1
+    g = torch.Generator().manual_seed(8)
+    z = torch.randn(T, V, generator=g) * 2.0
+    y = torch.randint(0, V, (T,), generator=g, dtype=torch.int32)
+    w = (0.5 + torch.rand(T, generator=g)) / (T if which == "policy" else 1.0)
+    lp = R.logp(z, y, V)[0]
+    # ratios well inside the clip's edges or well beyond them, so that none is crossed
+    lr = torch.tensor([0.05, -0.05, 0.7, -0.7], dtype=R.F64)[torch.arange(T) % 4]
+    old, ref = (lp - lr).float(), (lp + 0.3 * torch.randn(T, generator=g, dtype=R.F64)).float()
+    adv = torch.randn(T, generator=g)
+    seq = [0, 7, 12, 20, 24]
+    cu = [t.cuda() for t in (y, w, adv, old, ref, torch.tensor(seq, dtype=torch.int32))]
+
+    def kernel(zz):
+        zz = zz.float().cuda()
+        L, M, o, dz = (torch.empty(1, device="cuda"), torch.empty(2, device="cuda"), torch.empty(T, device="cuda"),
+                       torch.empty(T, V, device="cuda"))
+        if which == "policy":
+            lm.policy_loss(zz, cu[0], cu[1], cu[2], cu[3], cu[4], L, o, dz, clip_lo=0.2, clip_hi=0.3, kl_coef=kl)
+        else:
+            lm.preference_loss(zz, cu[0], cu[1], cu[4], cu[5], L, M, o, dz, beta=beta, label_smoothing=eps)
+        return float(L[0]), dz.cpu().double()
+
+    def exact(zz):
+        if which == "policy":
+            out = R.policy(zz, y, V, w, adv, old, ref, 0.2, 0.3, kl)
+            return out[0], out[2]
+        out = R.preference(zz, y, V, w, ref, seq, beta, eps)
+        return out[0], out[3]
+
+    loss, dz = kernel(z)
+    norm = float(dz.norm())
+    # the points are fp32 values, so that both see the same ones
+    X = (dz / norm).float().double()
+    step = torch.stack([(z.double() + k * h * X).float().double() for k in (-1, 1)])
+    want = float((dz * (step[1] - step[0])).sum()) / (2 * h)
+    diff = (kernel(step[1])[0] - kernel(step[0])[0]) / (2 * h)
+    _, cut = _along(lambda p: exact(p)[0], z.double(), X, h)
+    off = float(exact(z.double())[1].abs().sum()) * (float(R.logp_bound(z, y, V).max()) + 16 * R.U) + 4 * R.U * (1 + abs(loss))
+    tol = off / h + cut + 16 * R.U * norm
+    assert abs(want - norm) <= 1e-4 * norm
+    assert tol <= 0.03 * norm, (tol, norm)
+    assert abs(diff - want) <= tol, (diff, want, tol)
