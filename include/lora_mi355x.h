@@ -359,7 +359,10 @@ lora_status_t embed_bwd_rows(const int32_t *ids, const void *dout, int32_t *toke
  * one's derivative is taken.
  *
  * A target outside [0, V) at a position of weight != 0 gives NaN (logp, the loss and
- * that row); logits of -inf are forbidden tokens of probability 0.  Rows of logits
+ * that row; of a preference loss its pair's margin and rows); logits of -inf are
+ * forbidden tokens of probability 0.  Offsets in seq beyond the positions are cut to
+ * them; offsets that are not ascending give NaN (the margin of a pair where they
+ * fall, the loss and every row of dlogits).  Rows of logits
  * must be whole 16-byte vectors (ldz a multiple of 8 bf16, 4 fp32); V is any.  T up
  * to 2^23, ldz to 2^30, npairs to 2^22, logits to 2^40 elements (LORA_EUNSUPPORTED).  loss is one fp32, margins [npairs] and logp [T]
  * fp32.  Statistics are fp32, the sums over positions 64-bit.  Workspace:

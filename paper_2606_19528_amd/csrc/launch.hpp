@@ -413,7 +413,7 @@ struct TokenLoss {
   float *loss;
   int parts, part_vecs;  // loss_plan
   // workspace: (maximum, sum of exponentials) of each part of each row, and behind
-  // them of each row (preference); the targets' logits; w dL/dlogp (preference);
+  // them of each row (preference); the targets' logits; w dL/dlogp [T + 1] (preference);
   // w L (policy) or a pair's loss
   float *stat, *ztgt, *coef, *rows;
   // token_logp of rows in parts: the flags of the parts' meetings, this launch's tag

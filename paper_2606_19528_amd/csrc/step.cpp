@@ -98,7 +98,7 @@ LossLayout loss_layout(int op, int64_t T, int64_t V, int64_t pairs, lora_dtype_t
   L.ztgt = off;
   off += pref || L.plan.parts > 1 ? round256((size_t)T * 4) : 0;
   L.coef = off;
-  off += pref ? round256((size_t)T * 4) : 0;
+  off += pref ? round256((size_t)(T + 1) * 4) : 0;  // (and a word for offsets that are not ascending)
   L.rows = off;
   off += op == TOKEN_LOSS_OP_LOGP ? 0 : round256((size_t)(pref ? pairs : T) * 4);
   L.sync = off;

@@ -206,7 +206,10 @@ __global__ __launch_bounds__(TL_NT) void token_stat_kernel(TokenLoss a, Stat *st
   __shared__ Stat red[TL_NT / 64];
   const int64_t t = blockIdx.x / a.parts;
   const int p = blockIdx.x % a.parts;
-  if (a.coef && p == 0 && threadIdx.x == 0) a.coef[t] = 0.0f;
+  if (a.coef && p == 0 && threadIdx.x == 0) {
+    a.coef[t] = 0.0f;
+    if (t == 0) a.coef[a.T] = 0.0f;  // (pair_kernel: offsets that are not ascending)
+  }
   if (weight(a, t) == 0.0f) {
     if (!stat && threadIdx.x == 0) a.logp[t] = 0.0f;
     return;
@@ -404,7 +407,8 @@ constexpr int PR_NT = 512;
 __global__ __launch_bounds__(PR_NT) void pair_kernel(TokenLoss a, PairArgs p, const Stat *stat, Stat *rowstat) {
   __shared__ double red[PR_NT / 64];
   const int i = blockIdx.x;
-  const int b0 = min(max(p.seq[2 * i], 0), a.T), b1 = min(max(p.seq[2 * i + 1], b0), a.T), b2 = min(max(p.seq[2 * i + 2], b1), a.T);
+  const int s0 = p.seq[2 * i], s1 = p.seq[2 * i + 1], s2 = p.seq[2 * i + 2];
+  const int b0 = min(max(s0, 0), a.T), b1 = min(max(s1, b0), a.T), b2 = min(max(s2, b1), a.T);
   const int64_t first = i == 0 ? 0 : b0, last = i == p.pairs - 1 ? a.T : b2;
   double d = 0.0;
   for (int64_t t = first + threadIdx.x; t < last; t += PR_NT) {
@@ -429,10 +433,14 @@ __global__ __launch_bounds__(PR_NT) void pair_kernel(TokenLoss a, PairArgs p, co
     if (w != 0.0f) a.coef[t] = w * (t < b1 ? g : -g);
   }
   if (threadIdx.x == 0) {
-    p.margins[i] = mg;
     float l = (1.0f - s) * softplus(-mg);
     if (s != 0.0f) l += s * softplus(mg);
-    a.rows[i] = l;
+    // Offsets that fall at this pair: another one may hold the same rows, and which of the
+    // two leaves their c is left to chance.  The loss and every c are NaN then.
+    const bool falls = s1 < s0 || s2 < s1;
+    if (falls) a.coef[a.T] = NAN;
+    p.margins[i] = falls ? NAN : mg;
+    a.rows[i] = falls ? NAN : l;
   }
 }
 
@@ -449,7 +457,7 @@ __global__ __launch_bounds__(TL_NT) void pair_dz_kernel(TokenLoss a, const Stat 
   }
   const unsigned b = gridDim.x - 2 - blockIdx.x;
   const int64_t t = b / a.parts;
-  const float c = a.coef[t];
+  const float c = a.coef[t] + a.coef[a.T];
   write_dz<E, NTS>(a, t, b % a.parts, c != 0.0f ? rowstat[t] : Stat{0.0f, 1.0f}, c, a.y[t]);
 }
 

@@ -154,3 +154,31 @@ def test_kernel_gradients_along_themselves(which):
     assert abs(want - norm) <= 1e-4 * norm
     assert tol <= 0.03 * norm, (tol, norm)
     assert abs(diff - want) <= tol, (diff, want, tol)
+
+
+@pytest.mark.parametrize("seq,falls", [([0, 10, 20, 12, 30], [1]), ([5, 3, 9], [0]), ([0, 3, 10, 4, 6, 8, 12], [1]),
+                                       ([0, 10, 8, 20, 31], [0])])
+@pytest.mark.parametrize("T,V", [(40, 64), (40, 128256)])
+def test_offsets_that_are_not_ascending(T, V, seq, falls):
+    """Two pairs may then hold the same rows: NaN in the loss and every row of the gradient,
+    instead of what the one that comes last leaves.  The next call is not touched by it."""
+    _announce(f"falling offsets {seq} V={V}")
+    g = torch.Generator(device="cuda").manual_seed(V)
+    z = torch.randn(T, V, generator=g, device="cuda")
+    y = torch.randint(0, V, (T,), generator=g, dtype=torch.int32, device="cuda")
+    P = len(seq) // 2
+    ws = torch.empty(lm.token_loss_workspace_bytes(lm.TOKEN_LOSS_OP_PREFERENCE, T, V, V, P, lm.LORA_F32), dtype=torch.uint8,
+                     device="cuda")
+    L, M, lp, dz = (torch.empty(1, device="cuda"), torch.empty(P, device="cuda"), torch.empty(T, device="cuda"),
+                    torch.empty(T, V, device="cuda"))
+
+    def call(offsets):
+        lm.preference_loss(z, y, None, None, torch.tensor(offsets, dtype=torch.int32, device="cuda"), L, M, lp, dz, ws=ws)
+        return [t.clone() for t in (L, M, lp, dz)]
+
+    good = call(sorted(seq))
+    bad = call(seq)
+    assert torch.isnan(bad[0]).all() and torch.isnan(bad[3]).all()
+    assert torch.isnan(bad[1]).nonzero()[:, 0].tolist() == falls
+    assert torch.equal(bad[2], good[2])
+    assert all(torch.equal(a, b) for a, b in zip(call(sorted(seq)), good)) and torch.isfinite(good[3]).all()
