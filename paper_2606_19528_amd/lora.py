@@ -630,48 +630,56 @@ class GradList:
         if len(out) != len(grads):
             raise ValueError("as many outputs as gradients are required")
         arr = (_Grad * max(len(grads), 1))()
+        ranges = []
         for i, (g, o) in enumerate(zip(grads, out)):
-            if o.numel() != g.numel():
+            n = g.numel()
+            if o.numel() != n:
                 raise ValueError("an output has another size than its gradient")
-            arr[i] = _Grad(_arg(g, "a gradient", g.dtype, g.shape), _arg(o, "an output", o.dtype, o.shape), g.numel(),
-                           _dtype_code(g), _dtype_code(o))
+            dg, do = _dtype_code(g), _dtype_code(o)
+            pg, po = _arg(g, "a gradient", g.dtype, g.shape), _arg(o, "an output", o.dtype, o.shape)
+            arr[i] = _Grad(pg, po, n, dg, do)
+            if n:
+                ranges.append((pg, pg + n * (2 if dg == LORA_BF16 else 4)))
+                if po != pg:
+                    ranges.append((po, po + n * (2 if do == LORA_BF16 else 4)))
         n = lib().grad_list_bytes(arr, len(grads))
         if n == ctypes.c_size_t(-1).value:
             raise LoraError(LORA_EINVAL, "grad_list_bytes", lib().lora_last_error().decode())
         self.mem, nbytes = _ws(None, int(n), grads[0], stream)
         self.list = _GradList()
+        self.ref = ctypes.byref(self.list)
         self.tensors = (grads, out)
-        # Where the listed tensors lie, as disjoint ranges in ascending order (_apart).
+        # Where the listed tensors lie, as disjoint ranges in ascending order (_list_args).
         self.starts, self.ends = [], []
-        for lo, hi in sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in (*grads, *out) if t.numel()):
-            if self.ends and lo <= self.ends[-1]:
-                self.ends[-1] = max(self.ends[-1], hi)
-            else:
+        end = -1
+        for lo, hi in sorted(ranges):
+            if lo > end:
                 self.starts.append(lo)
                 self.ends.append(hi)
+                end = hi
+            elif hi > end:
+                self.ends[-1] = end = hi
         st = _stream(stream)
         self.stream = st.value
-        _check(lib().grad_list_init(ctypes.byref(self.list), arr, len(grads), _ptr(self.mem), nbytes, st), "grad_list_init")
+        _check(lib().grad_list_init(self.ref, arr, len(grads), _ptr(self.mem), nbytes, st), "grad_list_init")
 
 
-def _apart(grads: GradList, address: int, nbytes: int, where: str):
-    """Refuses a norm that lies in a listed tensor: it is written while others read there.
-    (The C entry points cannot: the list's addresses are in device memory.)"""
-    i = bisect.bisect_right(grads.ends, address)  # the first range that ends after `address`
-    if i < len(grads.starts) and grads.starts[i] < address + nbytes:
-        raise LoraError(LORA_EINVAL, where, "norm overlaps a listed gradient or output")
-    return address
-
-
-def _list_stream(grads: GradList, stream):
-    """The stream's handle.  The list's memory was allocated on the stream that laid it out; where
-    another one uses it, the allocator keeps it until that one is done."""
+def _list_args(grads: GradList, norm, n: int, stream, where: str):
+    """(list, address of norm [n], stream) for a call on a list."""
     import torch
 
+    at = _arg(norm, "norm", torch.float32, (n,))
+    # A norm in a listed tensor would be written while others read there.  (The C entry points
+    # cannot refuse it: the list's addresses are in device memory.)
+    i = bisect.bisect_right(grads.ends, at)  # the first range that ends behind `at`
+    if i < len(grads.starts) and grads.starts[i] < at + 4 * n:
+        raise LoraError(LORA_EINVAL, where, "norm overlaps a listed gradient or output")
     st = _stream(stream)
     if st.value != grads.stream:
+        # The list's memory was allocated on the stream that laid it out: the allocator keeps
+        # it until this one, too, is done with it.
         grads.mem.record_stream(torch.cuda.current_stream() if stream is None else stream)
-    return st
+    return grads.ref, at, st
 
 
 def grad_list(grads, out=None, stream=None) -> GradList:
@@ -682,20 +690,16 @@ def grad_list(grads, out=None, stream=None) -> GradList:
 
 def grad_norm(grads: GradList, norm, stream=None):
     """norm [1] = global norm of the listed gradients."""
-    import torch
-
-    at = _apart(grads, _arg(norm, "norm", torch.float32, (1,)), 4, "grad_norm")
-    _check(lib().grad_norm(ctypes.byref(grads.list), at, _list_stream(grads, stream)), "grad_norm")
+    ref, at, st = _list_args(grads, norm, 1, stream, "grad_norm")
+    _check(lib().grad_norm(ref, at, st), "grad_norm")
     return norm
 
 
 def grad_clip(grads: GradList, max_norm: float, norm, stream=None):
     """Scales the listed gradients so that their global norm is at most max_norm;
     norm [2] receives the norm before and the factor."""
-    import torch
-
-    at = _apart(grads, _arg(norm, "norm", torch.float32, (2,)), 8, "grad_clip")
-    _check(lib().grad_clip(ctypes.byref(grads.list), max_norm, at, _list_stream(grads, stream)), "grad_clip")
+    ref, at, st = _list_args(grads, norm, 2, stream, "grad_clip")
+    _check(lib().grad_clip(ref, max_norm, at, st), "grad_clip")
     return norm
 
 
