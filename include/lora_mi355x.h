@@ -319,8 +319,9 @@ lora_status_t lora_ckpt_backward(const lora_node_t *nodes, int n, int64_t T, con
  *                   -1, rows[i] [D] fp32 their gradients and then zeros.
  * ids are int32 device values; one outside [0, V) gives a zero row of out and
  * no gradient (a padding position, say).  table, out and dout have type dt; out is
- * rounded once.  Sums are fp32, over ascending t in groups whose size depends on T
- * and V alone.  D a multiple of 8 up to 2^20, T up to 2^25, T D up to 2^35, V up to
+ * rounded once.  Sums are fp32, over ascending t in groups; the same ids and sizes
+ * give the same bits, and with many positions where a token's groups end depends on
+ * the other ids too.  D a multiple of 8 up to 2^20, T up to 2^25, T D up to 2^35, V up to
  * 2^30, the table up to 2^40 elements (LORA_EUNSUPPORTED). */
 lora_status_t embed_fwd(const void *table, const int32_t *ids, void *out, int64_t T, int64_t V,
                         int64_t D, float scale, lora_dtype_t dt, void *hip_stream);

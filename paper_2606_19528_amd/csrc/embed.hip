@@ -9,7 +9,8 @@
 // how often a token occurs.  A chunk sums its tokens' rows one after another in
 // registers.  What it holds of a token that began in an earlier chunk goes to
 // its partial sum, and the join launch adds a token's partial sums in chunk
-// order: no atomics on values, one order of summation.
+// order, one after another, so that launch's time does depend on the most frequent
+// token: no atomics on values, one order of summation for given ids.
 //
 // The gradient of few positions: six to nine launches of a sort would take
 // longer than the sums.  A workgroup instead looks for its positions' tokens
@@ -373,7 +374,9 @@ __global__ __launch_bounds__(EG_NT) void embed_grad_kernel(EmbedGrad a, unsigned
 }
 
 // A token's partial sums, added to its row in chunk order by the workgroups of
-// the first chunk that the token runs into.
+// the first chunk that the token runs into.  Bound by that chain, a chunk's key and then its
+// sum, where a token is frequent: 32768 positions of 151936 x 2048 compact take 153 us with
+// a text's frequencies, 345 with half of them one token (512 chunks), 548 with all.
 template <typename E>
 __global__ __launch_bounds__(EG_COL) void embed_join_kernel(EmbedGrad a) {
   const int vpr = a.D / E::VEC;

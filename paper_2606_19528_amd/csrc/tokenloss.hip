@@ -181,8 +181,8 @@ __device__ __forceinline__ void policy_terms(const PolicyArgs &p, int64_t t, dou
 }
 
 // ---- statistics of rows, or of parts of rows -------------------------------------
-// Bound by reading the logits: 4096 x 151936 bf16, three quarters of them live, 165 us (933 MB,
-// 5.7 TB/s).  One pass: each thread keeps a running maximum and a sum relative to it,
+// Bound by reading the logits: 4096 x 151936 bf16, three quarters of them live, 167 us (933 MB,
+// 5.6 TB/s; 166 with one operation a logit less, log2 e in one term).  One pass: each thread keeps a running maximum and a sum relative to it,
 // joined over lanes, waves and parts.
 constexpr int TL_NT = 256;
 
@@ -324,12 +324,14 @@ __device__ __forceinline__ void write_dz(const TokenLoss &a, int64_t t, int p, S
   for (; i < end; i += TL_NT) put_dz<NTS>(zero16(), out + i);
 }
 
-// From this many rows on, rows in registers; fewer in parts (128256 bf16: 256 rows 36 and 48 us,
-// 128 rows 31 and 30; 32000 and shorter rows alike).
+// From this many rows on, rows in registers; fewer in parts.  128256 columns, us a call in registers /
+// in parts: bf16 128 rows 32 / 20, 193 35 / 29, 256 38 / 37, 300 64 / 49, 512 66 / 72, 513 84 /
+// 76; fp32 128 38 / 38, 193 54 / 56, 256 62 / 74, 300 101 / 87, 512 128 / 147.  A row takes a whole
+// CU's registers, so rows come in rounds of 256, which this rule does not follow.
 constexpr int POLICY_ROWS = 192;
 static_assert(POLICY_ROWS <= TL_NT, "a thread a row");
 
-// Bound by launches and latency: 97 x 8192 fp32 3.8 + 4.6 us on the GPU, 12 a call.
+// Bound by launches and latency: 97 x 8192 fp32 3.9 + 4.7 us on the GPU, 11.7 a call.
 // Policy loss of few rows, after token_stat_kernel: each workgroup writes one
 // part of a row of dz; ahead of them the first one sums the loss, and LOSS_WGS - 1 end at once:
 // a part is read again on the XCD, one of 8 in turn, whose cache has it from the statistics (60 x
@@ -577,8 +579,9 @@ __global__ __launch_bounds__(NT, 4) void policy_rows_kernel(TokenLoss a, PolicyA
 // 16 KB (of 4, 8, 16 and 32 KB the best over a pair, a short answer and a short rollout).
 // Before a gradient: enough for about 8192 workgroups (2048 x 151936 bf16 in pairs 326 us,
 // whole rows 370).  Log-probabilities alone, whose parts meet: 2048 workgroups, and rows up to
-// 64 KB whole (1024 x 32000 bf16 12.9 us, 16 in parts for 2048 workgroups; 512 x 151936 28.7,
-// whole rows 36.5, 33.3 in parts for 8192).
+// 64 KB whole (bf16, whole and in parts for 2048 workgroups: 1024 x 32000 12.9 and 16.0 us, 200
+// 6.8 and 8.0, 4 6.4 and 6.2; fp32 4 x 16000 6.2 and 6.6; 512 x 151936 bf16 28.7 in parts, whole rows
+// 36.5, 33.3 in parts for 8192).
 LossPlan loss_plan(int64_t T, int64_t V, Dtype d, bool logp_only) {
   const int64_t vec = d == DT_BF16 ? 8 : 4, nz = (V + vec - 1) / vec;
   const int64_t want = ((logp_only ? 2048 : 8192) + T - 1) / T;
