@@ -432,6 +432,115 @@ lora_status_t grad_norm(const lora_grad_list_t *list, float *norm, void *hip_str
 lora_status_t grad_clip(const lora_grad_list_t *list, float max_norm, float *norm,
                         void *hip_stream);
 
+/* ---- Activations kept in 8 bits ---------------------------------------------------
+ * What the backward pass needs of a forward activation x [T, D], in about half the
+ * memory of bf16.  Per row and group g of 128 consecutive columns (the last group of a
+ * row may be shorter), with m the largest magnitude in the group:
+ *   scale[t][g] = m / 127
+ *   code        = sign(x) floor(127 |x| / m + 1/2)    in [-127, 127], 0 where m = 0
+ *   value       = scale code,   |value - x| <= m / 254
+ * codes [T, D] int8, scale [T, ceil(D / 128)] fp32.  Codes are exactly these; a value
+ * that is not finite makes its group's scale NaN (and its codes 0), so that all of the
+ * group is restored as NaN.  D a multiple of 8 up to 2^20, T ceil(D / 128) up to 2^29
+ * (LORA_EUNSUPPORTED). */
+lora_status_t act8_quantize(const void *x, int8_t *codes, float *scale, int64_t T, int64_t D,
+                            lora_dtype_t dt, void *hip_stream);
+/* x = the values of the codes, rounded once to type dt. */
+lora_status_t act8_dequantize(const int8_t *codes, const float *scale, void *x, int64_t T, int64_t D,
+                              lora_dtype_t dt, void *hip_stream);
+
+/* lora_linear_bwd and lora_linear_bwd_q from an x kept in 8 bits (dt = LORA_BF16), with xq
+ * its values: dx and du as there,
+ *   dA = du^T xq,  dB = s dy^T u,  u = u_saved, or xq A^T where that is NULL.
+ * Neither xq nor a bf16 copy of it is formed in memory.  Unlike there, du and u are not
+ * rounded to bf16 in dA and dB (dx's LoRA term takes du in bf16).  A u recomputed differs
+ * from the forward's by what x lost in 8 bits.  r = 0: x's codes are not read and may be
+ * NULL.  Errors and limits as there; workspace lora_linear_x8_workspace_bytes ((size_t)-1
+ * for rejected sizes). */
+size_t lora_linear_x8_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, int64_t r);
+lora_status_t lora_linear_bwd_x8(const int8_t *x_codes, const float *x_scale, const void *W,
+                                 const void *A, const void *B, const float *u_saved, const void *dy,
+                                 void *dx, float *dA, float *dB, int64_t T, int64_t d_in,
+                                 int64_t d_out, int64_t r, float scale, void *ws, size_t ws_bytes,
+                                 void *hip_stream);
+lora_status_t lora_linear_bwd_q_x8(const int8_t *x_codes, const float *x_scale, const void *W_codes,
+                                   const float *W_scale, const float *W_offset, int bits,
+                                   int64_t group, const void *A, const void *B, const float *u_saved,
+                                   const void *dy, void *dx, float *dA, float *dB, int64_t T,
+                                   int64_t d_in, int64_t d_out, int64_t r, float scale, void *ws,
+                                   size_t ws_bytes, void *hip_stream);
+
+/* The checkpointed step with a stash in 8 bits: lora_ckpt_forward quantizes each node's input
+ * (act8_quantize) before it leaves for the host, lora_ckpt_backward runs
+ * lora_linear_bwd_x8 on what comes back, so about half the bytes cross the link.  out is
+ * bitwise that of lora_ckpt_forward.  Arguments, ownership and errors as there; nodes of
+ * rank 0 keep nothing. */
+size_t lora_ckpt_workspace_bytes_x8(const lora_node_t *nodes, int n, int64_t T);
+size_t lora_ckpt_host_bytes_x8(const lora_node_t *nodes, int n, int64_t T);
+lora_status_t lora_ckpt_forward_x8(const lora_node_t *nodes, int n, int64_t T, const void *x0,
+                                   void *out, void *host_stash, size_t host_bytes, void *ws,
+                                   size_t ws_bytes, void *compute_stream, void *copy_stream);
+lora_status_t lora_ckpt_backward_x8(const lora_node_t *nodes, int n, int64_t T, const void *g_n,
+                                    void *dx0, const void *host_stash, size_t host_bytes, void *ws,
+                                    size_t ws_bytes, void *compute_stream, void *copy_stream);
+
+/* ---- Norms, gate and residual sum between two blocks --------------------------------
+ * From a block's output y [T, D] and the residual stream h [T, D] to the stream behind the
+ * block and the normed input n of the next one, in one pass:
+ *   yn = y r2 (w_post + o)    r2 = 1 / sqrt(mean_c y^2 + eps)    (post_norm = 0: yn = y)
+ *   h' = h + a g yn
+ *   n  = h' r1 (w_pre + o)    r1 = 1 / sqrt(mean_c h'^2 + eps)
+ * with o = gain_offset (0, or 1 for gains stored as their distance from 1), a = res_scale,
+ * and gains of 1 where w_post or w_pre is NULL (o is then not added).  The gate g is one
+ * value a channel [D], a token [T], or each element [T, D].
+ * y, n, gains and gate have type dt; h, h' and their gradients res_dt: bf16 with either, or
+ * fp32 with fp32.  Each output is rounded once (n from the unrounded h').
+ *   h_out     h'; may be h itself; NULL: not stored
+ *   n         NULL, with n8 and rstd_pre too: no norm before the next block
+ *   rstd_*    r2 and r1 [T] fp32 for the backward pass, optional
+ *   y8 h8 n8  optional copies in 8 bits of y, h' and n as they are stored (bitwise what
+ *             act8_quantize makes of them), written in the same pass
+ * y NULL: h' = h, the norm alone.  eps >= 1e-30 (LORA_EINVAL).  D a multiple of 8 up to 16384,
+ * T up to 2^22 (LORA_EUNSUPPORTED). */
+typedef enum {
+  BLOCK_GATE_NONE = 0,
+  BLOCK_GATE_CHANNEL = 1,
+  BLOCK_GATE_TOKEN = 2,
+  BLOCK_GATE_FULL = 3
+} block_gate_t;
+typedef struct {
+  int64_t T, D;
+  lora_dtype_t dt, res_dt;
+  int post_norm, gate_mode;
+  float gain_offset, res_scale;
+  const void *w_post, *w_pre, *gate;
+} block_norm_t;
+typedef struct {
+  int8_t *codes;
+  float *scale;
+} lora_act8_t;
+lora_status_t block_norm_fwd(const block_norm_t *b, const void *h, const void *y, void *h_out, void *n,
+                             float *rstd_post, float *rstd_pre, const lora_act8_t *y8,
+                             const lora_act8_t *h8, const lora_act8_t *n8, float eps,
+                             void *hip_stream);
+/* Its backward, from dn (NULL: n had no use) and dh_out, the gradient of h' through the
+ * stream (NULL: 0; one of the two is required), with hh = h' r1, yh = y r2, e = dn (w_pre + o):
+ *   dh    = dh_out + r1 (e - hh mean(e hh))           [T, D], may be dh_out itself
+ *   z     = a dh,  f = g z (w_post + o)
+ *   dy    = r2 (f - yh mean(f yh)), or g z without a post norm   [T, D], optional
+ *   dw_pre = sum_t dn hh,  dw_post = sum_t g z yh     [D] fp32, optional
+ *   dgate = z yn, summed over what the gate is broadcast along, optional: fp32 for a gate a channel
+ *           or a token, type dt for a full one
+ * h is the forward's h_out, y its y, whole or as h8, y8; rstd_* the forward's.  Outputs are
+ * overwritten.  Sums over rows are fp32 in a fixed order; they need a workspace of
+ * block_norm_workspace_bytes ((size_t)-1 for rejected sizes), the other outputs none. */
+size_t block_norm_workspace_bytes(int64_t T, int64_t D);
+lora_status_t block_norm_bwd(const block_norm_t *b, const void *dn, const void *dh_out, const void *h,
+                             const lora_act8_t *h8, const void *y, const lora_act8_t *y8,
+                             const float *rstd_post, const float *rstd_pre, void *dh, void *dy,
+                             float *dw_pre, float *dw_post, void *dgate, void *ws, size_t ws_bytes,
+                             void *hip_stream);
+
 /* ---- Plan and hand-over diagnostics -----------------------------------------
  * Which kernel configuration lora_linear_fwd / lora_linear_bwd run for these
  * sizes (host logic only, no GPU work): the output tile of the forward GEMM

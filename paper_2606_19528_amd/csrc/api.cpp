@@ -33,7 +33,8 @@ const char *kKernelNames[K_COUNT] = {"gemm_fwd",   "gemm_bwd_dx",   "gemm_frozen
                                      "head_gather", "head_logits", "head_dz", "head_dh",
                                      "topk_sim", "topk_select", "embed_fwd", "embed_sort", "embed_grad",
                                      "token_logp", "policy_loss", "preference_loss", "grad_norm",
-                                     "grad_scale"};
+                                     "grad_scale", "act8_quantize", "act8_dequantize", "block_norm_fwd", "block_norm_bwd",
+                                     "x8_down", "x8_prod"};
 
 struct EventPair {
   hipEvent_t a, b;
@@ -723,6 +724,125 @@ lora_status_t bwd_impl(const void *x, const void *W, const void *qc, const float
   return LORA_OK;
 }
 
+// The backward from an x in 8 bits (act8.hpp), with a bf16 or a quantized W: du by the
+// row-skinny kernel, the plain dx product with its LoRA step, then dA and dB in a
+// launch of their own (x8prod.hip) that reads x's codes and dy once at the memory's
+// rate; u, where it is not saved, from the codes.
+struct X8Layout {
+  size_t u, du, dutail, acat, planes, total;
+  int ldt, u_parts;
+  RowSplit sp;
+};
+X8Layout x8_layout(int64_t T, int64_t K, int64_t N, int64_t r) {
+  X8Layout L{};
+  if (r == 0) return L;
+  L.u_parts = x8_down_parts(T, K);
+  L.sp = row_split(T, N, (int)r, DT_BF16);
+  L.ldt = tail_ld(L.sp.nsplit * (int)r, DT_BF16);
+  size_t off = 0;
+  L.u = off;  // partial sums of u (when it is recomputed)
+  off += round256((size_t)L.u_parts * T * r * 4);
+  L.du = off;  // partial sums of du = s dy B
+  off += round256((size_t)L.sp.nsplit * T * r * 4);
+  L.dutail = off;  // [T][ldt]: E(partial p of du) in columns p*r ..
+  off += round256((size_t)T * L.ldt * 2);
+  L.acat = off;  // [nsplit * r][K]: A repeated once per partial
+  off += L.sp.nsplit > 1 ? round256((size_t)L.sp.nsplit * r * K * 2) : 0;
+  L.planes = off;  // dA and dB of each range of tokens
+  off += round256(x8_plan(T, K, N, r).bytes);
+  L.total = off;
+  return L;
+}
+
+lora_status_t bwd_x8_impl(const int8_t *xc, const float *xs, const void *W, const void *qc, const float *qs, const float *qo,
+                          int bits, int64_t group, const void *A, const void *B, const float *u_saved, const void *dy, void *dx,
+                          float *dA, float *dB, int64_t T, int64_t d_in, int64_t d_out, int64_t r, float scale, void *ws,
+                          size_t ws_bytes, void *hip_stream) {
+  if (r == 0)  // x does not enter
+    return bwd_impl(nullptr, W, qc, qs, qo, bits, group, A, B, u_saved, dy, dx, dA, dB, T, d_in, d_out, r, scale, LORA_BF16, ws,
+                    ws_bytes, hip_stream);
+  lora_status_t s = check_shapes(T, d_in, d_out, r, LORA_BF16);
+  if (s != LORA_OK) return s;
+  QWeight qw{};
+  std::vector<Range> ins;
+  if (qc) {
+    if ((s = check_qweight(qc, qs, qo, bits, group, d_in, d_out, r, LORA_BF16, &qw, &ins)) != LORA_OK) return s;
+    W = qc;
+  } else {
+    ins.push_back(rng(W, d_out * d_in * 2));
+  }
+  if (!dy || !W || !xc || !xs || !A || !B || !dA || !dB)
+    return fail(LORA_EINVAL, "x's codes and scales, W, A, B, dy, dA and dB are required");
+  if (!std::isfinite(scale)) return fail(LORA_EINVAL, "scale must be finite");
+  const void *ptrs[] = {xc, xs, W, A, B, u_saved, dy, dx, dA, dB};
+  for (const void *p : ptrs)
+    if (p && !aligned16(p)) return fail(LORA_EINVAL, "pointers must be 16-byte aligned");
+  const X8Layout L = x8_layout(T, d_in, d_out, r);
+  if ((s = check_ws(ws, ws_bytes, L.total)) != LORA_OK) return s;
+  for (const Range &a : {rng(dy, T * d_out * 2), rng(xc, T * d_in), rng(xs, T * act8_groups(d_in) * 4), rng(A, r * d_in * 2),
+                         rng(B, d_out * r * 2), rng(u_saved, T * r * 4)})
+    ins.push_back(a);
+  if (any_overlap({rng(dx, T * d_in * 2), rng(dA, r * d_in * 4), rng(dB, d_out * r * 4), rng(ws, (int64_t)L.total)}, ins))
+    return fail(LORA_EINVAL, "an output overlaps an input or another output");
+
+  hipStream_t st = (hipStream_t)hip_stream;
+  char *wsb = (char *)ws;
+  hipError_t e;
+  X8Prod pr{};
+  pr.x = Act8In{xc, xs};
+  pr.dy = dy;
+  pr.u = u_saved; pr.u_parts = 1;
+  if (!u_saved) {
+    pr.u = (const float *)(wsb + L.u); pr.u_parts = L.u_parts;
+    Timed t(K_X8_DOWN, st);
+    e = launch_x8_down(X8Down{pr.x, A, (float *)(wsb + L.u), (int)T, (int)d_in, (int)r}, st);
+    t.done();
+    if (e != hipSuccess) return hip_fail(e, "x8_down launch");
+  }
+  const int ns = L.sp.nsplit;
+  pr.du = (const float *)(wsb + L.du); pr.du_parts = ns;
+  {
+    RowArgs ra{};
+    ra.X = dy; ra.ldx = d_out; ra.M = (int)T; ra.L = (int)d_out;
+    ra.V = B; ra.ldv = r; ra.vmode = V_KMAJ_TR; ra.r = (int)r;
+    ra.nsplit = ns; ra.seg = L.sp.seg; ra.mb = L.sp.mb;
+    ra.out_mult = scale; ra.out = (float *)(wsb + L.du); ra.out_stride = T * r;
+    if (dx) {
+      ra.tail = wsb + L.dutail; ra.ldt = L.ldt; ra.tail_mult = scale;
+      if (ns > 1) {  // A repeated once per partial of du
+        ra.bcopy_mode = BCOPY_FLAT; ra.bcopy_src = A; ra.bcopy_dst = wsb + L.acat;
+        ra.bcopy_period = r * d_in; ra.bcopy_elems = ns * r * d_in;
+      }
+    }
+    Timed t(K_LORA_DY_B, st);
+    e = launch_row_skinny(ra, DT_BF16, st);
+    t.done();
+    if (e != hipSuccess) return hip_fail(e, "lora_dy_b launch");
+  }
+  if (dx) {
+    GemmArgs g{};
+    g.A = dy; g.lda = d_out;
+    g.B = W; g.ldb = d_in;
+    g.M = (int)T; g.N = (int)d_in; g.K = (int)d_out;
+    g.C = dx; g.ldc = d_in;
+    g.A2 = wsb + L.dutail; g.lda2 = L.ldt;
+    g.B2 = ns > 1 ? (const void *)(wsb + L.acat) : A; g.ldb2 = d_in;
+    g.r = (int)(ns * r);
+    set_qweight(g, qc ? &qw : nullptr);
+    Timed t(qc ? K_GEMM_BWD_DX_Q : K_GEMM_BWD_DX, st);
+    e = run_gemm(g, DT_BF16, qc ? &qw : nullptr, true, nullptr, st);
+    t.done();
+    if (e != hipSuccess) return hip_fail(e, "gemm_bwd_dx launch");
+  }
+  pr.dA = dA; pr.dB = dB; pr.scale = scale;
+  pr.T = (int)T; pr.K = (int)d_in; pr.N = (int)d_out; pr.r = (int)r;
+  pr.planes = (float *)(wsb + L.planes);
+  Timed t(K_X8_PROD, st);
+  e = launch_x8_prod(pr, st);
+  t.done();
+  return e == hipSuccess ? LORA_OK : hip_fail(e, "x8_prod launch");
+}
+
 size_t frozen_split_bytes(int64_t T, int64_t d_in, int64_t d_out, lora_dtype_t dt, bool quant) {
   const int n = dt == LORA_BF16 ? gemm_splits(T, d_in, d_out, quant) : 1;
   return n > 1 ? (size_t)n * T * d_in * 4 : 0;
@@ -832,6 +952,28 @@ lora_status_t lora_linear_bwd_q(const void *x, const void *W_codes, const float 
   if (!W_codes) return fail(LORA_EINVAL, "codes, scale and offset are required");
   return bwd_impl(x, nullptr, W_codes, W_scale, W_offset, bits, group, A, B, u_saved, dy, dx, dA,
                   dB, T, d_in, d_out, r, scale, LORA_BF16, ws, ws_bytes, hip_stream);
+}
+
+size_t lora_linear_x8_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, int64_t r) {
+  if (check_shapes(T, d_in, d_out, r, LORA_BF16) != LORA_OK) return (size_t)-1;
+  if (r == 0) return lora_linear_workspace_bytes(LORA_OP_BWD, T, d_in, d_out, 0, LORA_BF16);
+  return x8_layout(T, d_in, d_out, r).total;
+}
+
+lora_status_t lora_linear_bwd_x8(const int8_t *x_codes, const float *x_scale, const void *W, const void *A, const void *B,
+                                 const float *u_saved, const void *dy, void *dx, float *dA, float *dB, int64_t T, int64_t d_in,
+                                 int64_t d_out, int64_t r, float scale, void *ws, size_t ws_bytes, void *hip_stream) {
+  return bwd_x8_impl(x_codes, x_scale, W, nullptr, nullptr, nullptr, 0, 0, A, B, u_saved, dy, dx, dA, dB, T, d_in, d_out, r,
+                     scale, ws, ws_bytes, hip_stream);
+}
+
+lora_status_t lora_linear_bwd_q_x8(const int8_t *x_codes, const float *x_scale, const void *W_codes, const float *W_scale,
+                                   const float *W_offset, int bits, int64_t group, const void *A, const void *B,
+                                   const float *u_saved, const void *dy, void *dx, float *dA, float *dB, int64_t T, int64_t d_in,
+                                   int64_t d_out, int64_t r, float scale, void *ws, size_t ws_bytes, void *hip_stream) {
+  if (!W_codes) return fail(LORA_EINVAL, "codes, scale and offset are required");
+  return bwd_x8_impl(x_codes, x_scale, nullptr, W_codes, W_scale, W_offset, bits, group, A, B, u_saved, dy, dx, dA, dB, T, d_in,
+                     d_out, r, scale, ws, ws_bytes, hip_stream);
 }
 
 lora_status_t frozen_linear_bwd_dx(const void *dy, const void *W, void *dx, int64_t T,

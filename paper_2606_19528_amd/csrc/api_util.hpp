@@ -49,6 +49,12 @@ enum KernelId {
   K_PREFERENCE_LOSS,  // preference loss and its gradient
   K_GRAD_NORM,        // norm of a list of gradients
   K_GRAD_SCALE,       // the list scaled by the clip coefficient
+  K_ACT8_QUANTIZE,    // activations to 8 bits
+  K_ACT8_DEQUANTIZE,  // and back
+  K_BLOCK_NORM_FWD,   // post norm, gate, residual sum, next norm
+  K_BLOCK_NORM_BWD,   // its backward
+  K_X8_DOWN,          // u = x A^T from an x in 8 bits
+  K_X8_PROD,          // dA and dB from an x in 8 bits
   K_COUNT
 };
 

@@ -464,6 +464,77 @@ hipError_t launch_grad_few(const GradChunk *c, int nchunk, bool clip, float max_
 hipError_t launch_grad_norm(const GradChunk *c, int nchunk, double *part, float *norm, hipStream_t st);
 hipError_t launch_grad_clip(const GradChunk *c, int nchunk, double *part, float max_norm, float *norm, hipStream_t st);
 
+// ---- activations in 8 bits (act8.hip; the format is in act8.hpp) ----
+inline int64_t act8_groups(int64_t D) { return (D + 127) / 128; }  // scales of a row
+hipError_t launch_act8_quantize(const void *x, int8_t *codes, float *scale, int64_t T, int64_t D, Dtype d, hipStream_t st);
+hipError_t launch_act8_dequantize(const int8_t *codes, const float *scale, void *x, int64_t T, int64_t D, Dtype d, hipStream_t st);
+struct Act8Out {  // codes [T][D] and scales [T][ng] to write; codes null: none
+  int8_t *codes;
+  float *scale;
+};
+struct Act8In {
+  const int8_t *codes;
+  const float *scale;
+};
+
+// ---- norms, gate and residual sum between two blocks (blocknorm.hip) ----
+enum { BN_GATE_NONE = 0, BN_GATE_CHANNEL = 1, BN_GATE_TOKEN = 2, BN_GATE_FULL = 3 };
+constexpr int64_t BN_MAX_D = 16384;  // a row is held by 1024 threads, 16 values each
+struct BlockNormFwd {
+  const void *y, *h, *gate, *w_post, *w_pre;  // y, gains and gate may be null
+  void *h_out, *n;
+  float *rstd_post, *rstd_pre;
+  Act8Out y8, h8, n8;
+  int64_t T;
+  int D, ng, gate_mode, post;
+  float eps, off, res_scale;
+};
+struct BlockNormBwd {
+  const void *dn, *dh_out, *h, *y, *gate, *w_post, *w_pre;
+  Act8In h8, y8;  // in the place of h, y
+  const float *rstd_post, *rstd_pre;
+  void *dh, *dy, *dgate;
+  float *want_w1, *want_w2, *want_gate;  // column sums [D] (want_gate: dgate of a gate [D]), or null
+  float *part;                           // workspace [3][block_norm_parts][D]
+  int64_t T;
+  int D, ng, gate_mode, post;
+  float off, res_scale;
+};
+int block_norm_parts(int64_t T, int64_t D);
+hipError_t launch_block_norm_fwd(const BlockNormFwd &a, Dtype d, Dtype res, hipStream_t st);
+hipError_t launch_block_norm_bwd(const BlockNormBwd &a, Dtype d, Dtype res, hipStream_t st);
+
+// ---- rank-r products of the LoRA backward from an input in 8 bits (x8prod.hip) ----
+// u [parts][T][r] = the values of the codes against A [r][K] (bf16), over `parts`
+// ranges of K.
+struct X8Down {
+  Act8In x;
+  const void *A;
+  float *u;
+  int T, K, r;
+};
+int x8_down_parts(int64_t T, int64_t K);
+hipError_t launch_x8_down(const X8Down &a, hipStream_t st);
+// dA [r][K] = du^T x and dB [N][r] = scale dy^T u, with du and u as the sums of
+// du_parts and u_parts planes [T][r] fp32, added in ascending order.  `planes`:
+// X8Plan::bytes, the sums of the ranges of tokens.
+struct X8Prod {
+  Act8In x;
+  const void *dy;
+  const float *du, *u;
+  int du_parts, u_parts;
+  float *dA, *dB;
+  float scale;
+  int T, K, N, r;
+  float *planes;
+};
+struct X8Plan {
+  int parts, chunk;  // ranges of tokens and their length
+  size_t bytes;
+};
+X8Plan x8_plan(int64_t T, int64_t K, int64_t N, int64_t r);
+hipError_t launch_x8_prod(const X8Prod &a, hipStream_t st);
+
 // Padded row length of the LoRA-step operands (a multiple of the GEMM stage).
 inline int tail_ld(int r, Dtype dt) {
   const int s = dt == DT_BF16 ? 64 : 32;

@@ -54,6 +54,19 @@ class _GradList(ctypes.Structure):
                 ("chunk", ctypes.c_int32), ("has_out", ctypes.c_int32)]
 
 
+class _Act8(ctypes.Structure):
+    """lora_act8_t of the C ABI."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
+class _BlockNorm(ctypes.Structure):
+    """block_norm_t of the C ABI."""
+    _fields_ = [("T", ctypes.c_int64), ("D", ctypes.c_int64), ("dt", ctypes.c_int), ("res_dt", ctypes.c_int),
+                ("post_norm", ctypes.c_int), ("gate_mode", ctypes.c_int), ("gain_offset", ctypes.c_float),
+                ("res_scale", ctypes.c_float), ("w_post", ctypes.c_void_p), ("w_pre", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p)]
+
+
 class LoraError(RuntimeError):
     def __init__(self, status: int, where: str, detail: str):
         super().__init__(f"{where}: status {status} ({detail})")
@@ -141,6 +154,29 @@ def lib() -> ctypes.CDLL:
     L.grad_norm.restype = i32
     L.grad_clip.argtypes = [LP, f32, vp, vp]
     L.grad_clip.restype = i32
+    L.act8_quantize.argtypes = [vp, vp, vp, i64, i64, i32, vp]
+    L.act8_quantize.restype = i32
+    L.act8_dequantize.argtypes = [vp, vp, vp, i64, i64, i32, vp]
+    L.act8_dequantize.restype = i32
+    L.lora_linear_x8_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    L.lora_linear_x8_workspace_bytes.restype = sz
+    L.lora_linear_bwd_x8.argtypes = [vp] * 10 + [i64, i64, i64, i64, f32, vp, sz, vp]
+    L.lora_linear_bwd_x8.restype = i32
+    L.lora_linear_bwd_q_x8.argtypes = [vp] * 5 + [i32, i64] + [vp] * 7 + [i64, i64, i64, i64, f32, vp, sz, vp]
+    L.lora_linear_bwd_q_x8.restype = i32
+    for name in ("lora_ckpt_workspace_bytes_x8", "lora_ckpt_host_bytes_x8"):
+        getattr(L, name).argtypes = [NP, i32, i64]
+        getattr(L, name).restype = sz
+    for name in ("lora_ckpt_forward_x8", "lora_ckpt_backward_x8"):
+        getattr(L, name).argtypes = [NP, i32, i64, vp, vp, vp, sz, vp, sz, vp, vp]
+        getattr(L, name).restype = i32
+    BP, AP = ctypes.POINTER(_BlockNorm), ctypes.POINTER(_Act8)
+    L.block_norm_fwd.argtypes = [BP, vp, vp, vp, vp, vp, vp, AP, AP, AP, f32, vp]
+    L.block_norm_fwd.restype = i32
+    L.block_norm_workspace_bytes.argtypes = [i64, i64]
+    L.block_norm_workspace_bytes.restype = sz
+    L.block_norm_bwd.argtypes = [BP, vp, vp, vp, AP, vp, AP] + [vp] * 8 + [sz, vp]
+    L.block_norm_bwd.restype = i32
     L.lora_status_str.argtypes = [i32]
     L.lora_status_str.restype = ctypes.c_char_p
     L.lora_last_error.argtypes = []
@@ -480,6 +516,40 @@ def lora_ckpt_backward(nodes, g_n, dx0, host_stash, ws, compute_stream=None, cop
     return dx0
 
 
+def lora_ckpt_sizes_x8(nodes, T: int):
+    """lora_ckpt_sizes of a step with its stash in 8 bits."""
+    arr = _nodes(nodes)
+    w = lib().lora_ckpt_workspace_bytes_x8(arr, len(nodes), T)
+    h = lib().lora_ckpt_host_bytes_x8(arr, len(nodes), T)
+    if w == ctypes.c_size_t(-1).value:
+        raise LoraError(LORA_EINVAL, "lora_ckpt_workspace_bytes_x8", "chain rejected")
+    return int(w), int(h)
+
+
+def lora_ckpt_forward_x8(nodes, x0, out, host_stash, ws, compute_stream=None, copy_stream=None):
+    """lora_ckpt_forward with every node input quantized to 8 bits before it leaves for the host."""
+    arr = _nodes(nodes)
+    T = x0.shape[0]
+    st = lib().lora_ckpt_forward_x8(arr, len(nodes), T, _ptr(x0), _ptr(out), _ptr(host_stash),
+                                    host_stash.numel() * host_stash.element_size(), _ptr(ws),
+                                    ws.numel() * ws.element_size(), _stream(compute_stream),
+                                    _stream(copy_stream))
+    _check(st, "lora_ckpt_forward_x8")
+    return out
+
+
+def lora_ckpt_backward_x8(nodes, g_n, dx0, host_stash, ws, compute_stream=None, copy_stream=None):
+    """lora_ckpt_backward from a stash of lora_ckpt_forward_x8."""
+    arr = _nodes(nodes)
+    T = g_n.shape[0]
+    st = lib().lora_ckpt_backward_x8(arr, len(nodes), T, _ptr(g_n), _ptr(dx0), _ptr(host_stash),
+                                     host_stash.numel() * host_stash.element_size(), _ptr(ws),
+                                     ws.numel() * ws.element_size(), _stream(compute_stream),
+                                     _stream(copy_stream))
+    _check(st, "lora_ckpt_backward_x8")
+    return dx0
+
+
 # --- embedding, losses over the targets, clipping ------------------------------------
 def _arg(t, name: str, dtype, shape):
     """Address of a tensor argument; refuses one of another type, shape, layout or
@@ -701,6 +771,209 @@ def grad_clip(grads: GradList, max_norm: float, norm, stream=None):
     ref, at, st = _list_args(grads, norm, 2, stream, "grad_clip")
     _check(lib().grad_clip(ref, max_norm, at, st), "grad_clip")
     return norm
+
+
+# --- activations in 8 bits, and the backward from them --------------------------------
+ACT8_GROUP = 128
+
+
+def _dev_arg(t, name: str, dtype, shape, dev: int):
+    """_arg of a tensor that has to be on device `dev`, the current one."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the current GPU")
+    if not t.is_contiguous():
+        raise ValueError("tensors must be contiguous (row-major, no padding)")
+    return t.data_ptr()
+
+
+def _dev_opt(t, name: str, dtype, shape, dev: int):
+    return None if t is None else _dev_arg(t, name, dtype, shape, dev)
+
+
+def _x8_args(x8, name: str, T: int, D: int, dev: int):
+    """Addresses of (codes, scale) of an activation [T, D] in 8 bits."""
+    import torch
+
+    codes, scale = x8
+    return (_dev_arg(codes, name + "'s codes", torch.int8, (T, D), dev),
+            _dev_arg(scale, name + "'s scale", torch.float32, (T, -(-D // ACT8_GROUP)), dev))
+
+
+def act8_empty(T: int, D: int, device="cuda"):
+    """(codes int8 [T, D], scale fp32 [T, ceil(D / 128)]) for an activation [T, D] in 8 bits."""
+    import torch
+
+    return (torch.empty(T, D, dtype=torch.int8, device=device),
+            torch.empty(T, -(-D // ACT8_GROUP), dtype=torch.float32, device=device))
+
+
+def act8_quantize(x, x8, stream=None):
+    """x8 = (codes, scale) of x [T, D]: of each 128 columns of a row the largest magnitude over
+    127, and the nearest multiples of it."""
+    import torch
+
+    (T, D), dev = x.shape, torch.cuda.current_device()
+    dt = _dtype_code(x)
+    st = lib().act8_quantize(_dev_arg(x, "x", x.dtype, (T, D), dev), *_x8_args(x8, "x8", T, D, dev), T, D, dt, _stream(stream))
+    _check(st, "act8_quantize")
+    return x8
+
+
+def act8_dequantize(x8, x, stream=None):
+    """x [T, D] = scale times codes, rounded to x's type."""
+    import torch
+
+    (T, D), dev = x.shape, torch.cuda.current_device()
+    dt = _dtype_code(x)
+    st = lib().act8_dequantize(*_x8_args(x8, "x8", T, D, dev), _dev_arg(x, "x", x.dtype, (T, D), dev), T, D, dt, _stream(stream))
+    _check(st, "act8_dequantize")
+    return x
+
+
+def lora_linear_x8_workspace_bytes(T: int, d_in: int, d_out: int, r: int) -> int:
+    n = lib().lora_linear_x8_workspace_bytes(T, d_in, d_out, r)
+    if n == ctypes.c_size_t(-1).value:
+        raise LoraError(LORA_EINVAL, "lora_linear_x8_workspace_bytes", lib().lora_last_error().decode())
+    return int(n)
+
+
+def _bwd_x8_args(x8, A, B, u_saved, dy, dx, dA, dB, T, d_in, d_out, dev):
+    import torch
+
+    bf, f32 = torch.bfloat16, torch.float32
+    r = 0 if A is None else A.shape[0]
+    # (at rank 0 x, A and B do not enter)
+    head = _x8_args(x8, "x8", T, d_in, dev) if r else (None, None)
+    AB = (_dev_arg(A, "A", bf, (r, d_in), dev), _dev_arg(B, "B", bf, (d_out, r), dev)) if r else (None, None)
+    grads = (_dev_arg(dA, "dA", f32, (r, d_in), dev), _dev_arg(dB, "dB", f32, (d_out, r), dev)) if r else (None, None)
+    return r, head, (*AB, _dev_opt(u_saved, "u_saved", f32, (T, r), dev) if r else None, _dev_arg(dy, "dy", bf, (T, d_out), dev),
+                     _dev_opt(dx, "dx", bf, (T, d_in), dev), *grads)
+
+
+def lora_linear_bwd_x8(x8, W, A, B, u_saved, dy, dx, dA, dB, scale: float = 1.0, ws=None, stream=None):
+    """lora_linear_bwd from an x kept in 8 bits (act8_quantize); u_saved None recomputes u from it."""
+    import torch
+
+    (T, d_out), d_in, dev = dy.shape, W.shape[1], torch.cuda.current_device()
+    r, head, rest = _bwd_x8_args(x8, A, B, u_saved, dy, dx, dA, dB, T, d_in, d_out, dev)
+    wp, wn, ws = _ws_for(ws, lambda: lora_linear_x8_workspace_bytes(T, d_in, d_out, r), dy, stream)
+    st = lib().lora_linear_bwd_x8(*head, _dev_arg(W, "W", torch.bfloat16, (d_out, d_in), dev), *rest, T, d_in, d_out, r, scale, wp,
+                                  wn, _stream(stream))
+    _check(st, "lora_linear_bwd_x8")
+    return dx, dA, dB
+
+
+def lora_linear_bwd_q_x8(x8, Wq, A, B, u_saved, dy, dx, dA, dB, scale: float = 1.0, ws=None, stream=None):
+    """lora_linear_bwd_x8 with the frozen W quantized (dict, see _qw)."""
+    import torch
+
+    codes, sc, off, bits, group, d_out, d_in = _qw(Wq)
+    T, dev = dy.shape[0], torch.cuda.current_device()
+    r, head, rest = _bwd_x8_args(x8, A, B, u_saved, dy, dx, dA, dB, T, d_in, d_out, dev)
+    weight = (_dev_arg(codes, "codes", torch.uint8, (d_out, codes.shape[1]), dev),
+              _dev_arg(sc, "scale", torch.float32, (sc.shape[0], d_out), dev),
+              _dev_arg(off, "offset", torch.float32, (sc.shape[0], d_out), dev))
+    wp, wn, ws = _ws_for(ws, lambda: lora_linear_x8_workspace_bytes(T, d_in, d_out, r), dy, stream)
+    st = lib().lora_linear_bwd_q_x8(*head, *weight, bits, group, *rest, T, d_in, d_out, r, scale, wp, wn, _stream(stream))
+    _check(st, "lora_linear_bwd_q_x8")
+    return dx, dA, dB
+
+
+# --- norms, gate and residual sum between two blocks ----------------------------------
+BLOCK_GATE_NONE, BLOCK_GATE_CHANNEL, BLOCK_GATE_TOKEN, BLOCK_GATE_FULL = range(4)
+
+
+def _gate_mode(gate, T: int, D: int) -> int:
+    if gate is None:
+        return BLOCK_GATE_NONE
+    for mode, shape in ((BLOCK_GATE_CHANNEL, (D,)), (BLOCK_GATE_TOKEN, (T, 1)), (BLOCK_GATE_FULL, (T, D))):
+        if gate.shape == shape:
+            return mode
+    raise ValueError(f"gate has shape {tuple(gate.shape)}, expected ({D},), ({T}, 1) or ({T}, {D})")
+
+
+def _block(T, D, dtype, res_dtype, post_norm, w_post, w_pre, gate, gain_offset, res_scale, dev):
+    import torch
+
+    code = {torch.bfloat16: LORA_BF16, torch.float32: LORA_F32}
+    if dtype not in code or res_dtype not in code:
+        raise TypeError(f"unsupported dtype {dtype} or {res_dtype} (bf16 or fp32)")
+    if post_norm is None:
+        post_norm = w_post is not None
+    # (an element of D = 1 or T = 1 makes two of a gate's shapes alike: either names the same values)
+    mode = _gate_mode(gate, T, D)
+    return _BlockNorm(T, D, code[dtype], code[res_dtype], 1 if post_norm else 0, mode, gain_offset, res_scale,
+                      _dev_opt(w_post, "w_post", dtype, (D,), dev), _dev_opt(w_pre, "w_pre", dtype, (D,), dev),
+                      None if gate is None else _dev_arg(gate, "gate", dtype, gate.shape, dev))
+
+
+def _act8(x8, name, T, D, dev):
+    return None if x8 is None else ctypes.byref(_Act8(*_x8_args(x8, name, T, D, dev)))
+
+
+def block_norm_fwd(h, y=None, h_out=None, n=None, w_pre=None, w_post=None, gate=None, post_norm=None, rstd_pre=None,
+                   rstd_post=None, y8=None, h8=None, n8=None, eps: float = 1e-6, gain_offset: float = 0.0,
+                   res_scale: float = 1.0, stream=None):
+    """h_out = h + res_scale gate norm(y) and n = norm(h_out) (see the header): the norm behind a block
+    (`post_norm`, by default where w_post is given), its gate ([D], [T, 1] or [T, D]) and residual
+    sum, and the norm before the next.  rstd_pre, rstd_post [T] are kept for the backward pass;
+    y8, h8, n8 receive copies in 8 bits.  Without y the norm alone."""
+    import torch
+
+    (T, D), dev, f32 = h.shape, torch.cuda.current_device(), torch.float32
+    like = next((t for t in (y, n, w_pre) if t is not None), h)
+    dt, rt = like.dtype, h.dtype
+    b = _block(T, D, dt, rt, post_norm, w_post, w_pre, gate, gain_offset, res_scale, dev)
+    st = lib().block_norm_fwd(ctypes.byref(b), _dev_arg(h, "h", rt, (T, D), dev), _dev_opt(y, "y", dt, (T, D), dev),
+                              _dev_opt(h_out, "h_out", rt, (T, D), dev), _dev_opt(n, "n", dt, (T, D), dev),
+                              _dev_opt(rstd_post, "rstd_post", f32, (T,), dev), _dev_opt(rstd_pre, "rstd_pre", f32, (T,), dev),
+                              _act8(y8, "y8", T, D, dev), _act8(h8, "h8", T, D, dev), _act8(n8, "n8", T, D, dev), eps,
+                              _stream(stream))
+    _check(st, "block_norm_fwd")
+    return h_out, n
+
+
+def block_norm_workspace_bytes(T: int, D: int) -> int:
+    n = lib().block_norm_workspace_bytes(T, D)
+    if n == ctypes.c_size_t(-1).value:
+        raise LoraError(LORA_EINVAL, "block_norm_workspace_bytes", lib().lora_last_error().decode())
+    return int(n)
+
+
+def block_norm_bwd(dn, dh_out, h, y=None, dh=None, dy=None, w_pre=None, w_post=None, gate=None, post_norm=None,
+                   rstd_pre=None, rstd_post=None, dw_pre=None, dw_post=None, dgate=None, gain_offset: float = 0.0,
+                   res_scale: float = 1.0, ws=None, stream=None):
+    """Gradients of block_norm_fwd (see the header): dh of its h (may be dh_out) and, where given, dy,
+    dw_pre, dw_post [D] fp32 and dgate.  h is the forward's h_out, y its y, each a
+    tensor or a pair (codes, scale) in 8 bits."""
+    import torch
+
+    (T, D), dev, f32 = dh.shape, torch.cuda.current_device(), torch.float32
+    like = next((t for t in (dn, dy, w_pre, gate) if t is not None), dh)
+    dt, rt = like.dtype, dh.dtype
+    b = _block(T, D, dt, rt, post_norm, w_post, w_pre, gate, gain_offset, res_scale, dev)
+    whole_h, whole_y = not isinstance(h, (tuple, list)), not isinstance(y, (tuple, list))
+    wp, wn = None, 0
+    if ws is not None or dw_pre is not None or dw_post is not None or (dgate is not None and b.gate_mode == BLOCK_GATE_CHANNEL):
+        wp, wn, ws = _ws_for(ws, lambda: block_norm_workspace_bytes(T, D), dh, stream)
+    dgate_at = None
+    if dgate is not None:
+        if gate is None:
+            raise ValueError("dgate needs a gate")
+        dgate_at = _dev_arg(dgate, "dgate", dt if b.gate_mode == BLOCK_GATE_FULL else f32, gate.shape, dev)
+    st = lib().block_norm_bwd(ctypes.byref(b), _dev_opt(dn, "dn", dt, (T, D), dev), _dev_opt(dh_out, "dh_out", rt, (T, D), dev),
+                              _dev_opt(h, "h", rt, (T, D), dev) if whole_h else None, None if whole_h else _act8(h, "h", T, D, dev),
+                              _dev_opt(y, "y", dt, (T, D), dev) if whole_y else None, None if whole_y else _act8(y, "y", T, D, dev),
+                              _dev_opt(rstd_post, "rstd_post", f32, (T,), dev), _dev_opt(rstd_pre, "rstd_pre", f32, (T,), dev),
+                              _dev_arg(dh, "dh", rt, (T, D), dev), _dev_opt(dy, "dy", dt, (T, D), dev),
+                              _dev_opt(dw_pre, "dw_pre", f32, (D,), dev), _dev_opt(dw_post, "dw_post", f32, (D,), dev), dgate_at,
+                              wp, wn, _stream(stream))
+    _check(st, "block_norm_bwd")
+    return dh, dy
 
 
 # --- kernel timing hook (benchmarks) -----------------------------------------------

@@ -1,0 +1,227 @@
+"""The LoRA backward from an input kept in 8 bits, on the GPU: bf16 and quantized weights, u saved
+and recomputed, against the definition in 64 bits; and the checkpointed chain with a stash in 8
+bits, which is bitwise the single calls."""
+import pytest
+import torch
+
+import block_reference as ref
+import paper_2606_19528_amd as lm
+from workloads import lora_inputs, quant_weight
+
+pytestmark = pytest.mark.gpu
+BF16, F32, F64 = torch.bfloat16, torch.float32, torch.float64
+
+
+def run(d, x8, W, u, s, want_dx=True, ws=None, stream=None):
+    """(dx, dA, dB) of the entry point for W (a tensor or a quantized weight's dict)."""
+    T, K = x8[0].shape
+    N, r = d["B"].shape
+    dx = torch.full((T, K), 9.0, dtype=BF16, device="cuda") if want_dx else None
+    dA, dB = torch.full((r, K), 9.0, device="cuda"), torch.full((N, r), 9.0, device="cuda")
+    fn = lm.lora_linear_bwd_q_x8 if isinstance(W, dict) else lm.lora_linear_bwd_x8
+    fn(x8, W, d["A"], d["B"], u, d["dy"], dx, dA, dB, s, ws=ws, stream=stream)
+    return dx, dA, dB
+
+
+def case(T, K, N, r, bits=16, group=128, seed=0):
+    inp = lora_inputs(T, K, N, r, seed=seed)
+    codes, scale = ref.act8(inp["x"])
+    W = inp["W"]
+    wide = W
+    if bits != 16:
+        W = quant_weight(N, K, bits, group, seed=seed + 1)
+        q = W["codes"]
+        if bits == 4:
+            q = torch.stack([q & 15, q >> 4], 2).view(N, K)
+        wide = (q.double() * W["scale"].double().T.repeat_interleave(group, 1) + W["offset"].double().T.repeat_interleave(group, 1))
+        wide = wide.float().to(BF16)  # as the product takes it: one fp32 rounding, then bf16
+        W = {k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in W.items()}
+    else:
+        W = W.cuda()
+    d = {k: inp[k].cuda() for k in ("A", "B", "dy")}
+    return inp, d, (codes.cuda(), scale.cuda()), ref.act8_values(codes, scale), W, wide
+
+
+def check(got, inp, xq, wide, u, s):
+    want = ref.linear_bwd(xq, wide, inp["A"], inp["B"], u, inp["dy"], s)
+    err = ref.linear_bwd_bounds(xq, wide, inp["A"], inp["B"], u, inp["dy"], s)
+    for name, g, w, e in zip(("dx", "dA", "dB"), got, want, err):
+        if g is not None:
+            ref.check(g, w, e, name)
+
+
+# one token and a few; ranks of every padding; a last group of 8 and of 120 columns; several token
+# ranges; every tile of the dx product that a call may take
+SIZES = [(1, 8, 8, 1), (1, 256, 264, 8), (3, 136, 64, 4), (24, 1000, 128, 13), (33, 128, 1000, 16), (128, 256, 256, 8),
+         (203, 520, 1032, 17), (257, 1024, 96, 32), (300, 376, 264, 33), (515, 264, 776, 48), (600, 640, 392, 64), (97, 264, 200, 100),
+         (129, 248, 152, 128), (1025, 768, 2048, 8), (2051, 1336, 264, 32), (4100, 256, 520, 24)]
+
+
+@pytest.mark.parametrize("T,K,N,r", SIZES)
+def test_against_the_definition(T, K, N, r):
+    s = 2.0
+    inp, d, x8, xq, W, wide = case(T, K, N, r)
+    u = (xq @ inp["A"].double().T).float()
+    check(run(d, x8, W, u.cuda(), s), inp, xq, wide, u, s)
+    check(run(d, x8, W, None, s), inp, xq, wide, None, s)
+    got = run(d, x8, W, None, s, want_dx=False)
+    check(got, inp, xq, wide, None, s)
+    again = run(d, x8, W, None, s, want_dx=False)
+    assert torch.equal(got[1], again[1]) and torch.equal(got[2], again[2])
+
+
+@pytest.mark.parametrize("bits,group", [(4, 128), (8, 128), (4, 16), (8, 64)])
+@pytest.mark.parametrize("T,K,N,r", [(5, 128, 264, 8), (203, 512, 1032, 16), (1030, 1024, 264, 33), (300, 256, 392, 64)])
+def test_quantized_weight(T, K, N, r, bits, group):
+    s = -0.5
+    inp, d, x8, xq, W, wide = case(T, K, N, r, bits, group)
+    check(run(d, x8, W, None, s), inp, xq, wide, None, s)
+
+
+def test_tiles_of_the_dx_product():
+    """4096 x 3072 outputs take the tile that launches beside dA and dB items never do."""
+    T, K, N, r = 4096, 3072, 64, 32
+    inp, d, x8, xq, W, wide = case(T, K, N, r)
+    check(run(d, x8, W, None, 1.0), inp, xq, wide, None, 1.0)
+    inp, d, x8, xq, W, wide = case(T, K, N, r, 4)
+    check(run(d, x8, W, None, 1.0), inp, xq, wide, None, 1.0)
+
+
+def test_a_scale_that_is_nan_and_one_that_is_zero():
+    """A group that held a value that is not finite: NaN in its columns of dA (and, with u recomputed, in
+    dB); the other columns are as without that token's group.  A group of zeros adds nothing."""
+    T, K, N, r = 70, 384, 136, 8
+    inp, d, x8, xq, W, wide = case(T, K, N, r)
+    u = (xq @ inp["A"].double().T).float()
+    x8[1][11, 1], x8[0][11, 128:256] = torch.nan, 0
+    x8[1][5, 0], x8[0][5, :128] = 0.0, 0
+    xq[5, :128] = 0.0
+    got = run(d, x8, W, u.cuda(), 1.0)
+    assert bool(got[1][:, 128:256].isnan().all())
+    xq[11, 128:256] = 0.0
+    got[1][:, 128:256] = ref.linear_bwd(xq, wide, inp["A"], inp["B"], u, inp["dy"], 1.0)[1][:, 128:256].float().cuda()
+    check(got, inp, xq, wide, u, 1.0)
+    assert bool(run(d, x8, W, None, 1.0)[2].isnan().all())
+
+
+@pytest.mark.parametrize("T", [40, 300])
+def test_rank_zero(T):
+    """dx = dy W as lora_linear_bwd has it (few tokens included); x is not read."""
+    K, N = 264, 136
+    inp, d, x8, xq, W, wide = case(T, K, N, 8)
+    want, got = torch.empty(T, K, dtype=BF16, device="cuda"), torch.empty(T, K, dtype=BF16, device="cuda")
+    lm.lora_linear_bwd(None, W, None, None, None, d["dy"], want, None, None)
+    lm.lora_linear_bwd_x8(None, W, None, None, None, d["dy"], got, None, None)
+    assert torch.equal(got, want)
+
+
+def test_stream_and_graph():
+    """On a stream of the caller's; captured with a workspace, and replayed on new values."""
+    T, K, N, r = 700, 520, 264, 16
+    inp, d, x8, xq, W, wide = case(T, K, N, r)
+    ws = torch.empty(lm.lora_linear_x8_workspace_bytes(T, K, N, r), dtype=torch.uint8, device="cuda")
+    want = run(d, x8, W, None, 1.0)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    got = run(d, x8, W, None, 1.0, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lm.lora_linear_bwd_x8(x8, W, d["A"], d["B"], None, d["dy"], *got, 1.0, ws=ws)
+    for seed in range(1, 5):
+        _, e, y8, *_ = case(T, K, N, r, seed=seed)
+        for k in d:
+            d[k].copy_(e[k])
+        for a, b in zip(x8, y8):
+            a.copy_(b)
+        ws.fill_(255)  # (what it holds does not matter)
+        graph.replay()
+        have = [t.clone() for t in got]
+        want = run(d, x8, W, None, 1.0)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(have, want)), seed
+
+
+# ---- the checkpointed chain -------------------------------------------------------------
+def chain(dims, ranks, seed=0):
+    nodes = []
+    for i, (k, n, r) in enumerate(zip(dims, dims[1:], ranks)):
+        p = lora_inputs(1, k, n, max(r, 1), seed=seed + i)
+        W = (torch.randn(n, k, generator=torch.Generator().manual_seed(seed + 50 + i)) / k ** 0.5).to(BF16).cuda()
+        nd = {"W": W, "A": None, "B": None, "dA": None, "dB": None, "scale": 2.0}
+        if r:
+            nd |= {"A": p["A"].cuda(), "B": p["B"].cuda(), "dA": torch.full((r, k), 9.0, device="cuda"),
+                   "dB": torch.full((n, r), 9.0, device="cuda")}
+        nodes.append(nd)
+    return nodes
+
+
+def by_hand(nodes, x0, g):
+    """The same from single calls: (out, dx0, [(dA, dB)])."""
+    kept, x = [], x0
+    for nd in nodes:
+        kept.append(lm.act8_quantize(x, lm.act8_empty(*x.shape)))
+        y = torch.empty(x.shape[0], nd["W"].shape[0], dtype=BF16, device="cuda")
+        lm.lora_linear_fwd(x, nd["W"], nd["A"], nd["B"], y, None, nd["scale"])
+        x = y
+    grads = []
+    for nd, x8 in zip(reversed(nodes), reversed(kept)):
+        dx = torch.empty(x8[0].shape, dtype=BF16, device="cuda")
+        dA, dB = (None, None) if nd["A"] is None else (torch.empty_like(nd["dA"]), torch.empty_like(nd["dB"]))
+        lm.lora_linear_bwd_x8(x8, nd["W"], nd["A"], nd["B"], None, g, dx, dA, dB, nd["scale"])
+        grads.append((dA, dB))
+        g = dx
+    return x, g, grads[::-1]
+
+
+@pytest.mark.parametrize("T,dims,ranks", [(128, (256, 512, 256), (8, 8)), (203, (264, 520, 136, 392, 128, 256), (8, 16, 4, 32, 13)),
+                                          (64, (128, 128), (8,)), (77, (256, 136, 256, 264, 128, 256, 64), (8, 0, 8, 0, 4, 0)),
+                                          (1100, (1024, 264, 1024), (16, 8))])
+@pytest.mark.parametrize("two_streams", [False, True])
+@pytest.mark.parametrize("pinned", [True, False])
+def test_chain(T, dims, ranks, two_streams, pinned):
+    nodes = chain(dims, ranks)
+    g = torch.Generator().manual_seed(3)
+    x0, gn = (torch.randn(T, d, generator=g).to(BF16).cuda() for d in (dims[0], dims[-1]))
+    ws_bytes, host_bytes = lm.lora_ckpt_sizes_x8(nodes, T)
+    stash = torch.empty(host_bytes, dtype=torch.uint8, pin_memory=pinned)
+    ws = torch.full((ws_bytes,), 255, dtype=torch.uint8, device="cuda")
+    out, dx0 = torch.empty(T, dims[-1], dtype=BF16, device="cuda"), torch.empty_like(x0)
+    want = by_hand(nodes, x0, gn)
+    cs = torch.cuda.Stream()
+    xs = torch.cuda.Stream() if two_streams else cs
+    for s in {cs, xs}:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(2):  # the second on what the first left
+        lm.lora_ckpt_forward_x8(nodes, x0, out, stash, ws, cs, xs)
+        lm.lora_ckpt_backward_x8(nodes, gn, dx0, stash, ws, cs, xs)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want[0]) and torch.equal(dx0, want[1])
+    for nd, (dA, dB) in zip(nodes, want[2]):
+        if dA is not None:
+            assert torch.equal(nd["dA"], dA) and torch.equal(nd["dB"], dB)
+
+
+def test_chain_near_the_one_that_keeps_16_bits():
+    """What the 8 bits cost: a value is off by half a 127th of its group's largest at most, and at random,
+    so gradients summed over many tokens by far less than that of their size."""
+    T, dims = 512, (512, 1024, 512)
+    nodes, plain = chain(dims, (16, 16)), chain(dims, (16, 16))
+    g = torch.Generator().manual_seed(4)
+    x0, gn = (torch.randn(T, d, generator=g).to(BF16).cuda() for d in (dims[0], dims[-1]))
+    res = []
+    for nd, sizes, f, b in ((nodes, lm.lora_ckpt_sizes_x8, lm.lora_ckpt_forward_x8, lm.lora_ckpt_backward_x8),
+                            (plain, lm.lora_ckpt_sizes, lm.lora_ckpt_forward, lm.lora_ckpt_backward)):
+        wb, hb = sizes(nd, T)
+        ws, stash = torch.empty(wb, dtype=torch.uint8, device="cuda"), torch.empty(hb, dtype=torch.uint8, pin_memory=True)
+        out, dx0 = torch.empty(T, dims[-1], dtype=BF16, device="cuda"), torch.empty_like(x0)
+        f(nd, x0, out, stash, ws)
+        b(nd, gn, dx0, stash, ws)
+        torch.cuda.synchronize()
+        res.append((out, dx0, [t for n in nd for t in (n["dA"], n["dB"])]))
+    assert torch.equal(res[0][0], res[1][0])
+    for a, b in zip(res[0][2], res[1][2]):
+        # Gaussian groups of 128: largest 2.7 deviations, a step 2.7 / 127, its rounding's deviation 0.29
+        # of it: 0.6 % of a value's; and bf16 operands of the other side, 2^-9
+        assert float((a - b).norm() / b.norm()) <= 0.0062 + 2.0 ** -8
