@@ -24,31 +24,40 @@ __device__ __forceinline__ uint32_t a8_row(const A8Div &d, uint32_t u) {
   return d.n == 1 ? u : __umulhi(u, d.mul) >> d.shift;
 }
 
+// What a lane takes of unit u: where its 8 values are, and whether they are there at all.  (Lanes
+// without any load the first values: a load in a branch is waited for at its end, so
+// the units' loads would come one after the other.)
+struct A8At {
+  int64_t at;
+  bool in;
+};
+__device__ __forceinline__ A8At a8_at(const A8Div &d, uint32_t u, uint32_t units, int D, int lane) {
+  const uint32_t row = a8_row(d, u);
+  const int col = (int)(u - row * d.n) * ACT8_G + lane * 8;
+  const bool in = u < units && col < D;
+  return {in ? (int64_t)row * D + col : 0, in};
+}
+
 template <class E, int U>
 __global__ __launch_bounds__(A8_NT) void act8_quantize_kernel(const void *x, int8_t *codes, float *scale, uint32_t units, int D,
                                                               A8Div div) {
   const int lane = threadIdx.x & 15;
   const uint32_t u0 = blockIdx.x * (uint32_t)(A8_UNITS * U) + threadIdx.x / 16;
-  float f[U][8];
-  int64_t at[U];
-  bool in[U];
+  Raw8<E> r[U];
+  A8At a[U];
 #pragma unroll
   for (int k = 0; k < U; ++k) {
-    const uint32_t u = u0 + k * A8_UNITS, row = a8_row(div, u);
-    const int col = (int)(u - row * div.n) * ACT8_G + lane * 8;
-    in[k] = u < units && col < D;
-    at[k] = (int64_t)row * D + col;
-    if (in[k]) load8(E(), (const typename E::T *)x + at[k], f[k]);
-    else
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[k][e] = 0.0f;
+    a[k] = a8_at(div, u0 + k * A8_UNITS, units, D, lane);
+    r[k].load(x, a[k].at);
   }
 #pragma unroll
   for (int k = 0; k < U; ++k) {
-    float s;
-    const uint2 q = act8_encode(E(), f[k], &s);
+    float f[8], s;
+    r[k].keep_if(a[k].in);
+    r[k].get(f);
+    const uint2 q = act8_encode(E(), f, &s);
     const uint32_t u = u0 + k * A8_UNITS;
-    if (in[k]) *(uint2 *)(codes + at[k]) = q;
+    if (a[k].in) *(uint2 *)(codes + a[k].at) = q;
     if (lane == 0 && u < units) scale[u] = s;
   }
 }
@@ -60,27 +69,21 @@ __global__ __launch_bounds__(A8_NT) void act8_dequantize_kernel(const int8_t *co
   const uint32_t u0 = blockIdx.x * (uint32_t)(A8_UNITS * U) + threadIdx.x / 16;
   uint2 q[U];
   float s[U];
-  int64_t at[U];
-  bool in[U];
+  A8At a[U];
 #pragma unroll
   for (int k = 0; k < U; ++k) {
-    const uint32_t u = u0 + k * A8_UNITS, row = a8_row(div, u);
-    const int col = (int)(u - row * div.n) * ACT8_G + lane * 8;
-    in[k] = u < units && col < D;
-    at[k] = (int64_t)row * D + col;
-    if (in[k]) {
-      q[k] = *(const uint2 *)(codes + at[k]);
-      s[k] = scale[u];
-    }
+    const uint32_t u = u0 + k * A8_UNITS;
+    a[k] = a8_at(div, u, units, D, lane);
+    q[k] = *(const uint2 *)(codes + a[k].at);
+    s[k] = scale[u < units ? u : 0];
   }
 #pragma unroll
   for (int k = 0; k < U; ++k) {
-    if (!in[k]) continue;
     float f[8];
     act8_floats(q[k], f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] *= s[k];
-    store8(E(), (typename E::T *)x + at[k], f);
+    if (a[k].in) store8(E(), (typename E::T *)x + a[k].at, f);
   }
 }
 

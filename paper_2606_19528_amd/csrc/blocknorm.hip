@@ -17,26 +17,6 @@
 
 namespace lora {
 
-// 8 values as loaded.
-template <class E>
-struct Raw8 {
-  static constexpr int N = 8 / E::VEC;
-  u32x4 v[N];
-  __device__ __forceinline__ void load(const void *base, int64_t i) {
-    const typename E::T *p = (const typename E::T *)base + i;
-#pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = ld16(p + k * E::VEC);
-  }
-  __device__ __forceinline__ void zero() {
-#pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = zero16();
-  }
-  __device__ __forceinline__ void get(float *f) const {
-#pragma unroll
-    for (int k = 0; k < N; ++k) unpack_vec(E(), v[k], f + k * E::VEC);
-  }
-};
-
 // Sums over the TPR threads of a row, the same bits in each.
 template <int TPR>
 struct RowSum {
@@ -85,6 +65,12 @@ __device__ __forceinline__ float row_rstd(const float (&x)[NV][8], int D, float 
 // Workgroup of rows of TPR threads: several rows where a wave holds one.
 constexpr int bn_threads(int tpr) { return tpr == 64 ? 256 : tpr; }
 
+template <class E>
+__device__ __forceinline__ void load8(E, const void *p, int64_t i, float *f) {
+  Raw8<E> r;
+  r.load(p, i);
+  r.get(f);
+}
 template <class E>
 __device__ __forceinline__ void round_to(E, float *f) {
 #pragma unroll
@@ -147,7 +133,7 @@ __global__ __launch_bounds__(bn_threads(TPR)) void block_norm_fwd_kernel(BlockNo
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = 1.0f;
         if (a.w_post && col < D) {
-          load8(E(), (const typename E::T *)a.w_post + col, w);
+          load8(E(), a.w_post, col, w);
 #pragma unroll
           for (int e = 0; e < 8; ++e) w[e] += a.off;
         }
@@ -194,7 +180,7 @@ __global__ __launch_bounds__(bn_threads(TPR)) void block_norm_fwd_kernel(BlockNo
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] = 1.0f;
     if (a.w_pre && col < D) {
-      load8(E(), (const typename E::T *)a.w_pre + col, w);
+      load8(E(), a.w_pre, col, w);
 #pragma unroll
       for (int e = 0; e < 8; ++e) w[e] += a.off;
     }
@@ -300,7 +286,7 @@ __global__ __launch_bounds__(bn_threads(TPR)) void block_norm_bwd_kernel(BlockNo
           w[e] = 1.0f;
         }
         if (a.w_pre && col < D) {
-          load8(E(), (const typename E::T *)a.w_pre + col, w);
+          load8(E(), a.w_pre, col, w);
 #pragma unroll
           for (int e = 0; e < 8; ++e) w[e] += a.off;
         }
@@ -341,7 +327,7 @@ __global__ __launch_bounds__(bn_threads(TPR)) void block_norm_bwd_kernel(BlockNo
         w[e] = 1.0f;
       }
       if (a.w_post && col < D) {
-        load8(E(), (const typename E::T *)a.w_post + col, w);
+        load8(E(), a.w_post, col, w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] += a.off;
       }

@@ -4,8 +4,9 @@
 // Codes are whole numbers up to 127, exact in bf16, so a product on the matrix
 // cores takes them as they are; a scale belongs to a row and 128 columns of x and goes
 // to the other side of the product: in u to the group's sum, in dA to du.  du and u
-// are fp32 and stay so: v = hi + lo, two bf16 each, the rest of v below 2^-17 of it.
-// (An fp32 gradient of whose operand the rounding to bf16 is left has 2^-9.)
+// are fp32 and stay so: v as the sum of three bf16, which hold its 24 bits.  (Two leave
+// 2^-18 of it, 2e-6 of the gradient's norm; one 2^-9.  The third product takes 1 us of
+// the 22 of 8192 -> 3072 at 4096 tokens.)
 #include <algorithm>
 
 #include "act8.hpp"
@@ -231,18 +232,22 @@ __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, float 
 #pragma unroll
     for (int j = 0; j < JB; ++j) acc[q][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   auto compute = [&](const Step &st) {
-    u32x4 hi[JB], lo[JB], xt[8];
+    u32x4 vb[JB][3], xt[8];
 #pragma unroll
     for (int j = 0; j < JB; ++j) {
       float v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = X8 ? st.v[j][i] * st.s[i] : st.v[j][i];
-      hi[j] = pack_vec(BF16(), v);
-      float h[8];
-      unpack_vec(BF16(), hi[j], h);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] -= h[i];
-      lo[j] = pack_vec(BF16(), v);
+      for (int p = 0; p < 3; ++p) {  // each the next bits of what is left
+#pragma unroll
+        for (int d = 0; d < 4; ++d) vb[j][p][d] = pack_bf16x2(v[2 * d], v[2 * d + 1]);
+        if (p == 2) break;
+        float h[8];
+        unpack_vec(BF16(), vb[j][p], h);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] -= h[i];
+      }
     }
     if constexpr (X8) {
       // column q of the 8 tokens: byte q of each
@@ -264,8 +269,8 @@ __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, float 
     for (int q = 0; q < 8; ++q)
 #pragma unroll
       for (int j = 0; j < JB; ++j) {
-        mma16(BF16(), acc[q][j], xt[q], hi[j]);
-        mma16(BF16(), acc[q][j], xt[q], lo[j]);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) mma16(BF16(), acc[q][j], xt[q], vb[j][p]);
       }
   };
   {
