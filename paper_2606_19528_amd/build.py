@@ -19,7 +19,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "liblora_mi355x.so")
 SOURCES = ["gemm.hip", "gemm_q.hip", "skinny.hip", "head.hip", "topk.hip", "narrow.hip", "hostcopy.hip", "embed.hip",
-           "tokenloss.hip", "gradclip.hip", "act8.hip", "blocknorm.hip", "x8prod.hip", "api.cpp", "ckpt.cpp", "step.cpp",
+           "tokenloss.hip", "gradclip.hip", "act8.hip", "blocknorm.hip", "blocknorm_bwd.hip", "x8prod.hip", "api.cpp", "ckpt.cpp", "step.cpp",
            "block.cpp", "static_ws.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -93,7 +93,8 @@ template <class E>
 struct Raw8 {
   static constexpr int N = 8 / E::VEC;
   u32x4 v[N];
-  __device__ __forceinline__ void load(const void *base, int64_t i) {
+  template <class I>
+  __device__ __forceinline__ void load(const void *base, I i) {
     const typename E::T *p = (const typename E::T *)base + i;
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = ld16(p + k * E::VEC);

@@ -1,0 +1,366 @@
+// blocknorm_bwd.hip -- the backward of blocknorm.hip, from dn and dh', the gradients of
+// the next block's normed input and of the stream behind this one.  With hh = h' r1, yh = y r2,
+// e = dn (w1 + o):
+//   dh = dh' + r1 (e - hh mean(e hh))                 dw1 = sum over rows of dn hh
+//   z = a dh,  f = g z (w2 + o)                       dg  = z yn, summed where g is broadcast
+//   dy = r2 (f - yh mean(f yh))                       dw2 = sum over rows of g z yh
+// One pass over the data (blocknorm.hpp): 4096 x 3072 in bf16 from 8-bit copies 28.2 us (126 MB, 4.5
+// TB/s), where a form with a branch a vector took 52: beside the memory path the vector
+// instructions count, a few hundred for 8 columns.  dh is linear in the
+// first mean, so that the second comes from sums taken with it: dh = p - c q with
+// p = dh' + r1 e, q = r1 hh and c = mean(e hh), and for weights k of a column
+//   sum k dh yh = sum k p yh - c sum k q yh,
+// one meeting of a row's waves instead of two.  Sums are fp32 in a fixed order.
+#include <algorithm>
+
+#include "blocknorm.hpp"
+
+namespace lora {
+
+// A row kept whole or in 8 bits, as loaded.  (Here and below one branch stands around all of a
+// lane's vectors: a branch in each kept the loads from being ahead of one another.)
+template <class E, int W, int NV>
+__device__ __forceinline__ void src_load(Raw8<E> (&r)[NV], const void *whole, const Act8In &k, int64_t row, int ng,
+                                         const BnCols<W, NV> &c) {
+  if (k.codes) {
+    const int8_t *q = k.codes + row * c.D;
+    const float *s = k.scale + row * ng;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const uint2 t = *(const uint2 *)(q + c.at(v));
+      r[v].v[0] = u32x4{t.x, t.y, __builtin_bit_cast(uint32_t, s[c.at(v) / ACT8_G]), 0u};
+    }
+  } else {
+    bn_load<E>(r, whole, row * c.D, c);
+  }
+}
+template <class E, int NV>
+__device__ __forceinline__ void src_floats(float (&x)[NV][8], const Raw8<E> (&r)[NV], const Act8In &k, float m) {
+  if (k.codes) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const u32x4 q = r[v].v[0];
+      act8_floats(make_uint2(q[0], q[1]), x[v]);
+      const float s = __builtin_bit_cast(float, (uint32_t)q[2]) * m;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[v][e] *= s;
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      r[v].get(x[v]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[v][e] *= m;
+    }
+  }
+}
+// x *= gains + off.
+template <class E, int NV>
+__device__ __forceinline__ void times(float (&x)[NV][8], const Raw8<E> (&w)[NV], float off) {
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    float f[8];
+    w[v].get(f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[v][e] *= f[e] + off;
+  }
+}
+
+// GRADS: the gradients that are sums over rows too.  Workgroups of 8 waves then (16 for the longest rows), which take
+// rows in turn and leave their sums of each column in part[0..2][workgroup][D]: of w1, w2
+// and a gate [D].
+constexpr int bnb_rows(int w, bool grads) { return grads ? (w >= 8 ? 1 : 8 / w) : w == 1 ? 4 : 1; }
+constexpr int bnb_threads(int w, bool grads) { return 64 * w * bnb_rows(w, grads); }
+
+template <class E, class R, int W, int NV, bool GRADS>
+__global__ __launch_bounds__(bnb_threads(W, GRADS)) void block_norm_bwd_kernel(BlockNormBwd a) {
+  constexpr int RPW = bnb_rows(W, GRADS), NWV = W * RPW;  // rows and waves of a workgroup
+  __shared__ float red[2][3][NWV];
+  const BnCols<W, NV> c{(int)threadIdx.x % (64 * W), a.D};
+  const int D = a.D, sub = bn_sub<W>(), wave = threadIdx.x >> 6;
+  const float inv_d = 1.0f / (float)D;
+  const bool need_y = a.post || a.dgate, block = a.dy || a.dgate || a.want_w2;
+  float s1[NV][8], s2[NV][8], sg[NV][8];
+  if constexpr (GRADS) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s1[v][e] = s2[v][e] = sg[v][e] = 0.0f;
+  }
+  int slot = 0;
+  // (all waves of a workgroup go round as often as its first row needs)
+  for (int64_t r0 = (int64_t)blockIdx.x * RPW; r0 < a.T; r0 += (int64_t)gridDim.x * RPW) {
+    const bool live = r0 + sub < a.T;
+    const int64_t row = live ? r0 + sub : a.T - 1, at = row * D;
+    Raw8<E> dnr[NV], yr[NV], gr[NV], w1[NV], w2[NV];
+    Raw8<R> dhr[NV], hr[NV];
+    if (a.dn) {
+      bn_load<E>(dnr, a.dn, at, c);
+      src_load<R>(hr, a.h, a.h8, row, a.ng, c);
+    }
+    if (a.dh_out) bn_load<R>(dhr, a.dh_out, at, c);
+    if (need_y) src_load<E>(yr, a.y, a.y8, row, a.ng, c);
+    if (a.gate_mode & 1) bn_load<E>(gr, a.gate, a.gate_mode == BN_GATE_FULL ? at : 0, c);  // (channel, full)
+    if (a.w_pre) bn_load<E>(w1, a.w_pre, 0, c);
+    if (a.w_post) bn_load<E>(w2, a.w_post, 0, c);
+    const float r1 = a.dn ? a.rstd_pre[row] : 0.0f, r2 = a.post ? a.rstd_post[row] : 1.0f;
+    const float gt = a.gate_mode == BN_GATE_TOKEN ? E::to_float(((const typename E::T *)a.gate)[row]) : 1.0f;
+    float h[NV][8], p[NV][8], y[NV][8], k[NV][8];  // hh, p and then dh, yh
+    float ca = 0.0f, cb = 0.0f, cc = 0.0f;
+    // e = dn (w1 + o), p = dh' + r1 e.  Lanes past the row, and rows past the last, have dn and y
+    // zeros, so that they add nothing to a sum.
+    if (a.dn) {
+      src_floats<R>(h, hr, a.h8, r1);
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        dnr[v].keep_if(live && c.in(v));
+        dnr[v].get(p[v]);
+        if constexpr (GRADS) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s1[v][e] = __builtin_fmaf(p[v][e], h[v][e], s1[v][e]);
+        }
+      }
+      if (a.w_pre) times<E>(p, w1, a.off);
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          ca = __builtin_fmaf(p[v][e], h[v][e], ca);
+          p[v][e] *= r1;
+        }
+    } else {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[v][e] = p[v][e] = 0.0f;
+    }
+    if (a.dh_out) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        float f[8];
+        dhr[v].get(f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[v][e] += f[e];
+      }
+    }
+    // k = a g (w2 + o), without a gate a token: f = k gt dh
+    if (block) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) k[v][e] = a.res_scale;
+      if (a.gate_mode & 1) times<E>(k, gr, 0.0f);
+      if (a.w_post) times<E>(k, w2, a.off);
+      if (need_y) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) yr[v].keep_if(live && c.in(v));
+        src_floats<E>(y, yr, a.y8, r2);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float ky = k[v][e] * y[v][e];
+            cb = __builtin_fmaf(ky, p[v][e], cb);
+            cc = __builtin_fmaf(ky, h[v][e], cc);
+          }
+      }
+    }
+    ca = wave_sum(ca);
+    cb = wave_sum(cb);
+    cc = wave_sum(cc);
+    if constexpr (W > 1) {
+      // (two slots in turn: whoever writes one again has passed the other's barrier, which
+      // every reader of the first has reached)
+      float(*s)[NWV] = red[slot];
+      if ((threadIdx.x & 63) == 0) {
+        s[0][wave] = ca;
+        s[1][wave] = cb;
+        s[2][wave] = cc;
+      }
+      __syncthreads();
+      const int w0 = sub * W;
+      ca = s[0][w0];
+      cb = s[1][w0];
+      cc = s[2][w0];
+#pragma unroll
+      for (int w = 1; w < W; ++w) {
+        ca += s[0][w0 + w];
+        cb += s[1][w0 + w];
+        cc += s[2][w0 + w];
+      }
+      slot ^= 1;
+    }
+    const float q = r1 * (ca * inv_d);            // dh = p - q hh
+    const float fy = __builtin_fmaf(-q, cc, cb);  // sum k dh yh
+    if (a.gate_mode == BN_GATE_TOKEN && a.dgate && c.t == 0 && live) ((float *)a.dgate)[row] = fy;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[v][e] = __builtin_fmaf(-q, h[v][e], p[v][e]);
+      if (live && c.in(v)) store8(R(), (typename R::T *)a.dh + at + c.at(v), p[v]);
+    }
+    if (!block) continue;
+    if constexpr (GRADS) {
+      // a yh dh, for w2 times the gate and for the gate times the gain
+      if (need_y) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float z = a.res_scale * y[v][e] * p[v][e];
+            if (a.want_w2 && !(a.gate_mode & 1)) s2[v][e] = __builtin_fmaf(z, gt, s2[v][e]);
+            h[v][e] = z;
+          }
+        if (a.want_w2 && (a.gate_mode & 1)) {
+#pragma unroll
+          for (int v = 0; v < NV; ++v) {
+            float g[8];
+            gr[v].get(g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s2[v][e] = __builtin_fmaf(h[v][e], g[e], s2[v][e]);
+          }
+        }
+        if (a.want_gate) {
+          if (a.w_post) times<E>(h, w2, a.off);
+#pragma unroll
+          for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sg[v][e] += h[v][e];
+        }
+      }
+    }
+    if (a.dgate && a.gate_mode == BN_GATE_FULL) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[v][e] = a.res_scale * y[v][e] * p[v][e];
+      if (a.w_post) times<E>(h, w2, a.off);
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        if (live && c.in(v)) store8(E(), (typename E::T *)a.dgate + at + c.at(v), h[v]);
+    }
+    if (!a.dy) continue;
+    // dy = r2 (f - yh mean(f yh)), or f
+    const float kf = gt * r2, c2 = kf * (fy * inv_d);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[v][e] = k[v][e] * kf * p[v][e];
+      if (a.post) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[v][e] = __builtin_fmaf(-c2, y[v][e], p[v][e]);
+      }
+      if (live && c.in(v)) store8(E(), (typename E::T *)a.dy + at + c.at(v), p[v]);
+    }
+  }
+  if constexpr (GRADS) {
+    // The rows' sums of the workgroup, one array after the other.
+    __shared__ float cols[RPW > 1 ? RPW - 1 : 1][64 * W * NV * 8 + 4];
+    const int64_t plane = (int64_t)gridDim.x * D;
+    float *const out = a.part + (int64_t)blockIdx.x * D;
+#pragma unroll
+    for (int which = 0; which < 3; ++which) {
+      if (!(which == 0 ? a.want_w1 : which == 1 ? a.want_w2 : a.want_gate)) continue;
+      float(&s)[NV][8] = which == 0 ? s1 : which == 1 ? s2 : sg;
+      if constexpr (RPW > 1) {
+        __syncthreads();
+        if (sub > 0) {
+#pragma unroll
+          for (int v = 0; v < NV; ++v) store8(F32(), &cols[sub - 1][c.col(v)], s[v]);
+        }
+        __syncthreads();
+      }
+      if (sub == 0) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+#pragma unroll
+          for (int k = 1; k < RPW; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[v][e] += cols[k - 1][c.col(v) + e];
+          if (c.in(v)) store8(F32(), out + which * plane + c.col(v), s[v]);
+        }
+      }
+    }
+  }
+}
+
+// out[c] = sum over p < np of part[p][c]: 16 ranges of p, each ascending, for 64 columns a
+// workgroup.
+__global__ __launch_bounds__(256) void block_norm_cols_kernel(const float *part, int np, int D, float *o1, float *o2, float *og) {
+  __shared__ f32x4 red[16][16];
+  const int which = blockIdx.y;
+  float *out = which == 0 ? o1 : which == 1 ? o2 : og;
+  if (!out) return;
+  const int c = threadIdx.x & 15, s = threadIdx.x >> 4, col = blockIdx.x * 64 + 4 * c;  // (D is a multiple of 8)
+  const int per = (np + 15) / 16, p0 = s * per, p1 = min(np, p0 + per);
+  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (col < D) {
+    const float *src = part + ((int64_t)which * np + p0) * D + col;
+#pragma unroll 8
+    for (int p = p0; p < p1; ++p, src += D) x += *(const f32x4 *)src;
+  }
+  red[s][c] = x;
+  __syncthreads();
+  if (s != 0 || col >= D) return;
+#pragma unroll
+  for (int k = 1; k < 16; ++k) x += red[k][c];
+  *(f32x4 *)(out + col) = x;
+}
+
+// Workgroups that sum over rows: one a CU, of 8 waves, with one vector a lane where the row allows it
+// (4096 x 2048 with an fp32 stream 37.7 us, in 12 waves 39.3, with two vectors 40.8, two
+// workgroups a CU 39.3).
+constexpr int BNB_PARTS = 256;
+static BnShape grads_shape(int64_t D) {
+  const int64_t n = (D + 511) / 512;
+  if (n <= 1) return {1, 1};
+  if (n <= 2) return {2, 1};
+  if (n <= 4) return {4, 1};
+  if (n <= 8) return {8, 1};
+  if (n <= 16) return {8, 2};
+  return {16, 2};
+}
+
+int block_norm_parts(int64_t T, int64_t D) {
+  const int rows = bnb_rows(grads_shape(D).w, true);
+  return (int)std::min<int64_t>((T + rows - 1) / rows, BNB_PARTS);
+}
+
+template <class E, class R>
+static hipError_t bwd_grads(const BlockNormBwd &a, hipStream_t st) {
+  const BnShape s = grads_shape(a.D);
+  const int np = block_norm_parts(a.T, a.D);
+#define BWD(W, NV) hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, true>), dim3(np), dim3(bnb_threads(W, true)), 0, st, a)
+  switch (s.w * 8 + s.nv) {
+    case 1 * 8 + 1: BWD(1, 1); break;
+    case 2 * 8 + 1: BWD(2, 1); break;
+    case 4 * 8 + 1: BWD(4, 1); break;
+    case 8 * 8 + 1: BWD(8, 1); break;
+    case 8 * 8 + 2: BWD(8, 2); break;
+    default: BWD(16, 2); break;
+  }
+#undef BWD
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(block_norm_cols_kernel, dim3((a.D + 63) / 64, 3), dim3(256), 0, st, a.part, np, a.D, a.want_w1, a.want_w2,
+                     a.want_gate);
+  return hipGetLastError();
+}
+
+template <class E, class R>
+static hipError_t bwd_rows(const BlockNormBwd &a, hipStream_t st) {
+  if (a.want_w1 || a.want_w2 || a.want_gate) return bwd_grads<E, R>(a, st);
+  const BnShape s = bn_shape(a.T, a.D);
+  const dim3 grid((unsigned)(s.w == 1 ? (a.T + 3) / 4 : a.T));
+#define BWD(W, NV) hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false>), grid, dim3(bnb_threads(W, false)), 0, st, a)
+  BN_SHAPES(s, BWD)
+#undef BWD
+  return hipGetLastError();
+}
+
+hipError_t launch_block_norm_bwd(const BlockNormBwd &a, Dtype d, Dtype res, hipStream_t st) {
+  if (d == DT_F32) return bwd_rows<F32, F32>(a, st);
+  return res == DT_F32 ? bwd_rows<BF16, F32>(a, st) : bwd_rows<BF16, BF16>(a, st);
+}
+
+}  // namespace lora

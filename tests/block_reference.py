@@ -106,13 +106,16 @@ def norm_fwd(h, y, post, w_post, gate, w_pre, eps, off, a):
 
 def norm_bwd(dn, dh_out, h, y, post, w_post, gate, w_pre, r2, r1, off, a):
     """dict of dh, dy, dw_pre, dw_post, dgate, and of their bounds before the outputs' rounding.
-    h and y as values in 64 bits; r1, r2 [T] as given."""
+    h and y as values in 64 bits; r1, r2 [T] as given.  A sum over a row of weights k times dh may be
+    taken in two parts, dh = p - q hh with q = r1 c: sum k p - q sum k hh, whose terms are up to
+    |k dh| + 2 |k q hh| together."""
     like = dn if dn is not None else dh_out
     T, D = like.shape
     over_rows = (T / 32.0 + 64.0) * U  # a sum over rows: rows of a workgroup in turn, then 512 sums in 16 ranges
     out, err = {}, {}
     dh = torch.zeros(T, D, dtype=F64) if dh_out is None else dh_out.double()
     eh = torch.zeros(T, D, dtype=F64)
+    parts = torch.zeros(T, D, dtype=F64)  # 2 |q hh|
     if dn is not None:
         hh, e = h.double() * r1.double()[:, None], dn.double() * _gain(w_pre, off, D)
         c = (e * hh).mean(1, keepdim=True)
@@ -121,6 +124,7 @@ def norm_bwd(dn, dh_out, h, y, post, w_post, gate, w_pre, r2, r1, off, a):
         eh = r * (4.0 * U * e.abs() + hh.abs() * ec + 4.0 * U * (hh * c).abs())
         dh = dh + r1.double()[:, None] * (e - hh * c)
         eh = eh + U * dh.abs()
+        parts = 2.0 * r * (hh * c).abs()
         out["dw_pre"] = (dn.double() * hh).sum(0)
         err["dw_pre"] = (over_rows + 3.0 * U) * (dn.double() * hh).abs().sum(0)
     out["dh"], err["dh"] = dh, eh
@@ -136,7 +140,7 @@ def norm_bwd(dn, dh_out, h, y, post, w_post, gate, w_pre, r2, r1, off, a):
                 out["dgate"], err["dgate"] = per.sum(0), (eper + over_rows * per.abs()).sum(0)
             elif gate.shape == (T, 1):
                 out["dgate"] = per.sum(1, keepdim=True)
-                err["dgate"] = (eper + SUM * U * per.abs()).sum(1, keepdim=True)
+                err["dgate"] = (eper + (SUM + 3.0) * U * (per.abs() + abs(a) * parts * (yh * w2).abs())).sum(1, keepdim=True)
             else:
                 out["dgate"], err["dgate"] = per, eper
         if post:
@@ -145,7 +149,7 @@ def norm_bwd(dn, dh_out, h, y, post, w_post, gate, w_pre, r2, r1, off, a):
     f, ef = z * g * w2, (ez * (g * w2).abs() + 3.0 * U * (z * g * w2).abs())
     if post:
         c = (f * yh).mean(1, keepdim=True)
-        ec = (ef * yh.abs() + (SUM + 2.0) * U * (f * yh).abs()).mean(1, keepdim=True)
+        ec = (ef * yh.abs() + (SUM + 3.0) * U * ((f * yh).abs() + abs(a) * parts * (g * w2 * yh).abs())).mean(1, keepdim=True)
         r = r2.double()[:, None]
         out["dy"] = r * (f - yh * c)
         err["dy"] = r.abs() * (ef + yh.abs() * ec + 4.0 * U * (f.abs() + (yh * c).abs()))
