@@ -729,7 +729,7 @@ lora_status_t bwd_impl(const void *x, const void *W, const void *qc, const float
 // launch of their own (x8prod.hip) that reads x's codes and dy once at the memory's
 // rate; u, where it is not saved, from the codes.
 struct X8Layout {
-  size_t u, du, dutail, acat, planes, total;
+  size_t u, du, dutail, acat, sync, slots, total;
   int ldt, u_parts;
   RowSplit sp;
 };
@@ -748,8 +748,11 @@ X8Layout x8_layout(int64_t T, int64_t K, int64_t N, int64_t r) {
   off += round256((size_t)T * L.ldt * 2);
   L.acat = off;  // [nsplit * r][K]: A repeated once per partial
   off += L.sp.nsplit > 1 ? round256((size_t)L.sp.nsplit * r * K * 2) : 0;
-  L.planes = off;  // dA and dB of each range of tokens
-  off += round256(x8_plan(T, K, N, r).bytes);
+  const X8Plan p = x8_plan(T, K, N, r);
+  L.sync = off;  // the flags of the meetings over ranges of tokens
+  off += round256(p.sync_bytes);
+  L.slots = off;  // dA's and dB's tiles of each range
+  off += round256(p.slot_bytes);
   L.total = off;
   return L;
 }
@@ -800,7 +803,7 @@ lora_status_t bwd_x8_impl(const int8_t *xc, const float *xs, const void *W, cons
     if (e != hipSuccess) return hip_fail(e, "x8_down launch");
   }
   const int ns = L.sp.nsplit;
-  pr.du = (const float *)(wsb + L.du); pr.du_parts = ns;
+  pr.du = (float *)(wsb + L.du); pr.du_parts = ns;
   {
     RowArgs ra{};
     ra.X = dy; ra.ldx = d_out; ra.M = (int)T; ra.L = (int)d_out;
@@ -836,7 +839,7 @@ lora_status_t bwd_x8_impl(const int8_t *xc, const float *xs, const void *W, cons
   }
   pr.dA = dA; pr.dB = dB; pr.scale = scale;
   pr.T = (int)T; pr.K = (int)d_in; pr.N = (int)d_out; pr.r = (int)r;
-  pr.planes = (float *)(wsb + L.planes);
+  pr.sync = (meet_word *)(wsb + L.sync); pr.slots = (float *)(wsb + L.slots); pr.gen = next_tag();
   Timed t(K_X8_PROD, st);
   e = launch_x8_prod(pr, st);
   t.done();

@@ -516,21 +516,24 @@ struct X8Down {
 int x8_down_parts(int64_t T, int64_t K);
 hipError_t launch_x8_down(const X8Down &a, hipStream_t st);
 // dA [r][K] = du^T x and dB [N][r] = scale dy^T u, with du and u as the sums of
-// du_parts and u_parts planes [T][r] fp32, added in ascending order.  `planes`:
-// X8Plan::bytes, the sums of the ranges of tokens.
+// du_parts and u_parts planes [T][r] fp32, added in ascending order and left in the first (a u in
+// one part is only read).  sync and slots: where the tokens go in ranges, X8Plan's bytes for
+// the meetings of an item's ranges and their sums.
 struct X8Prod {
   Act8In x;
   const void *dy;
-  const float *du, *u;
+  float *du;
+  const float *u;
   int du_parts, u_parts;
   float *dA, *dB;
   float scale;
   int T, K, N, r;
-  float *planes;
+  meet_word *sync, gen;  // (gen: this launch's tag, never 0)
+  float *slots;
 };
 struct X8Plan {
   int parts, chunk;  // ranges of tokens and their length
-  size_t bytes;
+  size_t sync_bytes, slot_bytes;
 };
 X8Plan x8_plan(int64_t T, int64_t K, int64_t N, int64_t r);
 hipError_t launch_x8_prod(const X8Prod &a, hipStream_t st);

@@ -11,6 +11,7 @@
 
 #include "act8.hpp"
 #include "launch.hpp"
+#include "meet_flags.hpp"
 
 namespace lora {
 
@@ -156,88 +157,122 @@ hipError_t launch_x8_down(const X8Down &a, hipStream_t st) {
 }
 
 // ---- dA = du^T x, dB = s dy^T u ------------------------------------------------------
-// An item is 128 columns of x (a group: one scale a token) or of dy by 16 JB ranks,
-// over a range of tokens.  Its waves take steps of 32 tokens in turn: lane (c = l % 16, g = l / 16)
-// loads 8 columns of tokens 8 g .. 8 g + 7, and the 8 tokens of one of its columns are
-// an operand whose reduction axis is the token axis; product q takes column 8 c + q of
-// every c.  The waves' tiles are summed pairwise.
+// An item is 128 columns of x (a group: one scale a token) or 64 of dy, 128 bytes of a row
+// either way, by 16 JB ranks, over a range of tokens.  Its waves take steps of 32 tokens in turn:
+// lane (c = l % 16, g = l / 16) loads Q = 8 (4) columns of tokens 8 g .. 8 g + 7, and the 8
+// tokens of one of its columns are an operand whose reduction axis is the token axis;
+// product q takes column Q c + q of every c.  The waves' tiles are summed pairwise.
+// The loads' latency bounds it, so they are two steps ahead.
 constexpr int X8P_NW = 8, X8P_ROWS = 32;
 
 struct X8Unit {
   const void *X;
   const float *scale, *V;
   float *out;
-  int L, ng, vparts, t0, t1, cb, jg;
+  int L, ng, t0, t1, cb, jg;
   float mult;
   bool transposed;  // out [r][L], else [L][r]
 };
 
-template <int JB, bool X8>
-__device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, float (*red)[ACT8_G][JB * 16 + 1]) {
+// LDS floats in which a wave turns a step's V around: 32 tokens of up to 16 JB ranks, 16 floats
+// more after each 8 tokens (the four quarters of a wave then read different banks), and the scales.
+constexpr int X8P_SLOT(int jb) { return ACT8_G * 16 * jb; }  // floats of a tile in the workspace
+constexpr int x8_turn(int jb) { return X8P_ROWS * 16 * jb + 3 * 16 + X8P_ROWS; }
+
+template <int JB, bool FLAT, bool X8>
+__device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, int item, int part, int parts, float *lds) {
   constexpr uint32_t OOB = 0x80000000u;
-  constexpr int ES = X8 ? 1 : 2, XW = X8 ? 2 : 4;
+  constexpr int ES = X8 ? 1 : 2, Q = 8 / ES, COLS = 16 * Q, RB = 16 * JB, TILE = COLS * RB, NT = 64 * X8P_NW;
+  float(*red)[COLS][RB + 1] = (float(*)[COLS][RB + 1])lds;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = n.cb * ACT8_G + 8 * c, r = a.r;
-  const int64_t plane = (int64_t)a.T * r;
-  struct Step {
-    uint32_t x[8][XW];
-    float v[JB][8], s[8];
+  float *const turn = lds + wave * x8_turn(JB), *const turn_s = turn + X8P_ROWS * RB + 48;
+  const int col = n.cb * COLS + Q * c, r = a.r;
+  const int row = FLAT ? r : RB;  // of V in `turn`
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  struct StepX {
+    u32x2 x[8];
+  };
+  struct StepV {
+    f32x4 v[2 * JB];
+    float s;
   };
   // Loads go through buffer resources based at the step's first token: tokens past the range,
   // columns past L and ranks past r read zeros.
-  auto load = [&](int tb, Step &st) {
+  auto load_x = [&](int tb, StepX &st) {
     const int rows = max(0, min(X8P_ROWS, n.t1 - tb));
     const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(
         (void *)((const char *)n.X + (int64_t)tb * n.L * ES), (short)0, rows * n.L * ES, 0x00020000);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t off = col < n.L ? (uint32_t)(((8 * g + i) * n.L + col) * ES) : OOB;
-      if constexpr (X8) {
-        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-        const u32x2 t = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, off, 0, 0));
-        st.x[i][0] = t[0];
-        st.x[i][1] = t[1];
-      } else {
-        const u32x4 t = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, off, 0, 0));
-#pragma unroll
-        for (int k = 0; k < 4; ++k) st.x[i][k] = t[k];
-      }
-    }
+    for (int i = 0; i < 8; ++i)
+      st.x[i] = __builtin_bit_cast(
+          u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, col < n.L ? (uint32_t)(((8 * g + i) * n.L + col) * ES) : OOB, 0, 0));
+  };
+  auto load_v = [&](int tb, StepV &st) {
+    const int rows = max(0, min(X8P_ROWS, n.t1 - tb));
     if constexpr (X8) {
       const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
           (void *)(n.scale + (int64_t)tb * n.ng), (short)0, rows * n.ng * 4, 0x00020000);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        st.s[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, ((8 * g + i) * n.ng + n.cb) * 4, 0, 0));
+      st.s = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, ((lane & 31) * n.ng + n.cb) * 4, 0, 0));
     }
-    for (int p = 0; p < n.vparts; ++p) {
-      const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(
-          (void *)(n.V + p * plane + (int64_t)tb * r), (short)0, rows * r * 4, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rv =
+        __builtin_amdgcn_make_buffer_rsrc((void *)(n.V + (int64_t)tb * r), (short)0, rows * r * 4, 0x00020000);
 #pragma unroll
-      for (int j = 0; j < JB; ++j) {
-        const int k = n.jg + 16 * j + c;
+    for (int k = 0; k < 2 * JB; ++k) {
+      if constexpr (FLAT) {
+        st.v[k] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, (k * 64 + lane) * 16, 0, 0));
+      } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t off = k < r ? (uint32_t)(((8 * g + i) * r + k) * 4) : OOB;
-          const float v = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rv, off, 0, 0));
-          st.v[j][i] = p == 0 ? v : st.v[j][i] + v;
+        for (int e = 0; e < 4; ++e) {
+          const int f = (4 * k + e) * 64 + lane, t = f / RB, j = n.jg + f % RB;
+          st.v[k][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rv, j < r ? (uint32_t)((t * r + j) * 4) : OOB, 0, 0));
         }
       }
     }
   };
-  f32x4 acc[8][JB];
+  // A step's V from the order of its loads to an operand's: ranks 16 j + c of tokens 8 g .. 8 g + 7, times
+  // their scales.  (A wave's own LDS: its accesses are in order.)
+  auto turned = [&](const StepV &st, float (&v)[JB][8]) {
+    if constexpr (FLAT) {
 #pragma unroll
-  for (int q = 0; q < 8; ++q)
+      for (int k = 0; k < 2 * JB; ++k) {
+        const int f = (k * 64 + lane) * 4, q = (f >= 8 * r) + (f >= 16 * r) + (f >= 24 * r);
+        *(f32x4 *)(turn + f + 16 * q) = st.v[k];  // (zeros behind the rows where r is less than the item's ranks)
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 2 * JB; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int f = (4 * k + e) * 64 + lane;
+          turn[f + 16 * (f / (8 * RB))] = st.v[k][e];
+        }
+    }
+    if (X8) turn_s[lane & 31] = st.s;
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = X8 ? turn_s[8 * g + i] : 1.0f;
+#pragma unroll
+    for (int j = 0; j < JB; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // (past the last rank whatever follows: it comes into sums of ranks that are not stored)
+        const float x = turn[(8 * g + i) * row + 16 * g + 16 * j + c];
+        v[j][i] = X8 ? x * s[i] : x;
+      }
+  };
+  f32x4 acc[Q][JB];
+#pragma unroll
+  for (int q = 0; q < Q; ++q)
 #pragma unroll
     for (int j = 0; j < JB; ++j) acc[q][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto compute = [&](const Step &st) {
-    u32x4 vb[JB][3], xt[8];
+  auto compute = [&](const StepX &sx, const StepV &sv) {
+    u32x4 vb[JB][3];
+    float vs[JB][8];
+    turned(sv, vs);
 #pragma unroll
     for (int j = 0; j < JB; ++j) {
-      float v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = X8 ? st.v[j][i] * st.s[i] : st.v[j][i];
+      float(&v)[8] = vs[j];
 #pragma unroll
       for (int p = 0; p < 3; ++p) {  // each the next bits of what is left
 #pragma unroll
@@ -249,146 +284,217 @@ __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, float 
         for (int i = 0; i < 8; ++i) v[i] -= h[i];
       }
     }
-    if constexpr (X8) {
-      // column q of the 8 tokens: byte q of each
+    // Four columns at a time: a product into a sum comes 4 JB products after the one before it.
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        float f[8];
+    for (int q0 = 0; q0 < Q; q0 += 4) {
+      u32x4 xt[4];  // columns of the 8 tokens
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = (float)(int8_t)(st.x[i][q >> 2] >> (8 * (q & 3)));
+      for (int q = 0; q < 4; ++q) {
+        if constexpr (X8) {
+          float f[8];
 #pragma unroll
-        for (int d = 0; d < 4; ++d) xt[q][d] = pack_bf16x2(f[2 * d], f[2 * d + 1]);
+          for (int i = 0; i < 8; ++i) f[i] = (float)(int8_t)(sx.x[i][q0 / 4] >> (8 * q));
+#pragma unroll
+          for (int d = 0; d < 4; ++d) xt[q][d] = pack_bf16x2(f[2 * d], f[2 * d + 1]);
+        } else {
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const uint32_t lo = sx.x[2 * d][q >> 1], hi = sx.x[2 * d + 1][q >> 1];
+            xt[q][d] = q & 1 ? (lo >> 16 | (hi & 0xffff0000u)) : ((lo & 0xffffu) | hi << 16);
+          }
+        }
       }
-    } else {
-      u32x4 x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = u32x4{st.x[i][0], st.x[i][1], st.x[i][2], st.x[i][3]};
-      transpose_block(BF16(), x, xt);
+      for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int j = 0; j < JB; ++j) mma16(BF16(), acc[q0 + q][j], xt[q], vb[j][p]);
     }
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-#pragma unroll
-      for (int j = 0; j < JB; ++j) {
-#pragma unroll
-        for (int p = 0; p < 3; ++p) mma16(BF16(), acc[q][j], xt[q], vb[j][p]);
-      }
   };
   {
-    Step cur, nxt;
+    // Three steps' registers in turn, by name: a copy of one would wait for its loads.
+    constexpr int STEP = X8P_NW * X8P_ROWS;
+    StepX x[3];
+    StepV v[3];
     int tb = n.t0 + wave * X8P_ROWS;
-    if (tb < n.t1) load(tb, cur);
-    for (; tb < n.t1; tb += X8P_NW * X8P_ROWS) {
-      load(min(tb + X8P_NW * X8P_ROWS, n.t1), nxt);  // (at the end: an empty resource)
-      compute(cur);
-      cur = nxt;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      load_x(min(tb + k * STEP, n.t1), x[k]);
+      load_v(min(tb + k * STEP, n.t1), v[k]);
+    }
+    for (; tb < n.t1; tb += 3 * STEP) {
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        load_x(min(tb + (k + 2) * STEP, n.t1), x[(k + 2) % 3]);  // (at the end: empty resources)
+        load_v(min(tb + (k + 2) * STEP, n.t1), v[(k + 2) % 3]);
+        if (tb + k * STEP < n.t1) compute(x[k], v[k]);
+      }
     }
   }
-  // acc[q][j] element i: column (4 g + i) 8 + q, rank 16 j + c
+  // acc[q][j] element i: column (4 g + i) Q + q, rank 16 j + c
 #pragma unroll
   for (int h = X8P_NW / 2; h >= 1; h /= 2) {
     __syncthreads();
     if (wave >= h && wave < 2 * h) {
 #pragma unroll
-      for (int q = 0; q < 8; ++q)
+      for (int q = 0; q < Q; ++q)
 #pragma unroll
         for (int j = 0; j < JB; ++j)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) red[wave - h][(4 * g + i) * 8 + q][16 * j + c] = acc[q][j][i];
+          for (int i = 0; i < 4; ++i) red[wave - h][(4 * g + i) * Q + q][16 * j + c] = acc[q][j][i];
     }
     __syncthreads();
     if (wave < h) {
 #pragma unroll
-      for (int q = 0; q < 8; ++q)
+      for (int q = 0; q < Q; ++q)
 #pragma unroll
         for (int j = 0; j < JB; ++j)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[q][j][i] += red[wave][(4 * g + i) * 8 + q][16 * j + c];
+          for (int i = 0; i < 4; ++i) acc[q][j][i] += red[wave][(4 * g + i) * Q + q][16 * j + c];
     }
   }
   // the tile to LDS, and from there out in whole rows
   __syncthreads();
   if (wave == 0) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
       for (int j = 0; j < JB; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) red[0][(4 * g + i) * 8 + q][16 * j + c] = n.mult * acc[q][j][i];
+        for (int i = 0; i < 4; ++i) red[0][(4 * g + i) * Q + q][16 * j + c] = n.mult * acc[q][j][i];
   }
   __syncthreads();
-  const int cols = min(ACT8_G, n.L - n.cb * ACT8_G), ranks = min(16 * JB, r - n.jg);
-  for (int i = threadIdx.x; i < ACT8_G * JB * 16; i += 64 * X8P_NW) {
-    if (n.transposed) {
-      const int k = i / ACT8_G, l = i % ACT8_G;
-      if (k < ranks && l < cols) n.out[(int64_t)(n.jg + k) * n.L + n.cb * ACT8_G + l] = red[0][l][k];
-    } else {
-      const int l = i / (JB * 16), k = i % (JB * 16);
-      if (k < ranks && l < cols) n.out[(int64_t)(n.cb * ACT8_G + l) * r + n.jg + k] = red[0][l][k];
+  const int cols = min(COLS, n.L - n.cb * COLS), ranks = min(RB, r - n.jg);
+  // place i of the tile: element (l, k) of it, in the order in which it lies in the output
+  auto place = [&](int i, int *l, int *k) {
+    *l = n.transposed ? i % COLS : i / RB;
+    *k = n.transposed ? i / COLS : i % RB;
+  };
+  if (parts > 1) {
+    // The parts of an item meet (meet.hpp): each leaves its tile in memory, and the one that comes last adds
+    // them in ascending order.  Tiles and flags are written and read at device scope.
+    float *slot = a.slots + (int64_t)item * parts * X8P_SLOT(JB);
+#pragma unroll
+    for (int i = threadIdx.x; i < TILE; i += NT) {
+      int l, k;
+      place(i, &l, &k);
+      __hip_atomic_store(slot + part * X8P_SLOT(JB) + i, red[0][l][k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    int *all = (int *)&red[1][0][0];
+    if (wave == 0) {
+      MeetFlags flags{a.sync + (int64_t)item * parts, lane};
+      const bool up = meet_arrive(flags, part, parts, a.gen);
+      if (up) meet_lower(flags, parts);
+      if (lane == 0) *all = up;
+    }
+    __syncthreads();
+    if (!*all) return;  // (two may see all: they store the same sums)
+#pragma unroll
+    for (int i = threadIdx.x; i < TILE; i += NT) {
+      float x = __hip_atomic_load(slot + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      for (int p = 1; p < parts; ++p) x += __hip_atomic_load(slot + p * X8P_SLOT(JB) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      int l, k;
+      place(i, &l, &k);
+      red[0][l][k] = x;  // (read by the same thread)
+    }
+  }
+#pragma unroll
+  for (int i = threadIdx.x; i < TILE; i += NT) {
+    int l, k;
+    place(i, &l, &k);
+    if (k < ranks && l < cols)
+      n.out[n.transposed ? (int64_t)(n.jg + k) * n.L + n.cb * COLS + l : (int64_t)(n.cb * COLS + l) * r + n.jg + k] = red[0][l][k];
   }
 }
 
-// Workgroups: the items of dB (twice the bytes an item), then those of dA, each in
-// `parts` ranges of tokens, which write to their own planes where there are several.
-template <int JB>
+// Workgroups: the items of dB, then those of dA, each in `parts` ranges of tokens.  FLAT: an item
+// has all r ranks, so that V's rows of a step are one run of memory, read in whole vectors.
+template <int JB, bool FLAT>
 __global__ __launch_bounds__(64 * X8P_NW) void x8_prod_kernel(X8Prod a, int parts, int chunk, int items_b) {
-  __shared__ float red[X8P_NW / 2][ACT8_G][JB * 16 + 1];
+  constexpr int RED = X8P_NW / 2 * ACT8_G * (JB * 16 + 1), TURN = X8P_NW * x8_turn(JB);
+  __shared__ __align__(16) float lds[RED > TURN ? RED : TURN];
   const int nz = (a.r + 16 * JB - 1) / (16 * JB);
-  const int unit = blockIdx.x, part = unit % parts;
-  int item = unit / parts;
+  const int unit = blockIdx.x, part = unit % parts, item = unit / parts;
   const bool dB = item < items_b;
-  if (!dB) item -= items_b;
-  const int64_t ra = (int64_t)a.r * a.K, rb = (int64_t)a.r * a.N;
-  float *const plane = parts > 1 ? a.planes + part * (ra + rb) : nullptr;
+  const int own = dB ? item : item - items_b;
   X8Unit n;
-  n.cb = item / nz;
-  n.jg = item % nz * 16 * JB;
+  n.cb = own / nz;
+  n.jg = own % nz * 16 * JB;
   n.t0 = part * chunk;
   n.t1 = min(a.T, n.t0 + chunk);
   n.X = dB ? a.dy : (const void *)a.x.codes;
   n.scale = a.x.scale;
   n.V = dB ? a.u : a.du;
-  n.vparts = dB ? a.u_parts : a.du_parts;
   n.L = dB ? a.N : a.K;
   n.ng = (a.K + ACT8_G - 1) / ACT8_G;
   n.mult = dB ? a.scale : 1.0f;
   n.transposed = !dB;
-  n.out = dB ? (plane ? plane + ra : a.dB) : (plane ? plane : a.dA);
-  if (dB) x8_item<JB, false>(a, n, red);
-  else x8_item<JB, true>(a, n, red);
+  n.out = dB ? a.dB : a.dA;
+  if (dB) x8_item<JB, FLAT, false>(a, n, item, part, parts, lds);
+  else x8_item<JB, FLAT, true>(a, n, item, part, parts, lds);
 }
 
-// dA and dB as the sums of the planes, in ascending order.
-__global__ __launch_bounds__(256) void x8_sum_kernel(const float *planes, int np, int64_t na, int64_t n, float *dA, float *dB) {
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;  // (na and n are multiples of 8)
-  if (i >= n) return;
-  f32x4 s = *(const f32x4 *)(planes + i);
-  for (int p = 1; p < np; ++p) s += *(const f32x4 *)(planes + p * n + i);
-  *(f32x4 *)(i < na ? dA + i : dB + (i - na)) = s;
+// du and u as one sum each, in place, of the partial sums that they came in: ascending, so the product
+// kernel's loads stay free of sums, which would wait for them.
+__global__ __launch_bounds__(256) void x8_join_kernel(float *du, int du_parts, float *u, int u_parts, int64_t n) {
+  float *const x = blockIdx.y == 0 ? du : u;
+  const int parts = blockIdx.y == 0 ? du_parts : u_parts;
+  if (parts == 1) return;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    float s = x[i];
+    for (int p = 1; p < parts; ++p) s += x[p * n + i];
+    x[i] = s;
+  }
 }
 
-static int64_t x8_items(int64_t L, int64_t r) { return (L + ACT8_G - 1) / ACT8_G * ((r + (r <= 16 ? 15 : 31)) / (r <= 16 ? 16 : 32)); }
+static int x8_jb(int64_t r) { return r <= 16 ? 1 : 2; }
+static int64_t x8_items(int64_t L, int64_t cols, int64_t r) {
+  return (L + cols - 1) / cols * ((r + 16 * x8_jb(r) - 1) / (16 * x8_jb(r)));
+}
 
+// Ranges of tokens: those that take the least time, in units of a step of a workgroup's waves (256
+// tokens).  A workgroup has a CU for itself, and spends about as much as X8_FIXED steps on
+// its first loads, the sums of its waves and the stores, X8_MEET more on a meeting.
+constexpr int X8_FIXED = 4, X8_MEET = 2;
 X8Plan x8_plan(int64_t T, int64_t K, int64_t N, int64_t r) {
   constexpr int64_t STEP = X8P_NW * X8P_ROWS;
-  const int64_t items = x8_items(K, r) + x8_items(N, r);
-  // two workgroups a CU, each of a step of every wave at least
-  const int64_t p = std::max<int64_t>(1, std::min<int64_t>({16, 512 / items, T / STEP}));
-  const int64_t chunk = ((T + p - 1) / p + STEP - 1) / STEP * STEP;
-  const int64_t parts = (T + chunk - 1) / chunk;
-  return {(int)parts, (int)chunk, parts > 1 ? (size_t)(parts * r * (K + N) * 4) : 0};
+  const int64_t items = x8_items(K, ACT8_G, r) + x8_items(N, ACT8_G / 2, r), steps = (T + STEP - 1) / STEP;
+  int64_t best = 0, parts = 1, per = steps;
+  for (int64_t p = 1; p <= std::min<int64_t>(steps, 16); ++p) {
+    const int64_t n = (steps + p - 1) / p;  // steps of a range
+    if ((steps + n - 1) / n != p) continue;
+    const int64_t t = (items * p + 255) / 256 * (n + X8_FIXED + (p > 1 ? X8_MEET : 0));
+    if (p == 1 || t < best) best = t, parts = p, per = n;
+  }
+  X8Plan q{(int)parts, (int)(per * STEP), 0, 0};
+  if (parts > 1) {
+    q.sync_bytes = (size_t)(items * parts) * sizeof(meet_word);
+    q.slot_bytes = (size_t)(items * parts) * X8P_SLOT(x8_jb(r)) * 4;
+  }
+  return q;
 }
 
 hipError_t launch_x8_prod(const X8Prod &a, hipStream_t st) {
   const X8Plan p = x8_plan(a.T, a.K, a.N, a.r);
-  const int items_b = (int)x8_items(a.N, a.r), items = items_b + (int)x8_items(a.K, a.r);
+  const int items_b = (int)x8_items(a.N, ACT8_G / 2, a.r), items = items_b + (int)x8_items(a.K, ACT8_G, a.r);
   const dim3 grid(items * p.parts), block(64 * X8P_NW);
-  if (a.r <= 16) hipLaunchKernelGGL((x8_prod_kernel<1>), grid, block, 0, st, a, p.parts, p.chunk, items_b);
-  else hipLaunchKernelGGL((x8_prod_kernel<2>), grid, block, 0, st, a, p.parts, p.chunk, items_b);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.parts == 1) return e;
-  const int64_t na = (int64_t)a.r * a.K, n = na + (int64_t)a.r * a.N;
-  hipLaunchKernelGGL(x8_sum_kernel, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, st, a.planes, p.parts, na, n, a.dA, a.dB);
+  if (p.parts > 64 || (p.parts > 1 && (!a.sync || !a.slots || a.gen == 0))) return hipErrorInvalidValue;
+  if (a.du_parts > 1 || a.u_parts > 1) {
+    const int64_t n = (int64_t)a.T * a.r;
+    const dim3 g((unsigned)std::min<int64_t>((n + 255) / 256, 1024), a.u_parts > 1 ? 2 : 1);
+    hipLaunchKernelGGL(x8_join_kernel, g, dim3(256), 0, st, a.du, a.du_parts, a.u_parts > 1 ? const_cast<float *>(a.u) : nullptr,
+                       a.u_parts, n);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+#define PROD(JB, FLAT) hipLaunchKernelGGL((x8_prod_kernel<JB, FLAT>), grid, block, 0, st, a, p.parts, p.chunk, items_b)
+  if (a.r <= 16) PROD(1, true);
+  else if (a.r <= 32) PROD(2, true);
+  else PROD(2, false);
+#undef PROD
   return hipGetLastError();
 }
 
