@@ -724,37 +724,57 @@ lora_status_t bwd_impl(const void *x, const void *W, const void *qc, const float
   return LORA_OK;
 }
 
-// The backward from an x in 8 bits (act8.hpp), with a bf16 or a quantized W: du by the
-// row-skinny kernel, the plain dx product with its LoRA step, then dA and dB in a
-// launch of their own (x8prod.hip) that reads x's codes and dy once at the memory's
-// rate; u, where it is not saved, from the codes.
+// The backward from an x in 8 bits (act8.hpp), with a bf16 or a quantized W: dx with its LoRA
+// step as in lora_linear_bwd, but for the dA / dB side items, and behind it dA and dB in a
+// launch of their own (x8prod.hip); u, where it is not saved, from the codes.  du comes from
+// the dx launch where that computes it -- the few-token kernel, or producers ahead of
+// the tiles -- and else from the row-skinny kernel.
 struct X8Layout {
-  size_t u, du, dutail, acat, sync, slots, total;
+  size_t fsync, sync, u, du, dutail, acat, slots, total;
+  size_t nsync, nslots;  // of the few-token kernel
   int ldt, u_parts;
+  bool few, fused;
+  NarrowPlan p;
   RowSplit sp;
 };
-X8Layout x8_layout(int64_t T, int64_t K, int64_t N, int64_t r) {
+X8Layout x8_layout(int64_t T, int64_t K, int64_t N, int64_t r, bool quant, bool dx) {
   X8Layout L{};
   if (r == 0) return L;
+  L.few = dx && !quant && few_rule(T, K, N, r, LORA_BF16).bwd;
+  L.fused = dx && !quant && !L.few && fuse_ok(T, K, N, r, LORA_BF16, true);
   L.u_parts = x8_down_parts(T, K);
-  L.sp = row_split(T, N, (int)r, DT_BF16);
+  L.sp = L.few || L.fused ? whole_rows(N, DT_BF16) : row_split(T, N, (int)r, DT_BF16);
   L.ldt = tail_ld(L.sp.nsplit * (int)r, DT_BF16);
   size_t off = 0;
+  const X8Plan x = x8_plan(T, K, N, r);
+  L.fsync = off;  // hand-over words of a fused launch
+  off += L.fused ? 256 : 0;
+  L.sync = off;  // the flags of the meetings over ranges of tokens
+  off += round256(x.sync_bytes);
   L.u = off;  // partial sums of u (when it is recomputed)
   off += round256((size_t)L.u_parts * T * r * 4);
-  L.du = off;  // partial sums of du = s dy B
+  L.du = off;  // partial sums of du = s dy B (few tokens: dy B)
   off += round256((size_t)L.sp.nsplit * T * r * 4);
   L.dutail = off;  // [T][ldt]: E(partial p of du) in columns p*r ..
-  off += round256((size_t)T * L.ldt * 2);
+  off += L.few ? 0 : round256((size_t)T * L.ldt * 2);
   L.acat = off;  // [nsplit * r][K]: A repeated once per partial
   off += L.sp.nsplit > 1 ? round256((size_t)L.sp.nsplit * r * K * 2) : 0;
-  const X8Plan p = x8_plan(T, K, N, r);
-  L.sync = off;  // the flags of the meetings over ranges of tokens
-  off += round256(p.sync_bytes);
   L.slots = off;  // dA's and dB's tiles of each range
-  off += round256(p.slot_bytes);
+  off += round256(x.slot_bytes);
+  if (L.few) {
+    L.p = narrow_plan(T, K, N, r);
+    L.nsync = off;
+    off += L.p.parts > 1 ? round256((size_t)L.p.flags * sizeof(meet_word)) : 0;
+    L.nslots = off;
+    off += round256(L.p.slot_bytes);
+  }
   L.total = off;
   return L;
+}
+// What serves any call of these sizes: with and without dx, either weight.
+size_t x8_bytes(int64_t T, int64_t K, int64_t N, int64_t r) {
+  return std::max({x8_layout(T, K, N, r, false, true).total, x8_layout(T, K, N, r, false, false).total,
+                   x8_layout(T, K, N, r, true, true).total});
 }
 
 lora_status_t bwd_x8_impl(const int8_t *xc, const float *xs, const void *W, const void *qc, const float *qs, const float *qo,
@@ -780,12 +800,13 @@ lora_status_t bwd_x8_impl(const int8_t *xc, const float *xs, const void *W, cons
   const void *ptrs[] = {xc, xs, W, A, B, u_saved, dy, dx, dA, dB};
   for (const void *p : ptrs)
     if (p && !aligned16(p)) return fail(LORA_EINVAL, "pointers must be 16-byte aligned");
-  const X8Layout L = x8_layout(T, d_in, d_out, r);
-  if ((s = check_ws(ws, ws_bytes, L.total)) != LORA_OK) return s;
+  const X8Layout L = x8_layout(T, d_in, d_out, r, qc != nullptr, dx != nullptr);
+  const size_t need = x8_bytes(T, d_in, d_out, r);
+  if ((s = check_ws(ws, ws_bytes, need)) != LORA_OK) return s;
   for (const Range &a : {rng(dy, T * d_out * 2), rng(xc, T * d_in), rng(xs, T * act8_groups(d_in) * 4), rng(A, r * d_in * 2),
                          rng(B, d_out * r * 2), rng(u_saved, T * r * 4)})
     ins.push_back(a);
-  if (any_overlap({rng(dx, T * d_in * 2), rng(dA, r * d_in * 4), rng(dB, d_out * r * 4), rng(ws, (int64_t)L.total)}, ins))
+  if (any_overlap({rng(dx, T * d_in * 2), rng(dA, r * d_in * 4), rng(dB, d_out * r * 4), rng(ws, (int64_t)need)}, ins))
     return fail(LORA_EINVAL, "an output overlaps an input or another output");
 
   hipStream_t st = (hipStream_t)hip_stream;
@@ -803,37 +824,58 @@ lora_status_t bwd_x8_impl(const int8_t *xc, const float *xs, const void *W, cons
     if (e != hipSuccess) return hip_fail(e, "x8_down launch");
   }
   const int ns = L.sp.nsplit;
-  pr.du = (float *)(wsb + L.du); pr.du_parts = ns;
-  {
-    RowArgs ra{};
-    ra.X = dy; ra.ldx = d_out; ra.M = (int)T; ra.L = (int)d_out;
-    ra.V = B; ra.ldv = r; ra.vmode = V_KMAJ_TR; ra.r = (int)r;
-    ra.nsplit = ns; ra.seg = L.sp.seg; ra.mb = L.sp.mb;
-    ra.out_mult = scale; ra.out = (float *)(wsb + L.du); ra.out_stride = T * r;
-    if (dx) {
-      ra.tail = wsb + L.dutail; ra.ldt = L.ldt; ra.tail_mult = scale;
-      if (ns > 1) {  // A repeated once per partial of du
-        ra.bcopy_mode = BCOPY_FLAT; ra.bcopy_src = A; ra.bcopy_dst = wsb + L.acat;
-        ra.bcopy_period = r * d_in; ra.bcopy_elems = ns * r * d_in;
-      }
+  pr.du = (float *)(wsb + L.du); pr.du_parts = ns; pr.du_scale = 1.0f;
+  RowArgs ra{};  // du = s dy B
+  ra.X = dy; ra.ldx = d_out; ra.M = (int)T; ra.L = (int)d_out;
+  ra.V = B; ra.ldv = r; ra.vmode = V_KMAJ_TR; ra.r = (int)r;
+  ra.nsplit = ns; ra.seg = L.sp.seg; ra.mb = L.sp.mb;
+  ra.out_mult = scale; ra.out = pr.du; ra.out_stride = T * r;
+  if (dx) {
+    ra.tail = wsb + L.dutail; ra.ldt = L.ldt; ra.tail_mult = scale;
+    if (ns > 1) {  // A repeated once per partial of du
+      ra.bcopy_mode = BCOPY_FLAT; ra.bcopy_src = A; ra.bcopy_dst = wsb + L.acat;
+      ra.bcopy_period = r * d_in; ra.bcopy_elems = ns * r * d_in;
     }
+  }
+  if (!L.few && !L.fused) {
     Timed t(K_LORA_DY_B, st);
     e = launch_row_skinny(ra, DT_BF16, st);
     t.done();
     if (e != hipSuccess) return hip_fail(e, "lora_dy_b launch");
   }
   if (dx) {
-    GemmArgs g{};
-    g.A = dy; g.lda = d_out;
-    g.B = W; g.ldb = d_in;
-    g.M = (int)T; g.N = (int)d_in; g.K = (int)d_out;
-    g.C = dx; g.ldc = d_in;
-    g.A2 = wsb + L.dutail; g.lda2 = L.ldt;
-    g.B2 = ns > 1 ? (const void *)(wsb + L.acat) : A; g.ldb2 = d_in;
-    g.r = (int)(ns * r);
-    set_qweight(g, qc ? &qw : nullptr);
     Timed t(qc ? K_GEMM_BWD_DX_Q : K_GEMM_BWD_DX, st);
-    e = run_gemm(g, DT_BF16, qc ? &qw : nullptr, true, nullptr, st);
+    if (L.few) {
+      NarrowArgs a{};
+      a.X = dy; a.W = W; a.V = B; a.P = A; a.out = dx; a.u_out = pr.du;
+      a.T = (int)T; a.N = (int)d_in; a.K = (int)d_out; a.r = (int)r; a.scale = scale;
+      a.sync = (meet_word *)(wsb + L.nsync);
+      a.slots = (float *)(wsb + L.nslots);
+      a.gen = next_tag();
+      pr.du_scale = scale;
+      e = launch_narrow_dx(a, L.p, st);
+    } else {
+      GemmArgs g{};
+      g.A = dy; g.lda = d_out;
+      g.B = W; g.ldb = d_in;
+      g.M = (int)T; g.N = (int)d_in; g.K = (int)d_out;
+      g.C = dx; g.ldc = d_in;
+      g.A2 = wsb + L.dutail; g.lda2 = L.ldt;
+      g.B2 = ns > 1 ? (const void *)(wsb + L.acat) : A; g.ldb2 = d_in;
+      g.r = (int)(ns * r);
+      set_qweight(g, qc ? &qw : nullptr);
+      if (L.fused) {
+        FuseArgs fz{};
+        fz.row = ra;
+        fz.nprod = (int)((T + 15) / 16);
+        fz.sync = (unsigned long long *)(wsb + L.fsync);
+        fz.gen = next_gen();
+        handover_params(fz);
+        e = launch_gemm_fused(g, &fz, nullptr, st);
+      } else {
+        e = run_gemm(g, DT_BF16, qc ? &qw : nullptr, true, nullptr, st);
+      }
+    }
     t.done();
     if (e != hipSuccess) return hip_fail(e, "gemm_bwd_dx launch");
   }
@@ -960,7 +1002,7 @@ lora_status_t lora_linear_bwd_q(const void *x, const void *W_codes, const float 
 size_t lora_linear_x8_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, int64_t r) {
   if (check_shapes(T, d_in, d_out, r, LORA_BF16) != LORA_OK) return (size_t)-1;
   if (r == 0) return lora_linear_workspace_bytes(LORA_OP_BWD, T, d_in, d_out, 0, LORA_BF16);
-  return x8_layout(T, d_in, d_out, r).total;
+  return x8_bytes(T, d_in, d_out, r);
 }
 
 lora_status_t lora_linear_bwd_x8(const int8_t *x_codes, const float *x_scale, const void *W, const void *A, const void *B,

@@ -359,6 +359,8 @@ NarrowPlan narrow_plan(int64_t T, int64_t N, int64_t K, int64_t r);
 // Workspace that lora_linear_bwd cannot do without (the tiled kernels').
 size_t bwd_least_workspace(int64_t T, int64_t d_in, int64_t d_out, int64_t r, bool bf16);
 hipError_t launch_narrow(NarrowArgs a, const NarrowPlan &p, bool k_major, hipStream_t st);
+// The backward's dx alone (out), with dy B [T][r] in u_out.
+hipError_t launch_narrow_dx(NarrowArgs a, const NarrowPlan &p, hipStream_t st);
 // u[i] = sum of planes[p * n + i] over p < parts, ascending; u may be planes.
 hipError_t launch_narrow_sum(const float *planes, int parts, int n, float *u, hipStream_t st);
 
@@ -515,7 +517,7 @@ struct X8Down {
 };
 int x8_down_parts(int64_t T, int64_t K);
 hipError_t launch_x8_down(const X8Down &a, hipStream_t st);
-// dA [r][K] = du^T x and dB [N][r] = scale dy^T u, with du and u as the sums of
+// dA [r][K] = du_scale du^T x and dB [N][r] = scale dy^T u, with du and u as the sums of
 // du_parts and u_parts planes [T][r] fp32, added in ascending order and left in the first (a u in
 // one part is only read).  sync and slots: where the tokens go in ranges, X8Plan's bytes for
 // the meetings of an item's ranges and their sums.
@@ -526,7 +528,7 @@ struct X8Prod {
   const float *u;
   int du_parts, u_parts;
   float *dA, *dB;
-  float scale;
+  float scale, du_scale;
   int T, K, N, r;
   meet_word *sync, gen;  // (gen: this launch's tag, never 0)
   float *slots;

@@ -58,7 +58,10 @@ __device__ __forceinline__ f32x4 nw_load(__amdgpu_buffer_rsrc_t rs, int off) {
 // waves) load less in all but spread over fewer CUs and end later at every
 // size tried: 64 tokens of 3072 -> 3072, fwd + bwd, 34 against 37 - 45 us.
 constexpr int NW_BM = 32, NW_BN = 64;
-template <int RB, int NBUF, bool KMAJ>
+//
+// GRADS = false (backward): without dA and dB, whose place another kernel takes, and with the
+// rank-r product dy B in u_out.
+template <int RB, int NBUF, bool KMAJ, bool GRADS = true>
 __global__ __launch_bounds__(256) void narrow_kernel(NarrowArgs a) {
   constexpr int BM = NW_BM, BN = NW_BN, NWV = 4, NT = 64 * NWV;
   constexpr int FN = BN / 32;  // blocks of 32 columns; one of 32 rows
@@ -83,7 +86,7 @@ __global__ __launch_bounds__(256) void narrow_kernel(NarrowArgs a) {
   // tile and part, which read the same W, follow one another on one XCD.
   const int units = a.tiles_n * a.parts, unit_wgs = (units + 7) / 8 * 8 * a.tiles_m;
   const int r = a.r, lrow = lane & 31, half = lane >> 5;
-  if constexpr (KMAJ && RB > 0) {
+  if constexpr (KMAJ && RB > 0 && GRADS) {
     if ((int)blockIdx.x >= unit_wgs) {
       // dB = s dy^T u: each wave 32 columns of dy by the r rank indices, the
       // reduction over all tokens on matrix cores, u rounded to bf16.  Every
@@ -337,7 +340,7 @@ __global__ __launch_bounds__(256) void narrow_kernel(NarrowArgs a) {
   EndX ex;
   if constexpr (RB > 0) {
     if (a.out && wv < FN) load_p(ep);
-    if constexpr (KMAJ) if (wv < DB) load_x(ex);
+    if constexpr (KMAJ && GRADS) if (wv < DB) load_x(ex);
   }
 
   // ---- sum of the four k-slices -----------------------------------------------------
@@ -455,7 +458,7 @@ __global__ __launch_bounds__(256) void narrow_kernel(NarrowArgs a) {
   }
 
   // ---- dA of this tile's rows and columns; the row tiles meet ------------------------
-  if constexpr (KMAJ && RB > 0) {
+  if constexpr (KMAJ && RB > 0 && GRADS) {
     const __amdgpu_buffer_rsrc_t rsD =
         nw_rsrc(a.da_slots + (int64_t)nt * a.tiles_m * (RB * 32 * BN), (int64_t)a.tiles_m * RB * 32 * BN * 4);
     if (wv < DB) {
@@ -559,6 +562,25 @@ static hipError_t narrow_dispatch(const NarrowArgs &a, int rank_blocks, int grid
     case 0: hipLaunchKernelGGL((narrow_kernel<0, 5, KMAJ>), dim3(grid), dim3(256), 0, st, a); break;
     case 1: hipLaunchKernelGGL((narrow_kernel<1, 4, KMAJ>), dim3(grid), dim3(256), 0, st, a); break;
     case 2: hipLaunchKernelGGL((narrow_kernel<2, 4, KMAJ>), dim3(grid), dim3(256), 0, st, a); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_narrow_dx(NarrowArgs a, const NarrowPlan &p, hipStream_t st) {
+  if (!p.ok || a.T < 1 || a.T > NARROW_MAX_T || a.K < 1 || p.parts < 1 || p.parts > 64 || (p.parts > 1 && !(a.slots && a.sync)) ||
+      a.r < 1 || a.r % 4 || a.r > 32 * p.rank_blocks || (int64_t)p.parts * p.part_k < a.K ||
+      (int64_t)(p.parts - 1) * p.part_k >= a.K || p.part_k % NW_BKE || p.tiles_m * NW_BM < a.T ||
+      (int64_t)p.tiles_n * NW_BN < a.N || !a.out || !a.u_out)
+    return hipErrorInvalidValue;
+  a.tiles_m = p.tiles_m;
+  a.tiles_n = p.tiles_n;
+  a.parts = p.parts;
+  a.part_k = p.part_k;
+  const int grid = (p.tiles_n * p.parts + 7) / 8 * 8 * p.tiles_m;
+  switch (p.rank_blocks) {
+    case 1: hipLaunchKernelGGL((narrow_kernel<1, 4, true, false>), dim3(grid), dim3(256), 0, st, a); break;
+    case 2: hipLaunchKernelGGL((narrow_kernel<2, 4, true, false>), dim3(grid), dim3(256), 0, st, a); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();

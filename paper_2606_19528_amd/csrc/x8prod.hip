@@ -164,6 +164,7 @@ hipError_t launch_x8_down(const X8Down &a, hipStream_t st) {
 // product q takes column Q c + q of every c.  The waves' tiles are summed pairwise.
 // The loads' latency bounds it, so they are two steps ahead.
 constexpr int X8P_NW = 8, X8P_ROWS = 32;
+constexpr int X8_SC1 = 16;  // cache policy of the device scope
 
 struct X8Unit {
   const void *X;
@@ -171,24 +172,25 @@ struct X8Unit {
   float *out;
   int L, ng, t0, t1, cb, jg;
   float mult;
-  bool transposed;  // out [r][L], else [L][r]
 };
 
 // LDS floats in which a wave turns a step's V around: 32 tokens of up to 16 JB ranks, 16 floats
 // more after each 8 tokens (the four quarters of a wave then read different banks), and the scales.
-constexpr int X8P_SLOT(int jb) { return ACT8_G * 16 * jb; }  // floats of a tile in the workspace
 constexpr int x8_turn(int jb) { return X8P_ROWS * 16 * jb + 3 * 16 + X8P_ROWS; }
+// And those of its tile: 16 JB ranks of up to 128 columns, 4 floats behind each.
+constexpr int x8_tile(int jb) { return 16 * jb * (ACT8_G + 4); }
+constexpr int X8P_SLOT(int jb) { return ACT8_G * 16 * jb; }  // floats of an item's sums in the workspace
 
-template <int JB, bool FLAT, bool X8>
+enum { V_FLAT = 0, V_ROWS = 1, V_EACH = 2 };
+template <int JB, int VK, bool X8>
 __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, int item, int part, int parts, float *lds) {
   constexpr uint32_t OOB = 0x80000000u;
   constexpr int ES = X8 ? 1 : 2, Q = 8 / ES, COLS = 16 * Q, RB = 16 * JB, TILE = COLS * RB, NT = 64 * X8P_NW;
-  float(*red)[COLS][RB + 1] = (float(*)[COLS][RB + 1])lds;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float *const turn = lds + wave * x8_turn(JB), *const turn_s = turn + X8P_ROWS * RB + 48;
   const int col = n.cb * COLS + Q * c, r = a.r;
-  const int row = FLAT ? r : RB;  // of V in `turn`
+  const int row = VK == V_FLAT ? r : RB;  // of V in `turn`
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
   struct StepX {
     u32x2 x[8];
@@ -219,8 +221,11 @@ __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, int it
         __builtin_amdgcn_make_buffer_rsrc((void *)(n.V + (int64_t)tb * r), (short)0, rows * r * 4, 0x00020000);
 #pragma unroll
     for (int k = 0; k < 2 * JB; ++k) {
-      if constexpr (FLAT) {
+      if constexpr (VK == V_FLAT) {
         st.v[k] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, (k * 64 + lane) * 16, 0, 0));
+      } else if constexpr (VK == V_ROWS) {
+        const int f = (k * 64 + lane) * 4, t = f / RB, j = n.jg + f % RB;
+        st.v[k] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, j < r ? (uint32_t)((t * r + j) * 4) : OOB, 0, 0));
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -233,10 +238,10 @@ __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, int it
   // A step's V from the order of its loads to an operand's: ranks 16 j + c of tokens 8 g .. 8 g + 7, times
   // their scales.  (A wave's own LDS: its accesses are in order.)
   auto turned = [&](const StepV &st, float (&v)[JB][8]) {
-    if constexpr (FLAT) {
+    if constexpr (VK != V_EACH) {
 #pragma unroll
       for (int k = 0; k < 2 * JB; ++k) {
-        const int f = (k * 64 + lane) * 4, q = (f >= 8 * r) + (f >= 16 * r) + (f >= 24 * r);
+        const int f = (k * 64 + lane) * 4, q = (f >= 8 * row) + (f >= 16 * row) + (f >= 24 * row);
         *(f32x4 *)(turn + f + 16 * q) = st.v[k];  // (zeros behind the rows where r is less than the item's ranks)
       }
     } else {
@@ -332,58 +337,51 @@ __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, int it
       }
     }
   }
-  // acc[q][j] element i: column (4 g + i) Q + q, rank 16 j + c
-#pragma unroll
-  for (int h = X8P_NW / 2; h >= 1; h /= 2) {
-    __syncthreads();
-    if (wave >= h && wave < 2 * h) {
-#pragma unroll
-      for (int q = 0; q < Q; ++q)
-#pragma unroll
-        for (int j = 0; j < JB; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) red[wave - h][(4 * g + i) * Q + q][16 * j + c] = acc[q][j][i];
-    }
-    __syncthreads();
-    if (wave < h) {
-#pragma unroll
-      for (int q = 0; q < Q; ++q)
-#pragma unroll
-        for (int j = 0; j < JB; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[q][j][i] += red[wave][(4 * g + i) * Q + q][16 * j + c];
-    }
-  }
-  // the tile to LDS, and from there out in whole rows
+  // acc[q][j] element i: column (4 g + i) Q + q, rank 16 j + c.  The waves' tiles side by side in LDS,
+  // columns of a rank together, and every thread the sums of some of its places: four columns of a
+  // rank, in the order of the output, dA [rank][column], dB [column][rank].  (A pairwise
+  // tree had seven barriers in the place of two.)
   __syncthreads();
-  if (wave == 0) {
+  float *const tile = lds + wave * x8_tile(JB);
+  constexpr int LD = COLS + 4;
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
+  for (int j = 0; j < JB; ++j)
 #pragma unroll
-      for (int j = 0; j < JB; ++j)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) red[0][(4 * g + i) * Q + q][16 * j + c] = n.mult * acc[q][j][i];
-  }
+      for (int q = 0; q < Q; q += 4)
+        *(f32x4 *)(tile + (16 * j + c) * LD + (4 * g + i) * Q + q) =
+            f32x4{acc[q][j][i], acc[q + 1][j][i], acc[q + 2][j][i], acc[q + 3][j][i]};
   __syncthreads();
-  const int cols = min(COLS, n.L - n.cb * COLS), ranks = min(RB, r - n.jg);
-  // place i of the tile: element (l, k) of it, in the order in which it lies in the output
-  auto place = [&](int i, int *l, int *k) {
-    *l = n.transposed ? i % COLS : i / RB;
-    *k = n.transposed ? i / COLS : i % RB;
+  constexpr int PER = (TILE / 4 + NT - 1) / NT;
+  static_assert(TILE / 4 % NT == 0 || TILE / 4 < NT, "whole rounds of threads");
+  const bool mine = (int)threadIdx.x < TILE / 4;
+  auto place = [&](int y, int *l, int *k) {
+    const int e = y * NT + (mine ? (int)threadIdx.x : 0);
+    *l = 4 * (X8 ? e % (COLS / 4) : e / RB);
+    *k = X8 ? e / (COLS / 4) : e % RB;
   };
-  if (parts > 1) {
-    // The parts of an item meet (meet.hpp): each leaves its tile in memory, and the one that comes last adds
-    // them in ascending order.  Tiles and flags are written and read at device scope.
-    float *slot = a.slots + (int64_t)item * parts * X8P_SLOT(JB);
+  f32x4 sum[PER];
 #pragma unroll
-    for (int i = threadIdx.x; i < TILE; i += NT) {
-      int l, k;
-      place(i, &l, &k);
-      __hip_atomic_store(slot + part * X8P_SLOT(JB) + i, red[0][l][k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+  for (int y = 0; y < PER; ++y) {
+    int l, k;
+    place(y, &l, &k);
+    sum[y] = *(const f32x4 *)(lds + k * LD + l);
+#pragma unroll
+    for (int w = 1; w < X8P_NW; ++w) sum[y] += *(const f32x4 *)(lds + w * x8_tile(JB) + k * LD + l);
+  }
+  if (parts > 1) {
+    // The parts of an item meet (meet.hpp): each leaves its sums in memory, and the one that comes last adds
+    // them in ascending order.  Sums and flags are written and read at device scope.
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        (void *)(a.slots + (int64_t)item * parts * X8P_SLOT(JB)), (short)0, parts * X8P_SLOT(JB) * 4, 0x00020000);
+    const uint32_t off = mine ? threadIdx.x * 16 : OOB;  // (threads without a place store and load nothing)
+#pragma unroll
+    for (int y = 0; y < PER; ++y)
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, sum[y]), rs, off + (part * X8P_SLOT(JB) + y * NT * 4) * 4, 0, X8_SC1);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    int *all = (int *)&red[1][0][0];
+    int *all = (int *)lds;
     if (wave == 0) {
       MeetFlags flags{a.sync + (int64_t)item * parts, lane};
       const bool up = meet_arrive(flags, part, parts, a.gen);
@@ -392,30 +390,43 @@ __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, int it
     }
     __syncthreads();
     if (!*all) return;  // (two may see all: they store the same sums)
+    for (int p = 0; p < parts; p += 4) {  // four parts' loads at once
+      f32x4 v[4][PER];
 #pragma unroll
-    for (int i = threadIdx.x; i < TILE; i += NT) {
-      float x = __hip_atomic_load(slot + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      for (int p = 1; p < parts; ++p) x += __hip_atomic_load(slot + p * X8P_SLOT(JB) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      int l, k;
-      place(i, &l, &k);
-      red[0][l][k] = x;  // (read by the same thread)
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int y = 0; y < PER; ++y)
+          v[x][y] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                  rs, off + (min(p + x, parts - 1) * X8P_SLOT(JB) + y * NT * 4) * 4, 0, X8_SC1));
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int y = 0; y < PER; ++y)
+          if (p + x < parts) sum[y] = p + x == 0 ? v[x][y] : sum[y] + v[x][y];
     }
   }
+  if (!mine) return;
 #pragma unroll
-  for (int i = threadIdx.x; i < TILE; i += NT) {
+  for (int y = 0; y < PER; ++y) {
     int l, k;
-    place(i, &l, &k);
-    if (k < ranks && l < cols)
-      n.out[n.transposed ? (int64_t)(n.jg + k) * n.L + n.cb * COLS + l : (int64_t)(n.cb * COLS + l) * r + n.jg + k] = red[0][l][k];
+    place(y, &l, &k);
+    if (k >= r - n.jg || n.cb * COLS + l >= n.L) continue;  // (columns are in whole eights)
+    if constexpr (X8) {
+      *(f32x4 *)(n.out + (int64_t)(n.jg + k) * n.L + n.cb * COLS + l) = sum[y] * n.mult;
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) n.out[(int64_t)(n.cb * COLS + l + x) * r + n.jg + k] = sum[y][x] * n.mult;
+    }
   }
 }
 
-// Workgroups: the items of dB, then those of dA, each in `parts` ranges of tokens.  FLAT: an item
-// has all r ranks, so that V's rows of a step are one run of memory, read in whole vectors.
-template <int JB, bool FLAT>
+// Workgroups: the items of dB, then those of dA, each in `parts` ranges of tokens.  An item has all r
+// ranks (V_FLAT: V's rows of a step are one run of memory, read in whole vectors), or some
+// of them (V_ROWS: vectors of each row, r a multiple of 4; V_EACH: a value each).
+template <int JB, int VK>
 __global__ __launch_bounds__(64 * X8P_NW) void x8_prod_kernel(X8Prod a, int parts, int chunk, int items_b) {
-  constexpr int RED = X8P_NW / 2 * ACT8_G * (JB * 16 + 1), TURN = X8P_NW * x8_turn(JB);
-  __shared__ __align__(16) float lds[RED > TURN ? RED : TURN];
+  constexpr int TILES = X8P_NW * x8_tile(JB), TURN = X8P_NW * x8_turn(JB);
+  __shared__ __align__(16) float lds[TILES > TURN ? TILES : TURN];
   const int nz = (a.r + 16 * JB - 1) / (16 * JB);
   const int unit = blockIdx.x, part = unit % parts, item = unit / parts;
   const bool dB = item < items_b;
@@ -430,11 +441,10 @@ __global__ __launch_bounds__(64 * X8P_NW) void x8_prod_kernel(X8Prod a, int part
   n.V = dB ? a.u : a.du;
   n.L = dB ? a.N : a.K;
   n.ng = (a.K + ACT8_G - 1) / ACT8_G;
-  n.mult = dB ? a.scale : 1.0f;
-  n.transposed = !dB;
+  n.mult = dB ? a.scale : a.du_scale;
   n.out = dB ? a.dB : a.dA;
-  if (dB) x8_item<JB, FLAT, false>(a, n, item, part, parts, lds);
-  else x8_item<JB, FLAT, true>(a, n, item, part, parts, lds);
+  if (dB) x8_item<JB, VK, false>(a, n, item, part, parts, lds);
+  else x8_item<JB, VK, true>(a, n, item, part, parts, lds);
 }
 
 // du and u as one sum each, in place, of the partial sums that they came in: ascending, so the product
@@ -490,10 +500,11 @@ hipError_t launch_x8_prod(const X8Prod &a, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-#define PROD(JB, FLAT) hipLaunchKernelGGL((x8_prod_kernel<JB, FLAT>), grid, block, 0, st, a, p.parts, p.chunk, items_b)
-  if (a.r <= 16) PROD(1, true);
-  else if (a.r <= 32) PROD(2, true);
-  else PROD(2, false);
+#define PROD(JB, VK) hipLaunchKernelGGL((x8_prod_kernel<JB, VK>), grid, block, 0, st, a, p.parts, p.chunk, items_b)
+  if (a.r <= 16) PROD(1, V_FLAT);
+  else if (a.r <= 32) PROD(2, V_FLAT);
+  else if (a.r % 4 == 0) PROD(2, V_ROWS);
+  else PROD(2, V_EACH);
 #undef PROD
   return hipGetLastError();
 }

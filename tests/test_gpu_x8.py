@@ -54,7 +54,20 @@ def check(got, inp, xq, wide, u, s):
 # ranges; every tile of the dx product that a call may take
 SIZES = [(1, 8, 8, 1), (1, 256, 264, 8), (3, 136, 64, 4), (24, 1000, 128, 13), (33, 128, 1000, 16), (128, 256, 256, 8),
          (203, 520, 1032, 17), (257, 1024, 96, 32), (300, 376, 264, 33), (515, 264, 776, 48), (600, 640, 392, 64), (97, 264, 200, 100),
-         (129, 248, 152, 128), (1025, 768, 2048, 8), (2051, 1336, 264, 32), (4100, 256, 520, 24)]
+         (129, 248, 152, 128), (1025, 768, 2048, 8), (2051, 1336, 264, 32), (4100, 256, 520, 24),
+         (30, 264, 520, 64), (100, 2056, 2048, 32), (128, 2048, 2056, 12), (7, 1024, 4104, 8), (1040, 1032, 1032, 16)]
+
+
+def test_the_sizes_reach_every_way_to_dx():
+    """The few-token kernel with one and two blocks of ranks and with parts, producers beside the tiles, and the
+    row-skinny kernel with one sum and with several."""
+    few = [lm.lora_few_token_plan(*c) for c in SIZES]
+    taken = [p["bwd_taken"] for p in few]
+    fused = [lm.lora_linear_plan(*c)["bwd_fused"] and not t for c, t in zip(SIZES, taken)]
+    assert any(t and c[3] > 32 for c, t in zip(SIZES, taken)) and any(t and p["bwd_parts"] > 1 for p, t in zip(few, taken))
+    assert any(t and c[0] > 64 for c, t in zip(SIZES, taken)) and any(fused)
+    du = [lm.lora_linear_plan(*c)["bwd_du_parts"] for c, t, f in zip(SIZES, taken, fused) if not t and not f]
+    assert 1 in du and max(du) > 1
 
 
 @pytest.mark.parametrize("T,K,N,r", SIZES)
