@@ -26,134 +26,136 @@ __device__ __forceinline__ u32x4 x8_operand(uint2 q) {
 }
 
 // ---- u = x A^T -----------------------------------------------------------------------
-// A workgroup of 8 waves takes 16 MB tokens and a range of groups; each wave every
-// eighth group, all ranks.  Lane (row or rank l % 16, quarter l / 16) holds 32
-// consecutive columns of a group: the four products of a group take them 8 at a
-// time, in the same order on both sides.
+// A workgroup of 8 waves takes 16 tokens, 16 JB ranks and a range of groups; each wave every
+// eighth group.  The wave loads a group of x and of A in whole lines, a step ahead, in
+// the one of two register sets that the step does not use, and turns it into operands (row or rank
+// l % 16, 8 columns l / 16 on) through LDS of its own.  Loads go through buffer resources:
+// tokens, columns and ranks past the end read zeros.
+// What bounds it is how many lines its loads touch: loads in the operands' layout, 16 rows
+// an instruction and no two neighbouring lanes in one, took 8.4 us at 4096 x 3072 codes and r =
+// 16 (10.1 at r = 32) in the place of 6.3 (9.4).  32 tokens a workgroup, which read A half as often, and two
+// ranges took as long (6.3, 8.5) and left sums of u to be added, 2.5 more.
 constexpr int X8D_NW = 8;
 
-template <int JB, int MB>
+template <int JB>
 __global__ __launch_bounds__(64 * X8D_NW) void x8_down_kernel(X8Down a, int groups_per) {
-  __shared__ float red[X8D_NW / 2][16 * MB][JB * 16 + 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q4 = lane >> 4;
+  constexpr uint32_t OOB = 0x80000000u;
+  constexpr int LD = JB * 16 + 1, ROWS = 16, RB = 16 * JB, TX = ACT8_G + 16, TA = 2 * ACT8_G + 16;  // bytes of a row
+  constexpr int TURN = ROWS * TX + RB * TA + ROWS * 4;
+  static_assert(ROWS * LD * 4 <= TURN, "a wave's sums take its LDS over");
+  __shared__ __align__(16) char lds[X8D_NW][TURN];
+  const int lane = threadIdx.x & 63, c = lane & 15, q4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  char *const turn_x = lds[wave], *const turn_a = turn_x + ROWS * TX;
+  float *const turn_s = (float *)(turn_a + RB * TA);
   const int ng = (a.K + ACT8_G - 1) / ACT8_G;
   const int g1 = min(ng, ((int)blockIdx.y + 1) * groups_per);
-  const int t0 = blockIdx.x * 16 * MB;
-  f32x4 tot[MB][JB];
+  const int t0 = blockIdx.x * ROWS, rows = min(ROWS, a.T - t0), j0 = blockIdx.z * RB;
+  const __amdgpu_buffer_rsrc_t rx =
+      __builtin_amdgcn_make_buffer_rsrc((void *)(a.x.codes + (int64_t)t0 * a.K), (short)0, rows * a.K, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rs =
+      __builtin_amdgcn_make_buffer_rsrc((void *)(a.x.scale + (int64_t)t0 * ng), (short)0, rows * ng * 4, 0x00020000);
+  const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void *)a.A, (short)0, a.r * a.K * 2, 0x00020000);
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  struct Step {
+    u32x2 x[4];  // rows 4 i + q4, columns 8 c on
+    u32x4 w[4 * JB];
+    float s;
+  };
+  const bool scale_lane = lane < ROWS;
+  auto load = [&](int g, Step &st) {
+    const int col = g * ACT8_G + 8 * c;
+    const bool in = g < g1 && col < a.K;
 #pragma unroll
-  for (int m = 0; m < MB; ++m)
+    for (int i = 0; i < 4; ++i)
+      st.x[i] = __builtin_bit_cast(
+          u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, in ? (uint32_t)((4 * i + q4) * a.K + col) : OOB, 0, 0));
 #pragma unroll
-    for (int j = 0; j < JB; ++j) tot[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int g = blockIdx.y * groups_per + wave; g < g1; g += X8D_NW) {
-    const int col = g * ACT8_G + q4 * 32;
-    uint2 x[MB][4];
+    for (int i = 0; i < 4 * JB; ++i)
+      st.w[i] = __builtin_bit_cast(
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, in ? (uint32_t)(((j0 + 4 * i + q4) * a.K + col) * 2) : OOB, 0, 0));
+    st.s = __builtin_bit_cast(
+        float, __builtin_amdgcn_raw_buffer_load_b32(rs, g < g1 && scale_lane ? (uint32_t)((lane * ng + g) * 4) : OOB, 0, 0));
+  };
+  f32x4 tot[JB];
+#pragma unroll
+  for (int j = 0; j < JB; ++j) tot[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto compute = [&](const Step &st) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *(u32x2 *)(turn_x + (4 * i + q4) * TX + 8 * c) = st.x[i];
+#pragma unroll
+    for (int i = 0; i < 4 * JB; ++i) *(u32x4 *)(turn_a + (4 * i + q4) * TA + 16 * c) = st.w[i];
+    if (scale_lane) turn_s[lane] = st.s;
     u32x4 w[JB][4];
-    float s[MB][4];
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-      const int t = t0 + 16 * m + c;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        x[m][k] = make_uint2(0u, 0u);
-        if (t < a.T && col + 8 * k < a.K) x[m][k] = *(const uint2 *)(a.x.codes + (int64_t)t * a.K + col + 8 * k);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int ts = t0 + 16 * m + 4 * q4 + i;
-        s[m][i] = ts < a.T ? a.x.scale[(int64_t)ts * ng + g] : 0.0f;
-      }
-    }
 #pragma unroll
     for (int j = 0; j < JB; ++j)
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        w[j][k] = j * 16 + c < a.r && col + 8 * k < a.K
-                      ? ld16((const uint16_t *)a.A + (int64_t)(j * 16 + c) * a.K + col + 8 * k)
-                      : zero16();
+      for (int k = 0; k < 4; ++k) w[j][k] = *(const u32x4 *)(turn_a + (16 * j + c) * TA + 64 * k + 16 * q4);
+    u32x4 xb[4];
 #pragma unroll
-    for (int m = 0; m < MB; ++m) {
-      u32x4 xb[4];
+    for (int k = 0; k < 4; ++k) xb[k] = x8_operand(*(const uint2 *)(turn_x + c * TX + 32 * k + 8 * q4));
+    const f32x4 s = *(const f32x4 *)(turn_s + 4 * q4);
+    f32x4 acc[JB];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) xb[k] = x8_operand(x[m][k]);
+    for (int j = 0; j < JB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < JB; ++j) {
-        f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mma16(BF16(), acc, xb[k], w[j][k]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tot[m][j][i] = __builtin_fmaf(s[m][i], acc[i], tot[m][j][i]);
-      }
-    }
-  }
-  // the waves' sums, pairwise: element i of lane is token 4 q4 + i, rank 16 j + c
-#pragma unroll
-  for (int h = X8D_NW / 2; h >= 1; h /= 2) {
-    __syncthreads();
-    if (wave >= h && wave < 2 * h) {
-#pragma unroll
-      for (int m = 0; m < MB; ++m)
-#pragma unroll
-        for (int j = 0; j < JB; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) red[wave - h][16 * m + 4 * q4 + i][16 * j + c] = tot[m][j][i];
-    }
-    __syncthreads();
-    if (wave < h) {
-#pragma unroll
-      for (int m = 0; m < MB; ++m)
-#pragma unroll
-        for (int j = 0; j < JB; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) tot[m][j][i] += red[wave][16 * m + 4 * q4 + i][16 * j + c];
-    }
-  }
-  if (wave != 0) return;
-  float *u = a.u + (int64_t)blockIdx.y * a.T * a.r;
-#pragma unroll
-  for (int m = 0; m < MB; ++m)
+      for (int j = 0; j < JB; ++j) mma16(BF16(), acc[j], xb[k], w[j][k]);
 #pragma unroll
     for (int j = 0; j < JB; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = t0 + 16 * m + 4 * q4 + i, k = 16 * j + c;
-        if (t < a.T && k < a.r) u[(int64_t)t * a.r + k] = tot[m][j][i];
+      for (int i = 0; i < 4; ++i) tot[j][i] = __builtin_fmaf(s[i], acc[j][i], tot[j][i]);
+  };
+  {
+    Step st[2];
+    int g = blockIdx.y * groups_per + wave;
+    load(g, st[0]);
+    for (; g < g1; g += 2 * X8D_NW) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        load(g + (k + 1) * X8D_NW, st[k ^ 1]);
+        if (g + k * X8D_NW < g1) compute(st[k]);
       }
+    }
+  }
+  // the waves' sums, each in its LDS: element i of a lane is token 4 q4 + i, rank 16 j + c
+  float *const red = (float *)lds[wave];
+#pragma unroll
+  for (int j = 0; j < JB; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) red[(4 * q4 + i) * LD + 16 * j + c] = tot[j][i];
+  __syncthreads();
+  float *u = a.u + ((int64_t)blockIdx.y * a.T + t0) * a.r;
+  for (int e = threadIdx.x; e < ROWS * RB; e += 64 * X8D_NW) {
+    const int t = e / RB, k = e % RB;
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < X8D_NW; ++w) v += ((const float *)lds[w])[t * LD + k];
+    if (t < rows && j0 + k < a.r) u[(int64_t)t * a.r + j0 + k] = v;
+  }
 }
 
 struct X8DownSplit {
-  int mb, parts, groups;
+  int blocks, parts, groups;
 };
 static X8DownSplit x8_down_split(int64_t T, int64_t K) {
-  const int64_t ng = (K + ACT8_G - 1) / ACT8_G;
-  const int mb = T >= 1024 ? 2 : 1;
-  const int64_t blocks = (T + 16 * mb - 1) / (16 * mb);
+  const int64_t ng = (K + ACT8_G - 1) / ACT8_G, blocks = (T + 15) / 16;
   // as many ranges as give each CU a workgroup, each of a group a wave at least
   const int64_t p = std::max<int64_t>(1, std::min<int64_t>({4, 256 / blocks, ng / X8D_NW}));
   const int64_t groups = (ng + p - 1) / p;
-  return {mb, (int)((ng + groups - 1) / groups), (int)groups};
+  return {(int)blocks, (int)((ng + groups - 1) / groups), (int)groups};
 }
 int x8_down_parts(int64_t T, int64_t K) { return x8_down_split(T, K).parts; }
 
-template <int JB>
-static hipError_t x8_down_jb(const X8Down &a, hipStream_t st) {
-  const X8DownSplit s = x8_down_split(a.T, a.K);
-  const dim3 grid((a.T + 16 * s.mb - 1) / (16 * s.mb), s.parts), block(64 * X8D_NW);
-  if (s.mb == 1) hipLaunchKernelGGL((x8_down_kernel<JB, 1>), grid, block, 0, st, a, s.groups);
-  else hipLaunchKernelGGL((x8_down_kernel<JB, 2>), grid, block, 0, st, a, s.groups);
-  return hipGetLastError();
-}
 hipError_t launch_x8_down(const X8Down &a, hipStream_t st) {
-  switch ((a.r + 15) / 16) {
-    case 1: return x8_down_jb<1>(a, st);
-    case 2: return x8_down_jb<2>(a, st);
-    case 3:
-    case 4: return x8_down_jb<4>(a, st);
-    case 5:
-    case 6:
-    case 7:
-    case 8: return x8_down_jb<8>(a, st);
-  }
-  return hipErrorInvalidValue;
+  if (a.r < 1 || a.r > 128) return hipErrorInvalidValue;
+  const X8DownSplit s = x8_down_split(a.T, a.K);
+  const int jb = a.r <= 16 ? 1 : 2;
+  const dim3 grid(s.blocks, s.parts, (a.r + 16 * jb - 1) / (16 * jb)), block(64 * X8D_NW);
+  if (jb == 1) hipLaunchKernelGGL((x8_down_kernel<1>), grid, block, 0, st, a, s.groups);
+  else hipLaunchKernelGGL((x8_down_kernel<2>), grid, block, 0, st, a, s.groups);
+  return hipGetLastError();
 }
 
 // ---- dA = du^T x, dB = s dy^T u ------------------------------------------------------
@@ -449,13 +451,19 @@ __global__ __launch_bounds__(64 * X8P_NW) void x8_prod_kernel(X8Prod a, int part
 
 // du and u as one sum each, in place, of the partial sums that they came in: ascending, so the product
 // kernel's loads stay free of sums, which would wait for them.
+constexpr int X8_JOIN = 4;
 __global__ __launch_bounds__(256) void x8_join_kernel(float *du, int du_parts, float *u, int u_parts, int64_t n) {
   float *const x = blockIdx.y == 0 ? du : u;
   const int parts = blockIdx.y == 0 ? du_parts : u_parts;
   if (parts == 1) return;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    float s = x[i];
-    for (int p = 1; p < parts; ++p) s += x[p * n + i];
+    float v[X8_JOIN];  // all parts' loads at once
+#pragma unroll
+    for (int p = 0; p < X8_JOIN; ++p) v[p] = x[min(p, parts - 1) * n + i];
+    float s = v[0];
+#pragma unroll
+    for (int p = 1; p < X8_JOIN; ++p) s = p < parts ? s + v[p] : s;
+    for (int p = X8_JOIN; p < parts; ++p) s += x[p * n + i];
     x[i] = s;
   }
 }
