@@ -99,6 +99,13 @@ struct Raw8 {
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = ld16(p + k * E::VEC);
   }
+  // Past the caches: for what is read once, which else takes the place of what comes to be read.
+  template <class I>
+  __device__ __forceinline__ void load_once(const void *base, I i) {
+    const typename E::T *p = (const typename E::T *)base + i;
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = __builtin_nontemporal_load((const u32x4 *)(p + k * E::VEC));
+  }
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = zero16();

@@ -22,10 +22,13 @@ struct BnCols {
 template <int W>
 __device__ __forceinline__ int bn_sub() { return __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W)); }
 
-template <class E, int W, int NV>
+template <class E, bool ONCE = false, int W, int NV>
 __device__ __forceinline__ void bn_load(Raw8<E> (&r)[NV], const void *p, int64_t at, const BnCols<W, NV> &c) {
 #pragma unroll
-  for (int v = 0; v < NV; ++v) r[v].load((const typename E::T *)p + at, c.at(v));
+  for (int v = 0; v < NV; ++v) {
+    if constexpr (ONCE) r[v].load_once((const typename E::T *)p + at, c.at(v));
+    else r[v].load((const typename E::T *)p + at, c.at(v));
+  }
 }
 template <class E, int W, int NV>
 __device__ __forceinline__ void bn_floats(float (&x)[NV][8], Raw8<E> (&r)[NV], const BnCols<W, NV> &c) {

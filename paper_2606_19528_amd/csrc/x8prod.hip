@@ -5,8 +5,8 @@
 // cores takes them as they are; a scale belongs to a row and 128 columns of x and goes
 // to the other side of the product: in u to the group's sum, in dA to du.  du and u
 // are fp32 and stay so: v as the sum of three bf16, which hold its 24 bits.  (Two leave
-// 2^-18 of it, 2e-6 of the gradient's norm; one 2^-9.  The third product takes 1 us of
-// the 22 of 8192 -> 3072 at 4096 tokens.)
+// 2^-18 of it, 2e-6 of the gradient's norm; one 2^-9.  The third product is in the noise of the 29.5 us
+// of 8192 -> 3072 at 4096 tokens.)
 #include <algorithm>
 
 #include "act8.hpp"

@@ -777,6 +777,37 @@ def grad_clip(grads: GradList, max_norm: float, norm, stream=None):
 ACT8_GROUP = 128
 
 
+_names = None
+
+
+def _torch_names():
+    """torch and its types, looked up once: an import statement in each of a call's helpers takes
+    longer than the call's launch where the sizes are small."""
+    global _names
+    if _names is None:
+        import torch
+
+        _names = (torch, torch.bfloat16, torch.float32, torch.int8, {torch.bfloat16: LORA_BF16, torch.float32: LORA_F32},
+                  getattr(torch._C, "_cuda_getCurrentRawStream", None))
+    return _names
+
+
+def _stream_on(stream, dev: int):
+    """_stream, for a caller that knows the current device."""
+    if stream is None:
+        raw = _torch_names()[5]
+        if raw is not None:
+            return raw(dev)
+    return _stream(stream)
+
+
+def _code(dtype) -> int:
+    code = _torch_names()[4].get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype} (bf16 or fp32)")
+    return code
+
+
 def _dev_arg(t, name: str, dtype, shape, dev: int):
     """_arg of a tensor that has to be on device `dev`, the current one."""
     if t.dtype != dtype:
@@ -796,11 +827,10 @@ def _dev_opt(t, name: str, dtype, shape, dev: int):
 
 def _x8_args(x8, name: str, T: int, D: int, dev: int):
     """Addresses of (codes, scale) of an activation [T, D] in 8 bits."""
-    import torch
-
     codes, scale = x8
-    return (_dev_arg(codes, name + "'s codes", torch.int8, (T, D), dev),
-            _dev_arg(scale, name + "'s scale", torch.float32, (T, -(-D // ACT8_GROUP)), dev))
+    _, _, f32, i8, _, _ = _torch_names()
+    return (_dev_arg(codes, name + "'s codes", i8, (T, D), dev),
+            _dev_arg(scale, name + "'s scale", f32, (T, -(-D // ACT8_GROUP)), dev))
 
 
 def act8_empty(T: int, D: int, device="cuda"):
@@ -814,23 +844,23 @@ def act8_empty(T: int, D: int, device="cuda"):
 def act8_quantize(x, x8, stream=None):
     """x8 = (codes, scale) of x [T, D]: of each 128 columns of a row the largest magnitude over
     127, and the nearest multiples of it."""
-    import torch
-
-    (T, D), dev = x.shape, torch.cuda.current_device()
-    dt = _dtype_code(x)
-    st = lib().act8_quantize(_dev_arg(x, "x", x.dtype, (T, D), dev), *_x8_args(x8, "x8", T, D, dev), T, D, dt, _stream(stream))
-    _check(st, "act8_quantize")
+    shape, dt, dev = x.shape, x.dtype, _torch_names()[0].cuda.current_device()
+    T, D = shape
+    code = _code(dt)
+    st = lib().act8_quantize(_dev_arg(x, "x", dt, shape, dev), *_x8_args(x8, "x8", T, D, dev), T, D, code, _stream_on(stream, dev))
+    if st:
+        _check(st, "act8_quantize")
     return x8
 
 
 def act8_dequantize(x8, x, stream=None):
     """x [T, D] = scale times codes, rounded to x's type."""
-    import torch
-
-    (T, D), dev = x.shape, torch.cuda.current_device()
-    dt = _dtype_code(x)
-    st = lib().act8_dequantize(*_x8_args(x8, "x8", T, D, dev), _dev_arg(x, "x", x.dtype, (T, D), dev), T, D, dt, _stream(stream))
-    _check(st, "act8_dequantize")
+    shape, dt, dev = x.shape, x.dtype, _torch_names()[0].cuda.current_device()
+    T, D = shape
+    code = _code(dt)
+    st = lib().act8_dequantize(*_x8_args(x8, "x8", T, D, dev), _dev_arg(x, "x", dt, shape, dev), T, D, code, _stream_on(stream, dev))
+    if st:
+        _check(st, "act8_dequantize")
     return x
 
 
@@ -842,9 +872,7 @@ def lora_linear_x8_workspace_bytes(T: int, d_in: int, d_out: int, r: int) -> int
 
 
 def _bwd_x8_args(x8, A, B, u_saved, dy, dx, dA, dB, T, d_in, d_out, dev):
-    import torch
-
-    bf, f32 = torch.bfloat16, torch.float32
+    _, bf, f32, _, _, _ = _torch_names()
     r = 0 if A is None else A.shape[0]
     # (at rank 0 x, A and B do not enter)
     head = _x8_args(x8, "x8", T, d_in, dev) if r else (None, None)
@@ -856,13 +884,11 @@ def _bwd_x8_args(x8, A, B, u_saved, dy, dx, dA, dB, T, d_in, d_out, dev):
 
 def lora_linear_bwd_x8(x8, W, A, B, u_saved, dy, dx, dA, dB, scale: float = 1.0, ws=None, stream=None):
     """lora_linear_bwd from an x kept in 8 bits (act8_quantize); u_saved None recomputes u from it."""
-    import torch
-
-    (T, d_out), d_in, dev = dy.shape, W.shape[1], torch.cuda.current_device()
+    (T, d_out), d_in, dev = dy.shape, W.shape[1], _torch_names()[0].cuda.current_device()
     r, head, rest = _bwd_x8_args(x8, A, B, u_saved, dy, dx, dA, dB, T, d_in, d_out, dev)
     wp, wn, ws = _ws_for(ws, lambda: lora_linear_x8_workspace_bytes(T, d_in, d_out, r), dy, stream)
-    st = lib().lora_linear_bwd_x8(*head, _dev_arg(W, "W", torch.bfloat16, (d_out, d_in), dev), *rest, T, d_in, d_out, r, scale, wp,
-                                  wn, _stream(stream))
+    st = lib().lora_linear_bwd_x8(*head, _dev_arg(W, "W", _torch_names()[1], (d_out, d_in), dev), *rest, T, d_in, d_out, r, scale, wp,
+                                  wn, _stream_on(stream, dev))
     _check(st, "lora_linear_bwd_x8")
     return dx, dA, dB
 
@@ -878,7 +904,7 @@ def lora_linear_bwd_q_x8(x8, Wq, A, B, u_saved, dy, dx, dA, dB, scale: float = 1
               _dev_arg(sc, "scale", torch.float32, (sc.shape[0], d_out), dev),
               _dev_arg(off, "offset", torch.float32, (sc.shape[0], d_out), dev))
     wp, wn, ws = _ws_for(ws, lambda: lora_linear_x8_workspace_bytes(T, d_in, d_out, r), dy, stream)
-    st = lib().lora_linear_bwd_q_x8(*head, *weight, bits, group, *rest, T, d_in, d_out, r, scale, wp, wn, _stream(stream))
+    st = lib().lora_linear_bwd_q_x8(*head, *weight, bits, group, *rest, T, d_in, d_out, r, scale, wp, wn, _stream_on(stream, dev))
     _check(st, "lora_linear_bwd_q_x8")
     return dx, dA, dB
 
@@ -897,16 +923,11 @@ def _gate_mode(gate, T: int, D: int) -> int:
 
 
 def _block(T, D, dtype, res_dtype, post_norm, w_post, w_pre, gate, gain_offset, res_scale, dev):
-    import torch
-
-    code = {torch.bfloat16: LORA_BF16, torch.float32: LORA_F32}
-    if dtype not in code or res_dtype not in code:
-        raise TypeError(f"unsupported dtype {dtype} or {res_dtype} (bf16 or fp32)")
     if post_norm is None:
         post_norm = w_post is not None
     # (an element of D = 1 or T = 1 makes two of a gate's shapes alike: either names the same values)
     mode = _gate_mode(gate, T, D)
-    return _BlockNorm(T, D, code[dtype], code[res_dtype], 1 if post_norm else 0, mode, gain_offset, res_scale,
+    return _BlockNorm(T, D, _code(dtype), _code(res_dtype), 1 if post_norm else 0, mode, gain_offset, res_scale,
                       _dev_opt(w_post, "w_post", dtype, (D,), dev), _dev_opt(w_pre, "w_pre", dtype, (D,), dev),
                       None if gate is None else _dev_arg(gate, "gate", dtype, gate.shape, dev))
 
@@ -922,18 +943,18 @@ def block_norm_fwd(h, y=None, h_out=None, n=None, w_pre=None, w_post=None, gate=
     (`post_norm`, by default where w_post is given), its gate ([D], [T, 1] or [T, D]) and residual
     sum, and the norm before the next.  rstd_pre, rstd_post [T] are kept for the backward pass;
     y8, h8, n8 receive copies in 8 bits.  Without y the norm alone."""
-    import torch
-
-    (T, D), dev, f32 = h.shape, torch.cuda.current_device(), torch.float32
-    like = next((t for t in (y, n, w_pre) if t is not None), h)
-    dt, rt = like.dtype, h.dtype
+    shape, rt = h.shape, h.dtype
+    torch, _, f32, _, _, _ = _torch_names()
+    (T, D), dev = shape, torch.cuda.current_device()
+    dt = next((t for t in (y, n, w_pre) if t is not None), h).dtype
     b = _block(T, D, dt, rt, post_norm, w_post, w_pre, gate, gain_offset, res_scale, dev)
-    st = lib().block_norm_fwd(ctypes.byref(b), _dev_arg(h, "h", rt, (T, D), dev), _dev_opt(y, "y", dt, (T, D), dev),
-                              _dev_opt(h_out, "h_out", rt, (T, D), dev), _dev_opt(n, "n", dt, (T, D), dev),
+    st = lib().block_norm_fwd(ctypes.byref(b), _dev_arg(h, "h", rt, shape, dev), _dev_opt(y, "y", dt, shape, dev),
+                              _dev_opt(h_out, "h_out", rt, shape, dev), _dev_opt(n, "n", dt, shape, dev),
                               _dev_opt(rstd_post, "rstd_post", f32, (T,), dev), _dev_opt(rstd_pre, "rstd_pre", f32, (T,), dev),
                               _act8(y8, "y8", T, D, dev), _act8(h8, "h8", T, D, dev), _act8(n8, "n8", T, D, dev), eps,
-                              _stream(stream))
-    _check(st, "block_norm_fwd")
+                              _stream_on(stream, dev))
+    if st:
+        _check(st, "block_norm_fwd")
     return h_out, n
 
 
@@ -950,11 +971,10 @@ def block_norm_bwd(dn, dh_out, h, y=None, dh=None, dy=None, w_pre=None, w_post=N
     """Gradients of block_norm_fwd (see the header): dh of its h (may be dh_out) and, where given, dy,
     dw_pre, dw_post [D] fp32 and dgate.  h is the forward's h_out, y its y, each a
     tensor or a pair (codes, scale) in 8 bits."""
-    import torch
-
-    (T, D), dev, f32 = dh.shape, torch.cuda.current_device(), torch.float32
-    like = next((t for t in (dn, dy, w_pre, gate) if t is not None), dh)
-    dt, rt = like.dtype, dh.dtype
+    shape, rt = dh.shape, dh.dtype
+    torch, _, f32, _, _, _ = _torch_names()
+    (T, D), dev = shape, torch.cuda.current_device()
+    dt = next((t for t in (dn, dy, w_pre, gate) if t is not None), dh).dtype
     b = _block(T, D, dt, rt, post_norm, w_post, w_pre, gate, gain_offset, res_scale, dev)
     whole_h, whole_y = not isinstance(h, (tuple, list)), not isinstance(y, (tuple, list))
     wp, wn = None, 0
@@ -965,13 +985,13 @@ def block_norm_bwd(dn, dh_out, h, y=None, dh=None, dy=None, w_pre=None, w_post=N
         if gate is None:
             raise ValueError("dgate needs a gate")
         dgate_at = _dev_arg(dgate, "dgate", dt if b.gate_mode == BLOCK_GATE_FULL else f32, gate.shape, dev)
-    st = lib().block_norm_bwd(ctypes.byref(b), _dev_opt(dn, "dn", dt, (T, D), dev), _dev_opt(dh_out, "dh_out", rt, (T, D), dev),
-                              _dev_opt(h, "h", rt, (T, D), dev) if whole_h else None, None if whole_h else _act8(h, "h", T, D, dev),
-                              _dev_opt(y, "y", dt, (T, D), dev) if whole_y else None, None if whole_y else _act8(y, "y", T, D, dev),
+    st = lib().block_norm_bwd(ctypes.byref(b), _dev_opt(dn, "dn", dt, shape, dev), _dev_opt(dh_out, "dh_out", rt, shape, dev),
+                              _dev_opt(h, "h", rt, shape, dev) if whole_h else None, None if whole_h else _act8(h, "h", T, D, dev),
+                              _dev_opt(y, "y", dt, shape, dev) if whole_y else None, None if whole_y else _act8(y, "y", T, D, dev),
                               _dev_opt(rstd_post, "rstd_post", f32, (T,), dev), _dev_opt(rstd_pre, "rstd_pre", f32, (T,), dev),
-                              _dev_arg(dh, "dh", rt, (T, D), dev), _dev_opt(dy, "dy", dt, (T, D), dev),
+                              _dev_arg(dh, "dh", rt, shape, dev), _dev_opt(dy, "dy", dt, shape, dev),
                               _dev_opt(dw_pre, "dw_pre", f32, (D,), dev), _dev_opt(dw_post, "dw_post", f32, (D,), dev), dgate_at,
-                              wp, wn, _stream(stream))
+                              wp, wn, _stream_on(stream, dev))
     _check(st, "block_norm_bwd")
     return dh, dy
 
