@@ -63,19 +63,21 @@ __global__ __launch_bounds__(64 * X8D_NW) void x8_down_kernel(X8Down a, int grou
     float s;
   };
   const bool scale_lane = lane < ROWS;
+  // (offsets added to one choice: a choice for each load became a branch around it, with its own wait)
   auto load = [&](int g, Step &st) {
     const int col = g * ACT8_G + 8 * c;
-    const bool in = g < g1 && col < a.K;
+    const uint32_t at = g < g1 && col < a.K ? (uint32_t)col : OOB;
+    const uint32_t at_a = at == OOB ? OOB : 2 * at;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      st.x[i] = __builtin_bit_cast(
-          u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, in ? (uint32_t)((4 * i + q4) * a.K + col) : OOB, 0, 0));
+      st.x[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, at + (uint32_t)((4 * i + q4) * a.K), 0, 0));
 #pragma unroll
     for (int i = 0; i < 4 * JB; ++i)
       st.w[i] = __builtin_bit_cast(
-          u32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, in ? (uint32_t)(((j0 + 4 * i + q4) * a.K + col) * 2) : OOB, 0, 0));
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, at_a + (uint32_t)((j0 + 4 * i + q4) * a.K * 2), 0, 0));
     st.s = __builtin_bit_cast(
         float, __builtin_amdgcn_raw_buffer_load_b32(rs, g < g1 && scale_lane ? (uint32_t)((lane * ng + g) * 4) : OOB, 0, 0));
+    __builtin_amdgcn_sched_barrier(0);
   };
   f32x4 tot[JB];
 #pragma unroll
@@ -203,14 +205,16 @@ __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, int it
   };
   // Loads go through buffer resources based at the step's first token: tokens past the range,
   // columns past L and ranks past r read zeros.
+  uint32_t off_x[8];  // (added to one choice: a choice for each load became a branch around it)
+#pragma unroll
+  for (int i = 0; i < 8; ++i) off_x[i] = (col < n.L ? (uint32_t)(col * ES) : OOB) + (uint32_t)((8 * g + i) * n.L * ES);
   auto load_x = [&](int tb, StepX &st) {
     const int rows = max(0, min(X8P_ROWS, n.t1 - tb));
     const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(
         (void *)((const char *)n.X + (int64_t)tb * n.L * ES), (short)0, rows * n.L * ES, 0x00020000);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      st.x[i] = __builtin_bit_cast(
-          u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, col < n.L ? (uint32_t)(((8 * g + i) * n.L + col) * ES) : OOB, 0, 0));
+      st.x[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, off_x[i], 0, 0));
   };
   auto load_v = [&](int tb, StepV &st) {
     const int rows = max(0, min(X8P_ROWS, n.t1 - tb));
@@ -329,12 +333,14 @@ __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, int it
     for (int k = 0; k < 2; ++k) {
       load_x(min(tb + k * STEP, n.t1), x[k]);
       load_v(min(tb + k * STEP, n.t1), v[k]);
+      __builtin_amdgcn_sched_barrier(0);  // (a wait for one step's loads is none for the next one's)
     }
     for (; tb < n.t1; tb += 3 * STEP) {
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
         load_x(min(tb + (k + 2) * STEP, n.t1), x[(k + 2) % 3]);  // (at the end: empty resources)
         load_v(min(tb + (k + 2) * STEP, n.t1), v[(k + 2) % 3]);
+        __builtin_amdgcn_sched_barrier(0);
         if (tb + k * STEP < n.t1) compute(x[k], v[k]);
       }
     }
