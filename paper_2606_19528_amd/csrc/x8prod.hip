@@ -165,8 +165,12 @@ hipError_t launch_x8_down(const X8Down &a, hipStream_t st) {
 // either way, by 16 JB ranks, over a range of tokens.  Its waves take steps of 32 tokens in turn:
 // lane (c = l % 16, g = l / 16) loads Q = 8 (4) columns of tokens 8 g .. 8 g + 7, and the 8
 // tokens of one of its columns are an operand whose reduction axis is the token axis;
-// product q takes column Q c + q of every c.  The waves' tiles are summed pairwise.
-// The loads' latency bounds it, so they are two steps ahead.
+// product q takes column Q c + q of every c.  The waves' tiles are summed in LDS.
+// 8192 -> 3072 at 4096 tokens, r = 32: 28 us, of which 7 are the sums, the meeting and the stores, 11
+// a step's arithmetic and turns (V in three terms, turned for each 128 bytes of a row), and the rest
+// loads that these do not hide; the 59 MB alone would be 11.  Loads are a step ahead: two steps
+// ahead, and none left out at the end, took as long there and 6.3 us for 4.5 where a wave has a step or
+// two (256 tokens, 3072 -> 3072, r = 16).
 constexpr int X8P_NW = 8, X8P_ROWS = 32;
 constexpr int X8_SC1 = 16;  // cache policy of the device scope
 
@@ -177,6 +181,15 @@ struct X8Unit {
   int L, ng, t0, t1, cb, jg;
   float mult;
 };
+
+// A buffer resource of scalars (the compiler moves their sums to vector registers in a loop, and then
+// loads lane by lane).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t x8_resource(const void *p, int bytes) {
+  const uint64_t v = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc((void *)((uint64_t)hi << 32 | lo), (short)0, __builtin_amdgcn_readfirstlane(bytes),
+                                           0x00020000);
+}
 
 // LDS floats in which a wave turns a step's V around: 32 tokens of up to 16 JB ranks, 16 floats
 // more after each 8 tokens (the four quarters of a wave then read different banks), and the scales.
@@ -210,8 +223,7 @@ __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, int it
   for (int i = 0; i < 8; ++i) off_x[i] = (col < n.L ? (uint32_t)(col * ES) : OOB) + (uint32_t)((8 * g + i) * n.L * ES);
   auto load_x = [&](int tb, StepX &st) {
     const int rows = max(0, min(X8P_ROWS, n.t1 - tb));
-    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(
-        (void *)((const char *)n.X + (int64_t)tb * n.L * ES), (short)0, rows * n.L * ES, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rx = x8_resource((const char *)n.X + (int64_t)tb * n.L * ES, rows * n.L * ES);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       st.x[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, off_x[i], 0, 0));
@@ -219,12 +231,10 @@ __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, int it
   auto load_v = [&](int tb, StepV &st) {
     const int rows = max(0, min(X8P_ROWS, n.t1 - tb));
     if constexpr (X8) {
-      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-          (void *)(n.scale + (int64_t)tb * n.ng), (short)0, rows * n.ng * 4, 0x00020000);
+      const __amdgpu_buffer_rsrc_t rs = x8_resource(n.scale + (int64_t)tb * n.ng, rows * n.ng * 4);
       st.s = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, ((lane & 31) * n.ng + n.cb) * 4, 0, 0));
     }
-    const __amdgpu_buffer_rsrc_t rv =
-        __builtin_amdgcn_make_buffer_rsrc((void *)(n.V + (int64_t)tb * r), (short)0, rows * r * 4, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rv = x8_resource(n.V + (int64_t)tb * r, rows * r * 4);
 #pragma unroll
     for (int k = 0; k < 2 * JB; ++k) {
       if constexpr (VK == V_FLAT) {
@@ -324,25 +334,28 @@ __device__ __forceinline__ void x8_item(const X8Prod &a, const X8Unit &n, int it
     }
   };
   {
-    // Three steps' registers in turn, by name: a copy of one would wait for its loads.
+    // Two steps' registers in turn, by name: a copy of one would wait for its loads.
     constexpr int STEP = X8P_NW * X8P_ROWS;
-    StepX x[3];
-    StepV v[3];
+    StepX x[2];
+    StepV v[2];
     int tb = n.t0 + wave * X8P_ROWS;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      load_x(min(tb + k * STEP, n.t1), x[k]);
-      load_v(min(tb + k * STEP, n.t1), v[k]);
+    auto load = [&](int at, int k) {
+      load_x(at, x[k]);
+      load_v(at, v[k]);
       __builtin_amdgcn_sched_barrier(0);  // (a wait for one step's loads is none for the next one's)
+    };
+    load(min(tb, n.t1), 0);
+    for (; tb + 2 * STEP < n.t1; tb += 2 * STEP) {
+      load(tb + STEP, 1);
+      compute(x[0], v[0]);
+      load(tb + 2 * STEP, 0);
+      compute(x[1], v[1]);
     }
-    for (; tb < n.t1; tb += 3 * STEP) {
-#pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        load_x(min(tb + (k + 2) * STEP, n.t1), x[(k + 2) % 3]);  // (at the end: empty resources)
-        load_v(min(tb + (k + 2) * STEP, n.t1), v[(k + 2) % 3]);
-        __builtin_amdgcn_sched_barrier(0);
-        if (tb + k * STEP < n.t1) compute(x[k], v[k]);
-      }
+    if (tb < n.t1) {
+      const bool two = tb + STEP < n.t1;
+      if (two) load(tb + STEP, 1);
+      compute(x[0], v[0]);
+      if (two) compute(x[1], v[1]);
     }
   }
   // acc[q][j] element i: column (4 g + i) Q + q, rank 16 j + c.  The waves' tiles side by side in LDS,
