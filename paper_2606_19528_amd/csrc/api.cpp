@@ -1008,8 +1008,10 @@ size_t lora_linear_x8_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, in
 lora_status_t lora_linear_bwd_x8(const int8_t *x_codes, const float *x_scale, const void *W, const void *A, const void *B,
                                  const float *u_saved, const void *dy, void *dx, float *dA, float *dB, int64_t T, int64_t d_in,
                                  int64_t d_out, int64_t r, float scale, void *ws, size_t ws_bytes, void *hip_stream) {
-  return bwd_x8_impl(x_codes, x_scale, W, nullptr, nullptr, nullptr, 0, 0, A, B, u_saved, dy, dx, dA, dB, T, d_in, d_out, r,
-                     scale, ws, ws_bytes, hip_stream);
+  return guarded([&] {
+    return bwd_x8_impl(x_codes, x_scale, W, nullptr, nullptr, nullptr, 0, 0, A, B, u_saved, dy, dx, dA, dB, T, d_in, d_out, r,
+                       scale, ws, ws_bytes, hip_stream);
+  });
 }
 
 lora_status_t lora_linear_bwd_q_x8(const int8_t *x_codes, const float *x_scale, const void *W_codes, const float *W_scale,
@@ -1017,8 +1019,10 @@ lora_status_t lora_linear_bwd_q_x8(const int8_t *x_codes, const float *x_scale, 
                                    const float *u_saved, const void *dy, void *dx, float *dA, float *dB, int64_t T, int64_t d_in,
                                    int64_t d_out, int64_t r, float scale, void *ws, size_t ws_bytes, void *hip_stream) {
   if (!W_codes) return fail(LORA_EINVAL, "codes, scale and offset are required");
-  return bwd_x8_impl(x_codes, x_scale, nullptr, W_codes, W_scale, W_offset, bits, group, A, B, u_saved, dy, dx, dA, dB, T, d_in,
-                     d_out, r, scale, ws, ws_bytes, hip_stream);
+  return guarded([&] {
+    return bwd_x8_impl(x_codes, x_scale, nullptr, W_codes, W_scale, W_offset, bits, group, A, B, u_saved, dy, dx, dA, dB, T, d_in,
+                       d_out, r, scale, ws, ws_bytes, hip_stream);
+  });
 }
 
 lora_status_t frozen_linear_bwd_dx(const void *dy, const void *W, void *dx, int64_t T,

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <cstdio>
+#include <exception>
 
 #include "../../include/lora_mi355x.h"
 #include "launch.hpp"
@@ -22,6 +23,16 @@ inline lora_status_t hip_fail(hipError_t e, const char *what) {
   std::snprintf(text, sizeof text, "%s: %s", what, hipGetErrorString(e));
   set_last_error(text);
   return LORA_EHIP;
+}
+
+// A C entry point's body, out of which no exception comes: its lists may be refused memory.
+template <class F>
+lora_status_t guarded(F body) {
+  try {
+    return body();
+  } catch (const std::exception &) {
+    return fail(LORA_EHIP, "out of host memory");
+  }
 }
 
 // ----- kernel timing hook ----------------------------------------------------

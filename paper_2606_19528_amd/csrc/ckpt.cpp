@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "../../include/lora_mi355x.h"
+#include "api_util.hpp"
 #include "launch.hpp"
 
 namespace {
@@ -152,6 +153,96 @@ lora_status_t check8(const lora_node_t *nodes, int n, int64_t T, void *host_stas
   return LORA_OK;
 }
 
+lora_status_t forward_x8(const lora_node_t *nodes, int n, int64_t T, const void *x0, void *out, void *host_stash,
+                         size_t host_bytes, void *ws, size_t ws_bytes, void *compute_stream, void *copy_stream) {
+  Plan8 p;
+  lora_status_t s = check8(nodes, n, T, host_stash, host_bytes, ws, ws_bytes, &p);
+  if (s != LORA_OK) return s;
+  if (!x0 || !out) return fail(LORA_EINVAL, "x0 and out are required");
+  hipStream_t cs = (hipStream_t)compute_stream, xs = (hipStream_t)copy_stream;
+  char *wsb = (char *)ws;
+  void *act[2] = {wsb, wsb + p.act_bytes};
+  char *kept[2] = {wsb + 2 * p.act_bytes, wsb + 2 * p.act_bytes + p.kept_bytes};
+  void *opws = wsb + 2 * p.act_bytes + 2 * p.kept_bytes;
+  Events E;
+  // made[i]: input of node i in 8 bits; copied[i]: its copy to the host done
+  hipError_t e = E.make(2 * (size_t)n);
+  if (e != hipSuccess) return hipfail(e, "event creation");
+  hipEvent_t *made = E.ev.data(), *copied = E.ev.data() + n;
+  const void *cur = x0;
+  int last = -1, user[2] = {-1, -1};  // the last nodes that kept their input, of all and in each buffer
+  for (int i = 0; i < n; ++i) {
+    const lora_node_t &nd = nodes[i];
+    if (const size_t bytes = p.node_bytes[i]) {
+      // what kept[i % 2] last held must have reached the host
+      if (user[i % 2] >= 0 && (e = hipStreamWaitEvent(cs, copied[user[i % 2]], 0)) != hipSuccess) return hipfail(e, "wait");
+      s = act8_quantize(cur, (int8_t *)kept[i % 2], (float *)(kept[i % 2] + codes_bytes(T, nd.d_in)), T, nd.d_in, LORA_BF16, cs);
+      if (s != LORA_OK) return s;  // message set by act8_quantize
+      if ((e = hipEventRecord(made[i], cs)) != hipSuccess) return hipfail(e, "event");
+      if ((e = hipStreamWaitEvent(xs, made[i], 0)) != hipSuccess) return hipfail(e, "wait");
+      if ((e = lora::launch_host_copy((char *)host_stash + p.stash_off[i], kept[i % 2], bytes, true, xs)) != hipSuccess)
+        return hipfail(e, "copy to host");
+      if ((e = hipEventRecord(copied[i], xs)) != hipSuccess) return hipfail(e, "event");
+      last = user[i % 2] = i;
+    }
+    // the output buffer held the input of node i - 1, which the compute stream has done with
+    void *dst = i == n - 1 ? out : act[i % 2];
+    s = lora_linear_fwd(cur, nd.W, nd.A, nd.B, dst, nullptr, T, nd.d_in, nd.d_out, nd.r, nd.scale, LORA_BF16, opws, p.op_ws, cs);
+    if (s != LORA_OK) return s;  // message set by lora_linear_fwd
+    cur = dst;
+  }
+  // the stash must be complete before the backward reads it back, and this call's buffers free
+  if (last >= 0 && (e = hipStreamWaitEvent(cs, copied[last], 0)) != hipSuccess) return hipfail(e, "wait");
+  return LORA_OK;
+}
+
+lora_status_t backward_x8(const lora_node_t *nodes, int n, int64_t T, const void *g_n, void *dx0, const void *host_stash,
+                          size_t host_bytes, void *ws, size_t ws_bytes, void *compute_stream, void *copy_stream) {
+  Plan8 p;
+  lora_status_t s = check8(nodes, n, T, (void *)host_stash, host_bytes, ws, ws_bytes, &p);
+  if (s != LORA_OK) return s;
+  if (!g_n) return fail(LORA_EINVAL, "g_n is required");
+  hipStream_t cs = (hipStream_t)compute_stream, xs = (hipStream_t)copy_stream;
+  char *wsb = (char *)ws;
+  void *grad[2] = {wsb, wsb + p.act_bytes};
+  char *kept[2] = {wsb + 2 * p.act_bytes, wsb + 2 * p.act_bytes + p.kept_bytes};
+  void *opws = wsb + 2 * p.act_bytes + 2 * p.kept_bytes;
+  Events E;
+  // loaded[i]: input of node i back on the device; done[i]: node i's backward issued
+  hipError_t e = E.make(2 * (size_t)n + 1);
+  if (e != hipSuccess) return hipfail(e, "event creation");
+  hipEvent_t *loaded = E.ev.data(), *done = E.ev.data() + n, start = E.ev[2 * (size_t)n];
+  // the copies must not overtake work already queued on the compute stream
+  if ((e = hipEventRecord(start, cs)) != hipSuccess) return hipfail(e, "event");
+  if ((e = hipStreamWaitEvent(xs, start, 0)) != hipSuccess) return hipfail(e, "wait");
+  auto load = [&](int i) -> hipError_t {
+    if (!p.node_bytes[i]) return hipSuccess;
+    // kept[i % 2] last held the input of node i + 2
+    hipError_t r;
+    if (i + 2 < n && (r = hipStreamWaitEvent(xs, done[i + 2], 0)) != hipSuccess) return r;
+    if ((r = lora::launch_host_copy(kept[i % 2], (const char *)host_stash + p.stash_off[i], p.node_bytes[i], false, xs)) !=
+        hipSuccess)
+      return r;
+    return hipEventRecord(loaded[i], xs);
+  };
+  if ((e = load(n - 1)) != hipSuccess) return hipfail(e, "copy to device");
+  const void *g = g_n;
+  for (int i = n - 1; i >= 0; --i) {
+    const lora_node_t &nd = nodes[i];
+    if (i >= 1 && (e = load(i - 1)) != hipSuccess) return hipfail(e, "copy to device");  // one ahead
+    if (p.node_bytes[i] && (e = hipStreamWaitEvent(cs, loaded[i], 0)) != hipSuccess) return hipfail(e, "wait");
+    void *gout = i == 0 ? dx0 : grad[i % 2];
+    if (nd.r > 0 || gout) {
+      s = lora_linear_bwd_x8((const int8_t *)kept[i % 2], (const float *)(kept[i % 2] + codes_bytes(T, nd.d_in)), nd.W, nd.A, nd.B,
+                             nullptr, g, gout, nd.dA, nd.dB, T, nd.d_in, nd.d_out, nd.r, nd.scale, opws, p.op_ws, cs);
+      if (s != LORA_OK) return s;  // message set by lora_linear_bwd_x8
+    }
+    if ((e = hipEventRecord(done[i], cs)) != hipSuccess) return hipfail(e, "event");
+    g = gout;
+  }
+  return LORA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -254,102 +345,24 @@ lora_status_t lora_ckpt_backward(const lora_node_t *nodes, int n, int64_t T, con
 
 size_t lora_ckpt_workspace_bytes_x8(const lora_node_t *nodes, int n, int64_t T) {
   Plan8 p;
-  return plan8(nodes, n, T, &p) == LORA_OK ? p.total : (size_t)-1;
+  return lora::guarded([&] { return plan8(nodes, n, T, &p); }) == LORA_OK ? p.total : (size_t)-1;
 }
 
 size_t lora_ckpt_host_bytes_x8(const lora_node_t *nodes, int n, int64_t T) {
   Plan8 p;
-  return plan8(nodes, n, T, &p) == LORA_OK ? p.stash_bytes : (size_t)-1;
+  return lora::guarded([&] { return plan8(nodes, n, T, &p); }) == LORA_OK ? p.stash_bytes : (size_t)-1;
 }
 
 lora_status_t lora_ckpt_forward_x8(const lora_node_t *nodes, int n, int64_t T, const void *x0, void *out, void *host_stash,
                                    size_t host_bytes, void *ws, size_t ws_bytes, void *compute_stream, void *copy_stream) {
-  Plan8 p;
-  lora_status_t s = check8(nodes, n, T, host_stash, host_bytes, ws, ws_bytes, &p);
-  if (s != LORA_OK) return s;
-  if (!x0 || !out) return fail(LORA_EINVAL, "x0 and out are required");
-  hipStream_t cs = (hipStream_t)compute_stream, xs = (hipStream_t)copy_stream;
-  char *wsb = (char *)ws;
-  void *act[2] = {wsb, wsb + p.act_bytes};
-  char *kept[2] = {wsb + 2 * p.act_bytes, wsb + 2 * p.act_bytes + p.kept_bytes};
-  void *opws = wsb + 2 * p.act_bytes + 2 * p.kept_bytes;
-  Events E;
-  // made[i]: input of node i in 8 bits; copied[i]: its copy to the host done
-  hipError_t e = E.make(2 * (size_t)n);
-  if (e != hipSuccess) return hipfail(e, "event creation");
-  hipEvent_t *made = E.ev.data(), *copied = E.ev.data() + n;
-  const void *cur = x0;
-  int last = -1, user[2] = {-1, -1};  // the last nodes that kept their input, of all and in each buffer
-  for (int i = 0; i < n; ++i) {
-    const lora_node_t &nd = nodes[i];
-    if (const size_t bytes = p.node_bytes[i]) {
-      // what kept[i % 2] last held must have reached the host
-      if (user[i % 2] >= 0 && (e = hipStreamWaitEvent(cs, copied[user[i % 2]], 0)) != hipSuccess) return hipfail(e, "wait");
-      s = act8_quantize(cur, (int8_t *)kept[i % 2], (float *)(kept[i % 2] + codes_bytes(T, nd.d_in)), T, nd.d_in, LORA_BF16, cs);
-      if (s != LORA_OK) return s;  // message set by act8_quantize
-      if ((e = hipEventRecord(made[i], cs)) != hipSuccess) return hipfail(e, "event");
-      if ((e = hipStreamWaitEvent(xs, made[i], 0)) != hipSuccess) return hipfail(e, "wait");
-      if ((e = lora::launch_host_copy((char *)host_stash + p.stash_off[i], kept[i % 2], bytes, true, xs)) != hipSuccess)
-        return hipfail(e, "copy to host");
-      if ((e = hipEventRecord(copied[i], xs)) != hipSuccess) return hipfail(e, "event");
-      last = user[i % 2] = i;
-    }
-    // the output buffer held the input of node i - 1, which the compute stream has done with
-    void *dst = i == n - 1 ? out : act[i % 2];
-    s = lora_linear_fwd(cur, nd.W, nd.A, nd.B, dst, nullptr, T, nd.d_in, nd.d_out, nd.r, nd.scale, LORA_BF16, opws, p.op_ws, cs);
-    if (s != LORA_OK) return s;  // message set by lora_linear_fwd
-    cur = dst;
-  }
-  // the stash must be complete before the backward reads it back, and this call's buffers free
-  if (last >= 0 && (e = hipStreamWaitEvent(cs, copied[last], 0)) != hipSuccess) return hipfail(e, "wait");
-  return LORA_OK;
+  return lora::guarded(
+      [&] { return forward_x8(nodes, n, T, x0, out, host_stash, host_bytes, ws, ws_bytes, compute_stream, copy_stream); });
 }
 
 lora_status_t lora_ckpt_backward_x8(const lora_node_t *nodes, int n, int64_t T, const void *g_n, void *dx0, const void *host_stash,
                                     size_t host_bytes, void *ws, size_t ws_bytes, void *compute_stream, void *copy_stream) {
-  Plan8 p;
-  lora_status_t s = check8(nodes, n, T, (void *)host_stash, host_bytes, ws, ws_bytes, &p);
-  if (s != LORA_OK) return s;
-  if (!g_n) return fail(LORA_EINVAL, "g_n is required");
-  hipStream_t cs = (hipStream_t)compute_stream, xs = (hipStream_t)copy_stream;
-  char *wsb = (char *)ws;
-  void *grad[2] = {wsb, wsb + p.act_bytes};
-  char *kept[2] = {wsb + 2 * p.act_bytes, wsb + 2 * p.act_bytes + p.kept_bytes};
-  void *opws = wsb + 2 * p.act_bytes + 2 * p.kept_bytes;
-  Events E;
-  // loaded[i]: input of node i back on the device; done[i]: node i's backward issued
-  hipError_t e = E.make(2 * (size_t)n + 1);
-  if (e != hipSuccess) return hipfail(e, "event creation");
-  hipEvent_t *loaded = E.ev.data(), *done = E.ev.data() + n, start = E.ev[2 * (size_t)n];
-  // the copies must not overtake work already queued on the compute stream
-  if ((e = hipEventRecord(start, cs)) != hipSuccess) return hipfail(e, "event");
-  if ((e = hipStreamWaitEvent(xs, start, 0)) != hipSuccess) return hipfail(e, "wait");
-  auto load = [&](int i) -> hipError_t {
-    if (!p.node_bytes[i]) return hipSuccess;
-    // kept[i % 2] last held the input of node i + 2
-    hipError_t r;
-    if (i + 2 < n && (r = hipStreamWaitEvent(xs, done[i + 2], 0)) != hipSuccess) return r;
-    if ((r = lora::launch_host_copy(kept[i % 2], (const char *)host_stash + p.stash_off[i], p.node_bytes[i], false, xs)) !=
-        hipSuccess)
-      return r;
-    return hipEventRecord(loaded[i], xs);
-  };
-  if ((e = load(n - 1)) != hipSuccess) return hipfail(e, "copy to device");
-  const void *g = g_n;
-  for (int i = n - 1; i >= 0; --i) {
-    const lora_node_t &nd = nodes[i];
-    if (i >= 1 && (e = load(i - 1)) != hipSuccess) return hipfail(e, "copy to device");  // one ahead
-    if (p.node_bytes[i] && (e = hipStreamWaitEvent(cs, loaded[i], 0)) != hipSuccess) return hipfail(e, "wait");
-    void *gout = i == 0 ? dx0 : grad[i % 2];
-    if (nd.r > 0 || gout) {
-      s = lora_linear_bwd_x8((const int8_t *)kept[i % 2], (const float *)(kept[i % 2] + codes_bytes(T, nd.d_in)), nd.W, nd.A, nd.B,
-                             nullptr, g, gout, nd.dA, nd.dB, T, nd.d_in, nd.d_out, nd.r, nd.scale, opws, p.op_ws, cs);
-      if (s != LORA_OK) return s;  // message set by lora_linear_bwd_x8
-    }
-    if ((e = hipEventRecord(done[i], cs)) != hipSuccess) return hipfail(e, "event");
-    g = gout;
-  }
-  return LORA_OK;
+  return lora::guarded(
+      [&] { return backward_x8(nodes, n, T, g_n, dx0, host_stash, host_bytes, ws, ws_bytes, compute_stream, copy_stream); });
 }
 
 int lora_debug_host_mapped(const void *host, size_t bytes) {

@@ -48,7 +48,8 @@ def linear_bwd(xq, W, A, B, u, dy, s):
 def linear_bwd_bounds(xq, W, A, B, u, dy, s):
     """Bounds of the error of (dx, dA, dB).  du and u: sums of N (K) fp32 terms, which are exact
     products.  dx: their sum and du's rounding to bf16, then its own.  dA: du times
-    x's scale as two bf16 (2^-17 of it left), times whole numbers, summed over T."""
+    x's scale, rounded, as three bf16 (each half a step, 2^-9, of what the one before left: 2^-27 at the end),
+    times whole numbers, three sums over T in one."""
     T, K = xq.shape
     N = dy.shape[1]
     dyd, Ad, Bd = dy.double().abs(), A.double().abs(), B.double().abs()
@@ -56,11 +57,11 @@ def linear_bwd_bounds(xq, W, A, B, u, dy, s):
     du_err = abs(s) * (N + 3) * U * (dyd @ Bd)
     u_err = (K + 3) * U * mag_u if u is None else torch.zeros_like(mag_u)
     mag_du = abs(s) * (dyd @ Bd)
-    split = 2.0 ** -17
+    split = 2.0 ** -27 + U
     dx_mag = dyd @ W.double().abs() + mag_du @ Ad
     dx = (N + 8 + A.shape[0]) * U * dx_mag + (du_err + 2.0 ** -8 * mag_du) @ Ad
-    dA = (du_err + (split + (T + 8) * U) * mag_du).T @ xq.abs()
-    dB = abs(s) * (dyd.T @ (u_err + (split + (T + 8) * U) * mag_u))
+    dA = (du_err + (split + (3 * T + 8) * U) * mag_du).T @ xq.abs()
+    dB = abs(s) * (dyd.T @ (u_err + (split + (3 * T + 8) * U) * mag_u))
     return dx, dA, dB
 
 
