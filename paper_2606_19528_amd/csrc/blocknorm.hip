@@ -5,21 +5,28 @@
 //   n  = h' r1 (w1 + o)     r1 = 1 / sqrt(mean h'^2 + eps)
 // One pass over the data (blocknorm.hpp), which the memory path bounds.  Sums are fp32
 // in a fixed order.
+#include <type_traits>
+
 #include "blocknorm.hpp"
 
 namespace lora {
 
-// 1 / sqrt(mean x^2 + eps) of a row.  Rows whose squares leave fp32 are summed again in 64
-// bits (the branch is the same in all waves of a row, which are a workgroup where several).
-template <int NV, class S>
+// 1 / sqrt(mean x^2 + eps) of a row.  WIDE (all values fp32): in 64 bits, so that the root is the nearest
+// 32-bit value but for a few; sums in 32 bits left it off by 5e-8 of itself, which the copies in 8 bits
+// show where a value is near the middle of two codes.  Else in 32 bits, and rows whose squares leave these are
+// summed again in 64 (the branch is the same in all waves of a row, which are a workgroup where
+// several).
+template <bool WIDE, int NV, class S>
 __device__ __forceinline__ float row_rstd(const float (&x)[NV][8], int D, float eps, S &sum) {
-  float s = 0.0f;
+  if constexpr (!WIDE) {
+    float s = 0.0f;
 #pragma unroll
-  for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s = __builtin_fmaf(x[v][e], x[v][e], s);
-  s = sum(s);
-  if (__builtin_expect(s < __builtin_inff(), 1)) return 1.0f / __builtin_sqrtf(s / (float)D + eps);
+      for (int e = 0; e < 8; ++e) s = __builtin_fmaf(x[v][e], x[v][e], s);
+    s = sum(s);
+    if (__builtin_expect(s < __builtin_inff(), 1)) return 1.0f / __builtin_sqrtf(s / (float)D + eps);
+  }
   double t = 0.0;
 #pragma unroll
   for (int v = 0; v < NV; ++v)
@@ -73,7 +80,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void block_norm_fwd_kernel(B
       for (int v = 0; v < NV; ++v) keep8(E(), a.y8, x[v], row, D, a.ng, c.col(v));
     }
     if (a.post) {
-      const float r2 = row_rstd(x, D, a.eps, sum);
+      const float r2 = row_rstd<std::is_same<E, F32>::value>(x, D, a.eps, sum);
       if (c.t == 0 && a.rstd_post) a.rstd_post[row] = r2;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
@@ -118,7 +125,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void block_norm_fwd_kernel(B
     }
   }
   if (!a.n && !a.n8.codes && !a.rstd_pre) return;
-  const float r1 = row_rstd(x, D, a.eps, sum);
+  const float r1 = row_rstd<std::is_same<E, F32>::value>(x, D, a.eps, sum);
   if (c.t == 0 && a.rstd_pre) a.rstd_pre[row] = r1;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
