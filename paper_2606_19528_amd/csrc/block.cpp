@@ -84,7 +84,7 @@ bool whole(const lora_act8_t *k) { return !k || (k->codes && k->scale); }  // bo
 Act8Out act8_out(const lora_act8_t *k) { return k ? Act8Out{k->codes, k->scale} : Act8Out{}; }
 Act8In act8_in(const lora_act8_t *k) { return k ? Act8In{k->codes, k->scale} : Act8In{}; }
 
-size_t block_ws(int64_t T, int64_t D) { return round256((size_t)3 * block_norm_parts(T, D) * D * 4); }
+size_t block_ws(int64_t T, int64_t D) { return round256((size_t)2 * block_norm_parts(T, D) * D * 4); }
 
 }  // namespace
 

@@ -66,10 +66,12 @@ __device__ __forceinline__ void times(float (&x)[NV][8], const Raw8<E> (&w)[NV],
   }
 }
 
-// GRADS: the gradients that are sums over rows too.  Workgroups of 8 waves then (16 for the longest rows), which take
-// rows in turn and leave their sums of each column in part[0..2][workgroup][D]: of w1, w2
-// and a gate [D].
-constexpr int bnb_rows(int w, bool grads) { return grads ? (w >= 8 ? 1 : 8 / w) : w == 1 ? 4 : 1; }
+// GRADS: the gradients that are sums over rows too.  Workgroups of bnb_waves waves then, which take rows in
+// turn and leave their sums of each column in part[0..1][workgroup][D]: of dn hh, and of a yh dh times
+// the gate where that has a value a row; the sums for w2 and for a gate [D] are this one times the
+// column's gate or gain.
+constexpr int bnb_waves(int w) { return w % 3 == 0 ? 12 : w > 8 ? w : 8; }
+constexpr int bnb_rows(int w, bool grads) { return grads ? bnb_waves(w) / w : w == 1 ? 4 : 1; }
 constexpr int bnb_threads(int w, bool grads) { return 64 * w * bnb_rows(w, grads); }
 
 template <class E, class R, int W, int NV, bool GRADS>
@@ -80,19 +82,22 @@ __global__ __launch_bounds__(bnb_threads(W, GRADS)) void block_norm_bwd_kernel(B
   const int D = a.D, sub = bn_sub<W>(), wave = threadIdx.x >> 6;
   const float inv_d = 1.0f / (float)D;
   const bool need_y = a.post || a.dgate, block = a.dy || a.dgate || a.want_w2;
-  float s1[NV][8], s2[NV][8], sg[NV][8];
+  float s1[NV][8], sz[NV][8];
   if constexpr (GRADS) {
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s1[v][e] = s2[v][e] = sg[v][e] = 0.0f;
+      for (int e = 0; e < 8; ++e) s1[v][e] = sz[v][e] = 0.0f;
   }
   int slot = 0;
+  Raw8<E> w1[NV], w2[NV];  // (the same for all rows)
+  if (a.w_pre) bn_load<E>(w1, a.w_pre, 0, c);
+  if (a.w_post) bn_load<E>(w2, a.w_post, 0, c);
   // (all waves of a workgroup go round as often as its first row needs)
   for (int64_t r0 = (int64_t)blockIdx.x * RPW; r0 < a.T; r0 += (int64_t)gridDim.x * RPW) {
     const bool live = r0 + sub < a.T;
     const int64_t row = live ? r0 + sub : a.T - 1, at = row * D;
-    Raw8<E> dnr[NV], yr[NV], gr[NV], w1[NV], w2[NV];
+    Raw8<E> dnr[NV], yr[NV], gr[NV];
     Raw8<R> dhr[NV], hr[NV];
     if (a.dn) {
       bn_load<E>(dnr, a.dn, at, c);
@@ -101,8 +106,6 @@ __global__ __launch_bounds__(bnb_threads(W, GRADS)) void block_norm_bwd_kernel(B
     if (a.dh_out) bn_load<R>(dhr, a.dh_out, at, c);
     if (need_y) src_load<E>(yr, a.y, a.y8, row, a.ng, c);
     if (a.gate_mode & 1) bn_load<E>(gr, a.gate, a.gate_mode == BN_GATE_FULL ? at : 0, c);  // (channel, full)
-    if (a.w_pre) bn_load<E>(w1, a.w_pre, 0, c);
-    if (a.w_post) bn_load<E>(w2, a.w_post, 0, c);
     const float r1 = a.dn ? a.rstd_pre[row] : 0.0f, r2 = a.post ? a.rstd_post[row] : 1.0f;
     const float gt = a.gate_mode == BN_GATE_TOKEN ? E::to_float(((const typename E::T *)a.gate)[row]) : 1.0f;
     float h[NV][8], p[NV][8], y[NV][8], k[NV][8];  // hh, p and then dh, yh
@@ -201,31 +204,21 @@ __global__ __launch_bounds__(bnb_threads(W, GRADS)) void block_norm_bwd_kernel(B
     }
     if (!block) continue;
     if constexpr (GRADS) {
-      // a yh dh, for w2 times the gate and for the gate times the gain
-      if (need_y) {
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float z = a.res_scale * y[v][e] * p[v][e];
-            if (a.want_w2 && !(a.gate_mode & 1)) s2[v][e] = __builtin_fmaf(z, gt, s2[v][e]);
-            h[v][e] = z;
-          }
-        if (a.want_w2 && (a.gate_mode & 1)) {
+      if (a.want_w2 || a.want_gate) {
+        if (a.gate_mode == BN_GATE_FULL) {
 #pragma unroll
           for (int v = 0; v < NV; ++v) {
             float g[8];
             gr[v].get(g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s2[v][e] = __builtin_fmaf(h[v][e], g[e], s2[v][e]);
+            for (int e = 0; e < 8; ++e) sz[v][e] = __builtin_fmaf(a.res_scale * y[v][e] * p[v][e], g[e], sz[v][e]);
           }
-        }
-        if (a.want_gate) {
-          if (a.w_post) times<E>(h, w2, a.off);
+        } else {
+          const float m = a.res_scale * gt;
 #pragma unroll
           for (int v = 0; v < NV; ++v)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sg[v][e] += h[v][e];
+            for (int e = 0; e < 8; ++e) sz[v][e] = __builtin_fmaf(m * y[v][e], p[v][e], sz[v][e]);
         }
       }
     }
@@ -259,9 +252,9 @@ __global__ __launch_bounds__(bnb_threads(W, GRADS)) void block_norm_bwd_kernel(B
     const int64_t plane = (int64_t)gridDim.x * D;
     float *const out = a.part + (int64_t)blockIdx.x * D;
 #pragma unroll
-    for (int which = 0; which < 3; ++which) {
-      if (!(which == 0 ? a.want_w1 : which == 1 ? a.want_w2 : a.want_gate)) continue;
-      float(&s)[NV][8] = which == 0 ? s1 : which == 1 ? s2 : sg;
+    for (int which = 0; which < 2; ++which) {
+      if (!(which == 0 ? a.want_w1 : a.want_w2 ? a.want_w2 : a.want_gate)) continue;
+      float(&s)[NV][8] = which == 0 ? s1 : sz;
       if constexpr (RPW > 1) {
         __syncthreads();
         if (sub > 0) {
@@ -284,19 +277,19 @@ __global__ __launch_bounds__(bnb_threads(W, GRADS)) void block_norm_bwd_kernel(B
   }
 }
 
-// out[c] = sum over p < np of part[p][c]: 16 ranges of p, each ascending, for 64 columns a
+// Sums over p < np of part[which][p][c]: 16 ranges of p, each ascending, for 64 columns a
 // workgroup.
-__global__ __launch_bounds__(256) void block_norm_cols_kernel(const float *part, int np, int D, float *o1, float *o2, float *og) {
+template <class E>
+__global__ __launch_bounds__(256) void block_norm_cols_kernel(BlockNormBwd a, int np) {
   __shared__ f32x4 red[16][16];
-  const int which = blockIdx.y;
-  float *out = which == 0 ? o1 : which == 1 ? o2 : og;
-  if (!out) return;
+  const int which = blockIdx.y, D = a.D;
+  if (!(which == 0 ? a.want_w1 : a.want_w2 ? a.want_w2 : a.want_gate)) return;
   const int c = threadIdx.x & 15, s = threadIdx.x >> 4, col = blockIdx.x * 64 + 4 * c;  // (D is a multiple of 8)
   const int per = (np + 15) / 16, p0 = s * per, p1 = min(np, p0 + per);
   f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
   if (col < D) {
-    const float *src = part + ((int64_t)which * np + p0) * D + col;
-#pragma unroll 8
+    const float *src = a.part + ((int64_t)which * np + p0) * D + col;
+#pragma unroll 16
     for (int p = p0; p < p1; ++p, src += D) x += *(const f32x4 *)src;
   }
   red[s][c] = x;
@@ -304,19 +297,37 @@ __global__ __launch_bounds__(256) void block_norm_cols_kernel(const float *part,
   if (s != 0 || col >= D) return;
 #pragma unroll
   for (int k = 1; k < 16; ++k) x += red[k][c];
-  *(f32x4 *)(out + col) = x;
+  if (which == 0) {
+    *(f32x4 *)(a.want_w1 + col) = x;
+    return;
+  }
+  const bool channel = a.gate_mode == BN_GATE_CHANNEL;
+  f32x4 w2 = x, wg = x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (channel) w2[e] *= E::to_float(((const typename E::T *)a.gate)[col + e]);
+    if (a.w_post) wg[e] *= E::to_float(((const typename E::T *)a.w_post)[col + e]) + a.off;
+  }
+  if (a.want_w2) *(f32x4 *)(a.want_w2 + col) = w2;
+  if (a.want_gate) *(f32x4 *)(a.want_gate + col) = wg;
 }
 
-// Workgroups that sum over rows: one a CU, of 8 waves, with one vector a lane where the row allows it
-// (4096 x 2048 with an fp32 stream 37.7 us, in 12 waves 39.3, with two vectors 40.8, two
-// workgroups a CU 39.3).
+// Workgroups that sum over rows: one a CU, one vector a lane where the row allows it, as many waves as the
+// registers of two sums leave room for (4096 x 2048 with an fp32 stream 34.8 us: with 16 waves 39, with
+// two vectors 41, the next row's loads ahead 34.0, but 36.8 in the place of 32.7 for 4096 x 3072 in bf16
+// from 8 bits).  Rows of 6 vectors in 12 waves, two at a time: in 8 waves, one at a time and a quarter of the
+// lanes idle, 42.6 for 32.7.  Beyond 8192 columns a lane's two vectors do not fit 16 waves' registers, and
+// some of them go through memory: 1024 x 16384 253 us.
 constexpr int BNB_PARTS = 256;
 static BnShape grads_shape(int64_t D) {
   const int64_t n = (D + 511) / 512;
   if (n <= 1) return {1, 1};
   if (n <= 2) return {2, 1};
+  if (n <= 3) return {3, 1};
   if (n <= 4) return {4, 1};
+  if (n <= 6) return {6, 1};
   if (n <= 8) return {8, 1};
+  if (n <= 12) return {12, 1};
   if (n <= 16) return {8, 2};
   return {16, 2};
 }
@@ -334,16 +345,18 @@ static hipError_t bwd_grads(const BlockNormBwd &a, hipStream_t st) {
   switch (s.w * 8 + s.nv) {
     case 1 * 8 + 1: BWD(1, 1); break;
     case 2 * 8 + 1: BWD(2, 1); break;
+    case 3 * 8 + 1: BWD(3, 1); break;
     case 4 * 8 + 1: BWD(4, 1); break;
+    case 6 * 8 + 1: BWD(6, 1); break;
     case 8 * 8 + 1: BWD(8, 1); break;
+    case 12 * 8 + 1: BWD(12, 1); break;
     case 8 * 8 + 2: BWD(8, 2); break;
     default: BWD(16, 2); break;
   }
 #undef BWD
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(block_norm_cols_kernel, dim3((a.D + 63) / 64, 3), dim3(256), 0, st, a.part, np, a.D, a.want_w1, a.want_w2,
-                     a.want_gate);
+  hipLaunchKernelGGL((block_norm_cols_kernel<E>), dim3((a.D + 63) / 64, 2), dim3(256), 0, st, a, np);
   return hipGetLastError();
 }
 

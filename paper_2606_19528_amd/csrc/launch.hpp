@@ -497,7 +497,7 @@ struct BlockNormBwd {
   const float *rstd_post, *rstd_pre;
   void *dh, *dy, *dgate;
   float *want_w1, *want_w2, *want_gate;  // column sums [D] (want_gate: dgate of a gate [D]), or null
-  float *part;                           // workspace [3][block_norm_parts][D]
+  float *part;                           // workspace [2][block_norm_parts][D]
   int64_t T;
   int D, ng, gate_mode, post;
   float off, res_scale;
