@@ -470,19 +470,17 @@ __global__ __launch_bounds__(64 * X8P_NW) void x8_prod_kernel(X8Prod a, int part
 
 // du and u as one sum each, in place, of the partial sums that they came in: ascending, so the product
 // kernel's loads stay free of sums, which would wait for them.
-constexpr int X8_JOIN = 4;
 __global__ __launch_bounds__(256) void x8_join_kernel(float *du, int du_parts, float *u, int u_parts, int64_t n) {
   float *const x = blockIdx.y == 0 ? du : u;
   const int parts = blockIdx.y == 0 ? du_parts : u_parts;
   if (parts == 1) return;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    float v[X8_JOIN];  // all parts' loads at once
+    float v[MAX_SPLIT];  // all parts' loads at once
 #pragma unroll
-    for (int p = 0; p < X8_JOIN; ++p) v[p] = x[min(p, parts - 1) * n + i];
+    for (int p = 0; p < MAX_SPLIT; ++p) v[p] = x[min(p, parts - 1) * n + i];
     float s = v[0];
 #pragma unroll
-    for (int p = 1; p < X8_JOIN; ++p) s = p < parts ? s + v[p] : s;
-    for (int p = X8_JOIN; p < parts; ++p) s += x[p * n + i];
+    for (int p = 1; p < MAX_SPLIT; ++p) s = p < parts ? s + v[p] : s;
     x[i] = s;
   }
 }
@@ -518,6 +516,7 @@ hipError_t launch_x8_prod(const X8Prod &a, hipStream_t st) {
   const X8Plan p = x8_plan(a.T, a.K, a.N, a.r);
   const int items_b = (int)x8_items(a.N, ACT8_G / 2, a.r), items = items_b + (int)x8_items(a.K, ACT8_G, a.r);
   const dim3 grid(items * p.parts), block(64 * X8P_NW);
+  if (a.du_parts > MAX_SPLIT || a.u_parts > MAX_SPLIT) return hipErrorInvalidValue;
   if (p.parts > 64 || (p.parts > 1 && (!a.sync || !a.slots || a.gen == 0))) return hipErrorInvalidValue;
   if (a.du_parts > 1 || a.u_parts > 1) {
     const int64_t n = (int64_t)a.T * a.r;
