@@ -141,6 +141,7 @@ __global__ __launch_bounds__(bnb_threads(W, GRADS)) void block_norm_bwd_kernel(B
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         float f[8];
+        if constexpr (GRADS) dhr[v].keep_if(live);  // (an infinity there times y's zeros would be a NaN in a sum)
         dhr[v].get(f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[v][e] += f[e];

@@ -219,6 +219,20 @@ def test_backward_many_rows(T):
 
 
 @pytest.mark.parametrize("dt,rt", TYPES)
+@pytest.mark.parametrize("D", [256, 768, 1536, 3072])
+def test_an_infinite_gradient_in_the_last_row(D, dt, rt):
+    """Its column's sums are infinite, not NaN: rows of a workgroup behind the last add nothing to them."""
+    T = 5
+    c = make(T, D, dt, rt)
+    c["dh_out"][T - 1, 9] = float("inf")
+    r1, r2 = roots(c)
+    got = backward(c, r1, r2, True, True)
+    assert got["dw_post"][9].isinf() and got["dgate"][9].isinf()
+    for k in ("dw_pre", "dw_post", "dgate"):
+        assert got[k][torch.arange(D, device="cuda") != 9].isfinite().all(), k
+
+
+@pytest.mark.parametrize("dt,rt", TYPES)
 @pytest.mark.parametrize("kept", ["h", "y", "hy"])
 def test_backward_from_copies(dt, rt, kept):
     T, D = 45, 1000
