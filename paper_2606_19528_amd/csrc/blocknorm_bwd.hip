@@ -278,6 +278,183 @@ __global__ __launch_bounds__(bnb_threads(W, GRADS)) void block_norm_bwd_kernel(B
   }
 }
 
+// Rows whose values do not fit a workgroup's registers (over 12288 columns, or 8192 in fp32 or with sums over
+// rows): 16 waves (fp32: 8, which leave the registers for it) take two passes over a row, the first
+// for the three sums, the second for the outputs, a vector of a lane after the other; what the second reads is in
+// the caches.  Sums over rows stand in LDS, each lane's its own.  1024 x 16384 bf16 56 us, with sums 59, fp32
+// 118; with all of a row in registers, some of which go through memory, 116, 263 and 265.
+template <class E, class R>
+struct BnbVec {
+  Raw8<E> dn[1], y[1], g[1], w1[1], w2[1];
+  Raw8<R> dho[1], h[1];
+  template <int W>
+  __device__ __forceinline__ void load(const BlockNormBwd &a, int64_t row, const BnCols<W, 1> &c, bool need_y) {
+    const int64_t at = row * c.D;
+    if (a.dn) {
+      bn_load<E>(dn, a.dn, at, c);
+      src_load<R>(h, a.h, a.h8, row, a.ng, c);
+      if (a.w_pre) bn_load<E>(w1, a.w_pre, 0, c);
+    }
+    if (a.dh_out) bn_load<R>(dho, a.dh_out, at, c);
+    if (need_y) src_load<E>(y, a.y, a.y8, row, a.ng, c);
+    if (a.gate_mode & 1) bn_load<E>(g, a.gate, a.gate_mode == BN_GATE_FULL ? at : 0, c);
+    if (a.w_post) bn_load<E>(w2, a.w_post, 0, c);
+  }
+  // dn, hh, p, yh and k of the vector (dn and yh zeros past the row).
+  template <int W>
+  __device__ __forceinline__ void floats(const BlockNormBwd &a, const BnCols<W, 1> &c, float r1, float r2, bool need_y,
+                                         float (&d)[1][8], float (&x)[1][8], float (&p)[1][8], float (&z)[1][8],
+                                         float (&k)[1][8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d[0][e] = x[0][e] = p[0][e] = z[0][e] = 0.0f, k[0][e] = a.res_scale;
+    if (a.dn) {
+      src_floats<R>(x, h, a.h8, r1);
+      dn[0].keep_if(c.in(0));
+      dn[0].get(d[0]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[0][e] = d[0][e];
+      if (a.w_pre) times<E>(p, w1, a.off);
+    }
+    if (a.gate_mode & 1) times<E>(k, g, 0.0f);
+    if (a.w_post) times<E>(k, w2, a.off);
+    if (need_y) {
+      y[0].keep_if(c.in(0));
+      src_floats<E>(z, y, a.y8, r2);
+    }
+  }
+  // p, which is e, becomes dh' + r1 e.
+  __device__ __forceinline__ void add_stream(const BlockNormBwd &a, float r1, float (&p)[1][8]) {
+    float f[8];
+    dho[0].get(f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[0][e] = a.dh_out ? __builtin_fmaf(r1, p[0][e], f[e]) : r1 * p[0][e];
+  }
+};
+
+constexpr int BNL_V = 32;  // vectors of 64 lanes in the longest row
+template <class E, class R, int W, bool GRADS>
+__global__ __launch_bounds__(64 * W) void block_norm_bwd_long_kernel(BlockNormBwd a) {
+  constexpr int NV = BNL_V / W, NT = 64 * W;
+  __shared__ float red[2][3][W];
+  __shared__ f32x4 sums[GRADS ? 2 * NV * 2 : 1][GRADS ? NT : 1];  // [which][vector][half][lane]
+  const int D = a.D, t = threadIdx.x, wave = t >> 6;
+  const float inv_d = 1.0f / (float)D;
+  const bool need_y = a.post || a.dgate, block = a.dy || a.dgate || a.want_w2;
+  auto cols = [&](int v) { return BnCols<W, 1>{v * NT + t, D}; };
+  if constexpr (GRADS) {
+#pragma unroll
+    for (int k = 0; k < 4 * NV; ++k) sums[k][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  auto add = [&](int k, const float *f) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      f32x4 x = sums[2 * k + half][t];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += f[4 * half + e];
+      sums[2 * k + half][t] = x;
+    }
+  };
+  int slot = 0;
+  for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
+    const int64_t at = row * D;
+    const float r1 = a.dn ? a.rstd_pre[row] : 0.0f, r2 = a.post ? a.rstd_post[row] : 1.0f;
+    const float gt = a.gate_mode == BN_GATE_TOKEN ? E::to_float(((const typename E::T *)a.gate)[row]) : 1.0f;
+    float d[1][8], h[1][8], p[1][8], y[1][8], k[1][8];
+    float ca = 0.0f, cb = 0.0f, cc = 0.0f;
+#pragma unroll 1
+    for (int v = 0; v < NV; ++v) {
+      BnbVec<E, R> x;
+      x.load(a, row, cols(v), need_y);
+      x.floats(a, cols(v), r1, r2, need_y, d, h, p, y, k);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ca = __builtin_fmaf(p[0][e], h[0][e], ca);
+      x.add_stream(a, r1, p);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float ky = k[0][e] * y[0][e];
+        cb = __builtin_fmaf(ky, p[0][e], cb);
+        cc = __builtin_fmaf(ky, h[0][e], cc);
+      }
+    }
+    ca = wave_sum(ca);
+    cb = wave_sum(cb);
+    cc = wave_sum(cc);
+    // (two slots in turn, as in the kernel above)
+    float(*s)[W] = red[slot];
+    if ((t & 63) == 0) {
+      s[0][wave] = ca;
+      s[1][wave] = cb;
+      s[2][wave] = cc;
+    }
+    __syncthreads();
+    ca = s[0][0];
+    cb = s[1][0];
+    cc = s[2][0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+      ca += s[0][w];
+      cb += s[1][w];
+      cc += s[2][w];
+    }
+    slot ^= 1;
+    const float q = r1 * (ca * inv_d);            // dh = p - q hh
+    const float fy = __builtin_fmaf(-q, cc, cb);  // sum k dh yh
+    if (a.gate_mode == BN_GATE_TOKEN && a.dgate && t == 0) ((float *)a.dgate)[row] = fy;
+    const float kf = gt * r2, c2 = a.post ? kf * (fy * inv_d) : 0.0f;
+#pragma unroll 1
+    for (int v = 0; v < NV; ++v) {
+      const BnCols<W, 1> c = cols(v);
+      BnbVec<E, R> x;
+      x.load(a, row, c, need_y);
+      x.floats(a, c, r1, r2, need_y, d, h, p, y, k);
+      x.add_stream(a, r1, p);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[0][e] = __builtin_fmaf(-q, h[0][e], p[0][e]);
+        d[0][e] *= h[0][e];
+      }
+      if (c.in(0)) store8(R(), (typename R::T *)a.dh + at + c.at(0), p[0]);
+      if constexpr (GRADS) {
+        if (a.want_w1) add(v, d[0]);
+      }
+      if (!block) continue;
+      float z[1][8];  // a dh yh
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[0][e] = a.res_scale * y[0][e] * p[0][e];
+      if constexpr (GRADS) {
+        if (a.want_w2 || a.want_gate) {
+          float f[1][8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[0][e] = gt * z[0][e];
+          if (a.gate_mode == BN_GATE_FULL) times<E>(f, x.g, 0.0f);
+          add(NV + v, f[0]);
+        }
+      }
+      if (a.dgate && a.gate_mode == BN_GATE_FULL) {
+        if (a.w_post) times<E>(z, x.w2, a.off);
+        if (c.in(0)) store8(E(), (typename E::T *)a.dgate + at + c.at(0), z[0]);
+      }
+      if (!a.dy) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[0][e] = __builtin_fmaf(-c2, y[0][e], k[0][e] * kf * p[0][e]);
+      if (c.in(0)) store8(E(), (typename E::T *)a.dy + at + c.at(0), p[0]);
+    }
+  }
+  if constexpr (GRADS) {
+    float *const out = a.part + (int64_t)blockIdx.x * D;
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const BnCols<W, 1> c = cols(v);
+        if (!c.in(0) || !(which == 0 ? a.want_w1 : a.want_w2 ? a.want_w2 : a.want_gate)) continue;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          *(f32x4 *)(out + which * (int64_t)gridDim.x * D + c.col(0) + 4 * half) = sums[2 * (which * NV + v) + half][t];
+      }
+  }
+}
+
 // Sums over p < np of part[which][p][c]: 16 ranges of p, each ascending, for 64 columns a
 // workgroup.
 template <class E>
@@ -317,8 +494,7 @@ __global__ __launch_bounds__(256) void block_norm_cols_kernel(BlockNormBwd a, in
 // registers of two sums leave room for (4096 x 2048 with an fp32 stream 34.8 us: with 16 waves 39, with
 // two vectors 41, the next row's loads ahead 34.0, but 36.8 in the place of 32.7 for 4096 x 3072 in bf16
 // from 8 bits).  Rows of 6 vectors in 12 waves, two at a time: in 8 waves, one at a time and a quarter of the
-// lanes idle, 42.6 for 32.7.  Beyond 8192 columns a lane's two vectors do not fit 16 waves' registers, and
-// some of them go through memory: 1024 x 16384 253 us.
+// lanes idle, 42.6 for 32.7.
 constexpr int BNB_PARTS = 256;
 static BnShape grads_shape(int64_t D) {
   const int64_t n = (D + 511) / 512;
@@ -330,12 +506,19 @@ static BnShape grads_shape(int64_t D) {
   if (n <= 8) return {8, 1};
   if (n <= 12) return {12, 1};
   if (n <= 16) return {8, 2};
-  return {16, 2};
+  return {BNL_V, 1};  // (two passes)
 }
 
 int block_norm_parts(int64_t T, int64_t D) {
   const int rows = bnb_rows(grads_shape(D).w, true);
   return (int)std::min<int64_t>((T + rows - 1) / rows, BNB_PARTS);
+}
+
+template <class E, class R, bool GRADS>
+static hipError_t bwd_long(const BlockNormBwd &a, int grid, hipStream_t st) {
+  constexpr int W = E::VEC == 4 ? 8 : 16;
+  hipLaunchKernelGGL((block_norm_bwd_long_kernel<E, R, W, GRADS>), dim3(grid), dim3(64 * W), 0, st, a);
+  return hipPeekAtLastError();
 }
 
 template <class E, class R>
@@ -352,7 +535,7 @@ static hipError_t bwd_grads(const BlockNormBwd &a, hipStream_t st) {
     case 8 * 8 + 1: BWD(8, 1); break;
     case 12 * 8 + 1: BWD(12, 1); break;
     case 8 * 8 + 2: BWD(8, 2); break;
-    default: BWD(16, 2); break;
+    default: (void)bwd_long<E, R, true>(a, np, st); break;
   }
 #undef BWD
   const hipError_t e = hipGetLastError();
@@ -365,6 +548,7 @@ template <class E, class R>
 static hipError_t bwd_rows(const BlockNormBwd &a, hipStream_t st) {
   if (a.want_w1 || a.want_w2 || a.want_gate) return bwd_grads<E, R>(a, st);
   const BnShape s = bn_shape(a.T, a.D);
+  if (s.w * s.nv > (E::VEC == 4 ? 16 : 24)) return bwd_long<E, R, false>(a, (int)a.T, st);
   const dim3 grid((unsigned)(s.w == 1 ? (a.T + 3) / 4 : a.T));
 #define BWD(W, NV) hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false>), grid, dim3(bnb_threads(W, false)), 0, st, a)
   BN_SHAPES(s, BWD)

@@ -218,6 +218,25 @@ def test_backward_many_rows(T):
         assert all(torch.equal(got[k], again[k]) for k in got)  # (a fixed order)
 
 
+@pytest.mark.parametrize("dt,rt,gate", [(BF16, BF16, "channel"), (BF16, F32, "full"), (F32, F32, "token")])
+def test_backward_of_long_rows(dt, rt, gate):
+    """Rows that are passed over twice, two of them a workgroup, from whole values and from copies, the stream's
+    gradient in place."""
+    T, D = 258, 8264
+    c = make(T, D, dt, rt, gate=gate)
+    r1, r2 = roots(c)
+    got = backward(c, r1, r2, True, True)
+    check_backward(c, got, r1, r2, True)
+    d = dev(c)
+    dh = d["dh_out"].clone()
+    lm.block_norm_bwd(d["dn"], dh, d["h"], d["y"], dh=dh, w_pre=d["w_pre"], w_post=d["w_post"], gate=d["gate"], rstd_pre=r1.cuda(),
+                      rstd_post=r2.cuda(), res_scale=0.75, dw_pre=torch.empty(D, device="cuda"))
+    assert torch.equal(dh, got["dh"])
+    h8, y8 = (lm.act8_quantize(d[k], lm.act8_empty(T, D)) for k in ("h", "y"))
+    again = backward(c, r1, r2, True, True, h=h8, y=y8)
+    check_backward(c, again, r1, r2, True, h=ref.act8_values(*(t.cpu() for t in h8)), y=ref.act8_values(*(t.cpu() for t in y8)))
+
+
 @pytest.mark.parametrize("dt,rt", TYPES)
 @pytest.mark.parametrize("D", [256, 768, 1536, 3072])
 def test_an_infinite_gradient_in_the_last_row(D, dt, rt):
