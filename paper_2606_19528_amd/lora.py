@@ -810,15 +810,15 @@ def _code(dtype) -> int:
 
 def _dev_arg(t, name: str, dtype, shape, dev: int):
     """_arg of a tensor that has to be on device `dev`, the current one."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.get_device() != dev:
         raise ValueError(f"{name} must be on the current GPU")
-    if not t.is_contiguous():
-        raise ValueError("tensors must be contiguous (row-major, no padding)")
-    return t.data_ptr()
+    raise ValueError("tensors must be contiguous (row-major, no padding)")
 
 
 def _dev_opt(t, name: str, dtype, shape, dev: int):
@@ -946,7 +946,7 @@ def block_norm_fwd(h, y=None, h_out=None, n=None, w_pre=None, w_post=None, gate=
     shape, rt = h.shape, h.dtype
     torch, _, f32, _, _, _ = _torch_names()
     (T, D), dev = shape, torch.cuda.current_device()
-    dt = next((t for t in (y, n, w_pre) if t is not None), h).dtype
+    dt = (y if y is not None else n if n is not None else w_pre if w_pre is not None else h).dtype
     b = _block(T, D, dt, rt, post_norm, w_post, w_pre, gate, gain_offset, res_scale, dev)
     st = lib().block_norm_fwd(ctypes.byref(b), _dev_arg(h, "h", rt, shape, dev), _dev_opt(y, "y", dt, shape, dev),
                               _dev_opt(h_out, "h_out", rt, shape, dev), _dev_opt(n, "n", dt, shape, dev),
