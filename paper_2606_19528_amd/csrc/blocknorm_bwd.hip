@@ -548,7 +548,7 @@ template <class E, class R>
 static hipError_t bwd_rows(const BlockNormBwd &a, hipStream_t st) {
   if (a.want_w1 || a.want_w2 || a.want_gate) return bwd_grads<E, R>(a, st);
   const BnShape s = bn_shape(a.T, a.D);
-  if (s.w * s.nv > (E::VEC == 4 ? 16 : 24)) return bwd_long<E, R, false>(a, (int)a.T, st);
+  if (s.w * s.nv > (E::VEC == 4 ? 16 : 24)) return bwd_long<E, R, false>(a, (int)std::min<int64_t>(a.T, 1 << 16), st);
   const dim3 grid((unsigned)(s.w == 1 ? (a.T + 3) / 4 : a.T));
 #define BWD(W, NV) hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false>), grid, dim3(bnb_threads(W, false)), 0, st, a)
   BN_SHAPES(s, BWD)

@@ -18,6 +18,8 @@ def run(d, x8, W, u, s, want_dx=True, ws=None, stream=None):
     N, r = d["B"].shape
     dx = torch.full((T, K), 9.0, dtype=BF16, device="cuda") if want_dx else None
     dA, dB = torch.full((r, K), 9.0, device="cuda"), torch.full((N, r), 9.0, device="cuda")
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())  # (the outputs are filled there)
     fn = lm.lora_linear_bwd_q_x8 if isinstance(W, dict) else lm.lora_linear_bwd_x8
     fn(x8, W, d["A"], d["B"], u, d["dy"], dx, dA, dB, s, ws=ws, stream=stream)
     return dx, dA, dB
@@ -154,6 +156,46 @@ def test_stream_and_graph():
         want = run(d, x8, W, None, 1.0)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(have, want)), seed
+
+
+@pytest.mark.parametrize("T,K,N,r,bits", [(1, 264, 256, 8, 16), (24, 1024, 1024, 16, 16), (300, 520, 264, 32, 16),
+                                          (1040, 1032, 1032, 16, 16), (600, 264, 520, 33, 16), (520, 512, 1032, 8, 4)])
+def test_two_calls_at_once_and_replays(T, K, N, r, bits):
+    """Every way to dx, with u saved in one call and recomputed in another: on two streams at a time, each with
+    its workspace, and as two graphs that share one."""
+    inp, d, x8, xq, W, wide = case(T, K, N, r, bits=bits)
+    u = (xq @ inp["A"].double().T).float().cuda()
+    n = lm.lora_linear_x8_workspace_bytes(T, K, N, r)
+    want = [run(d, x8, W, v, 1.0) for v in (u, None)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    wss = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in streams]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    got = []
+    for _ in range(3):
+        both = []
+        for v, ws, st in zip((u, None), wss, streams):
+            with torch.cuda.stream(st):  # (the outputs are made there too)
+                both.append(run(d, x8, W, v, 1.0, ws=ws))
+        got.append(both)
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(a, b) for x, y in zip(g, want) for a, b in zip(x, y))
+    graphs, outs = [], []
+    for v in (u, None):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(run(d, x8, W, v, 1.0, ws=wss[0]))
+        graphs.append(g)
+    for k in range(4):
+        for o in outs:
+            for t in o:
+                t.zero_()
+        graphs[k % 2].replay()
+        run(d, x8, W, None, 1.0, ws=wss[1])
+        graphs[1 - k % 2].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(outs, want) for a, b in zip(x, y)), k
 
 
 # ---- the checkpointed chain -------------------------------------------------------------
