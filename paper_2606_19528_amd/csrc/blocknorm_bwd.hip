@@ -4,7 +4,7 @@
 //   dh = dh' + r1 (e - hh mean(e hh))                 dw1 = sum over rows of dn hh
 //   z = a dh,  f = g z (w2 + o)                       dg  = z yn, summed where g is broadcast
 //   dy = r2 (f - yh mean(f yh))                       dw2 = sum over rows of g z yh
-// One pass over the data (blocknorm.hpp): 4096 x 3072 in bf16 from 8-bit copies 28.2 us (126 MB, 4.5
+// One pass over the data (blocknorm.hpp): 4096 x 3072 in bf16 from 8-bit copies 25.4 us (126 MB, 5.0
 // TB/s), where a form with a branch a vector took 52: beside the memory path the vector
 // instructions count, a few hundred for 8 columns.  dh is linear in the
 // first mean, so that the second comes from sums taken with it: dh = p - c q with
@@ -74,7 +74,8 @@ constexpr int bnb_waves(int w) { return w % 3 == 0 ? 12 : w > 8 ? w : 8; }
 constexpr int bnb_rows(int w, bool grads) { return grads ? bnb_waves(w) / w : w == 1 ? 4 : 1; }
 constexpr int bnb_threads(int w, bool grads) { return 64 * w * bnb_rows(w, grads); }
 
-template <class E, class R, int W, int NV, bool GRADS>
+// ONCE: dn and dh' are read past the caches.
+template <class E, class R, int W, int NV, bool GRADS, bool ONCE>
 __global__ __launch_bounds__(bnb_threads(W, GRADS)) void block_norm_bwd_kernel(BlockNormBwd a) {
   constexpr int RPW = bnb_rows(W, GRADS), NWV = W * RPW;  // rows and waves of a workgroup
   __shared__ float red[2][3][NWV];
@@ -100,10 +101,10 @@ __global__ __launch_bounds__(bnb_threads(W, GRADS)) void block_norm_bwd_kernel(B
     Raw8<E> dnr[NV], yr[NV], gr[NV];
     Raw8<R> dhr[NV], hr[NV];
     if (a.dn) {
-      bn_load<E>(dnr, a.dn, at, c);
+      bn_load<E, ONCE>(dnr, a.dn, at, c);
       src_load<R>(hr, a.h, a.h8, row, a.ng, c);
     }
-    if (a.dh_out) bn_load<R>(dhr, a.dh_out, at, c);
+    if (a.dh_out) bn_load<R, ONCE>(dhr, a.dh_out, at, c);
     if (need_y) src_load<E>(yr, a.y, a.y8, row, a.ng, c);
     if (a.gate_mode & 1) bn_load<E>(gr, a.gate, a.gate_mode == BN_GATE_FULL ? at : 0, c);  // (channel, full)
     const float r1 = a.dn ? a.rstd_pre[row] : 0.0f, r2 = a.post ? a.rstd_post[row] : 1.0f;
@@ -525,7 +526,7 @@ template <class E, class R>
 static hipError_t bwd_grads(const BlockNormBwd &a, hipStream_t st) {
   const BnShape s = grads_shape(a.D);
   const int np = block_norm_parts(a.T, a.D);
-#define BWD(W, NV) hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, true>), dim3(np), dim3(bnb_threads(W, true)), 0, st, a)
+#define BWD(W, NV) hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, true, false>), dim3(np), dim3(bnb_threads(W, true)), 0, st, a)
   switch (s.w * 8 + s.nv) {
     case 1 * 8 + 1: BWD(1, 1); break;
     case 2 * 8 + 1: BWD(2, 1); break;
@@ -550,9 +551,20 @@ static hipError_t bwd_rows(const BlockNormBwd &a, hipStream_t st) {
   const BnShape s = bn_shape(a.T, a.D);
   if (s.w * s.nv > (E::VEC == 4 ? 16 : 24)) return bwd_long<E, R, false>(a, (int)std::min<int64_t>(a.T, 1 << 16), st);
   const dim3 grid((unsigned)(s.w == 1 ? (a.T + 3) / 4 : a.T));
-#define BWD(W, NV) hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false>), grid, dim3(bnb_threads(W, false)), 0, st, a)
-  BN_SHAPES(s, BWD)
+  // What is large and read once goes past the caches, which what is written then has: 4096 x 3072 from 8 bits 25.2 us
+  // for 27.6, 4096 x 2048 22.2 for 22.9.  (With sums over rows it gains nothing, 35.5 for 35.3.)
+  const bool once = a.T * (int64_t)a.D >= (int64_t)1 << 23;
+#define BWD(W, NV) \
+  hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false, false>), grid, dim3(bnb_threads(W, false)), 0, st, a)
+#define BWD_ONCE(W, NV) \
+  hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false, true>), grid, dim3(bnb_threads(W, false)), 0, st, a)
+  if (once) {
+    BN_SHAPES(s, BWD_ONCE)
+  } else {
+    BN_SHAPES(s, BWD)
+  }
 #undef BWD
+#undef BWD_ONCE
   return hipGetLastError();
 }
 
