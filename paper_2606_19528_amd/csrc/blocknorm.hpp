@@ -92,7 +92,7 @@ struct RowSum {
 };
 
 // Waves a row and vectors a lane, for a row of D columns.  Throughput: two vectors a lane
-// (16384 x 2048 forward with its 8-bit copies 79.7 us, one vector 81.5, four 88; 4096 x 3072
+// (16384 x 2048 forward with its 8-bit copies, read through the caches, 79.7 us, one vector 81.5, four 88; 4096 x 3072
 // backward 28.7, one 38, three 30.7).  Few rows: a lane's chain of loads and sums is the time,
 // so more waves share a row (one row of 2048 forward 2.2 us, with two waves 3.1).
 struct BnShape {

@@ -279,7 +279,7 @@ __global__ __launch_bounds__(bnb_threads(W, GRADS)) void block_norm_bwd_kernel(B
   }
 }
 
-// Rows whose values do not fit a workgroup's registers (over 12288 columns, or 8192 in fp32 or with sums over
+// Rows whose values do not fit a workgroup's registers (over 12288 columns, or 8192 with a stream of fp32 or sums over
 // rows): 16 waves (fp32: 8, which leave the registers for it) take two passes over a row, the first
 // for the three sums, the second for the outputs, a vector of a lane after the other; what the second reads is in
 // the caches.  Sums over rows stand in LDS, each lane's its own.  1024 x 16384 bf16 56 us, with sums 59, fp32
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(64 * W) void block_norm_bwd_long_kernel(BlockNormBw
   constexpr int NV = BNL_V / W, NT = 64 * W;
   __shared__ float red[2][3][W];
   __shared__ f32x4 sums[GRADS ? 2 * NV * 2 : 1][GRADS ? NT : 1];  // [which][vector][half][lane]
-  const int D = a.D, t = threadIdx.x, wave = t >> 6;
+  const int D = a.D, t = threadIdx.x, wave = t >> 6, nv = (D + 8 * NT - 1) / (8 * NT);
   const float inv_d = 1.0f / (float)D;
   const bool need_y = a.post || a.dgate, block = a.dy || a.dgate || a.want_w2;
   auto cols = [&](int v) { return BnCols<W, 1>{v * NT + t, D}; };
@@ -363,7 +363,7 @@ __global__ __launch_bounds__(64 * W) void block_norm_bwd_long_kernel(BlockNormBw
     float d[1][8], h[1][8], p[1][8], y[1][8], k[1][8];
     float ca = 0.0f, cb = 0.0f, cc = 0.0f;
 #pragma unroll 1
-    for (int v = 0; v < NV; ++v) {
+    for (int v = 0; v < nv; ++v) {
       BnbVec<E, R> x;
       x.load(a, row, cols(v), need_y);
       x.floats(a, cols(v), r1, r2, need_y, d, h, p, y, k);
@@ -403,7 +403,7 @@ __global__ __launch_bounds__(64 * W) void block_norm_bwd_long_kernel(BlockNormBw
     if (a.gate_mode == BN_GATE_TOKEN && a.dgate && t == 0) ((float *)a.dgate)[row] = fy;
     const float kf = gt * r2, c2 = a.post ? kf * (fy * inv_d) : 0.0f;
 #pragma unroll 1
-    for (int v = 0; v < NV; ++v) {
+    for (int v = 0; v < nv; ++v) {
       const BnCols<W, 1> c = cols(v);
       BnbVec<E, R> x;
       x.load(a, row, c, need_y);
@@ -545,26 +545,52 @@ static hipError_t bwd_grads(const BlockNormBwd &a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Waves a row and vectors a lane without sums over rows.  A stream of fp32 leaves registers for one vector a
+// lane (8192 x 2048 57.5 us, two 64.5; 4096 x 2048 all fp32 40.1, 53.3), one of bf16 for two (4096 x 3072 from
+// 8 bits 25.1, one 34.2) up to 4096 columns; beyond them more waves are faster (2048 x 5632 from
+// 8 bits 32.6 in 12 waves, 35.8 in 6; 2048 x 8192 with an fp32 stream 70 in 16, 76 in 8).
+static BnShape rows_shape(int64_t T, int64_t D, bool wide) {
+  const int64_t n = (D + 511) / 512;
+  if (T * n <= 1024 && n <= 8) return bn_shape(T, D);
+  if (n <= 1) return {1, 1};
+  if (n <= 8 && !wide) return bn_shape(T, D);
+  if (n <= 4) return {(int)n, 1};
+  if (n <= 6) return {6, 1};
+  if (n <= 8) return {8, 1};
+  if (n <= 12) return {12, 1};
+  if (n <= 16) return {16, 1};
+  return {12, 2};
+}
+
 template <class E, class R>
 static hipError_t bwd_rows(const BlockNormBwd &a, hipStream_t st) {
   if (a.want_w1 || a.want_w2 || a.want_gate) return bwd_grads<E, R>(a, st);
-  const BnShape s = bn_shape(a.T, a.D);
-  if (s.w * s.nv > (E::VEC == 4 ? 16 : 24)) return bwd_long<E, R, false>(a, (int)std::min<int64_t>(a.T, 1 << 16), st);
+  constexpr bool wide = R::VEC == 4;
+  if (a.D > (wide ? 8192 : 12288)) return bwd_long<E, R, false>(a, (int)std::min<int64_t>(a.T, 1 << 16), st);
+  const BnShape s = rows_shape(a.T, a.D, wide);
   const dim3 grid((unsigned)(s.w == 1 ? (a.T + 3) / 4 : a.T));
   // What is large and read once goes past the caches, which what is written then has: 4096 x 3072 from 8 bits 25.2 us
   // for 27.6, 4096 x 2048 22.2 for 22.9.  (With sums over rows it gains nothing, 35.5 for 35.3.)
   const bool once = a.T * (int64_t)a.D >= (int64_t)1 << 23;
-#define BWD(W, NV) \
-  hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false, false>), grid, dim3(bnb_threads(W, false)), 0, st, a)
-#define BWD_ONCE(W, NV) \
-  hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false, true>), grid, dim3(bnb_threads(W, false)), 0, st, a)
-  if (once) {
-    BN_SHAPES(s, BWD_ONCE)
+#define BWD(W, NV)                                                                                                     \
+  case W * 8 + NV:                                                                                                     \
+    if (once)                                                                                                          \
+      hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false, true>), grid, dim3(bnb_threads(W, false)), 0, st, a); \
+    else                                                                                                               \
+      hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false, false>), grid, dim3(bnb_threads(W, false)), 0, st, a); \
+    break;
+  if constexpr (wide) {
+    switch (s.w * 8 + s.nv) {
+      BWD(1, 1) BWD(2, 1) BWD(3, 1) BWD(4, 1) BWD(6, 1) BWD(8, 1) BWD(12, 1) BWD(16, 1)
+      default: return hipErrorInvalidValue;
+    }
   } else {
-    BN_SHAPES(s, BWD)
+    switch (s.w * 8 + s.nv) {
+      BWD(1, 1) BWD(4, 1) BWD(8, 1) BWD(12, 1) BWD(16, 1) BWD(1, 2) BWD(2, 2) BWD(3, 2) BWD(4, 2) BWD(12, 2)
+      default: return hipErrorInvalidValue;
+    }
   }
 #undef BWD
-#undef BWD_ONCE
   return hipGetLastError();
 }
 
