@@ -218,6 +218,44 @@ def test_backward_many_rows(T):
         assert all(torch.equal(got[k], again[k]) for k in got)  # (a fixed order)
 
 
+# rows of one to 25 vectors of a wave, as many as leave the forms for few rows
+MANY = [512, 1024, 1536, 2040, 2056, 3592, 4104, 6152, 8192, 12288, 12296]
+
+
+@pytest.mark.parametrize("dt,rt", TYPES)
+@pytest.mark.parametrize("D", MANY)
+def test_many_rows_of_every_width(D, dt, rt):
+    T = 1024 // ((D + 511) // 512) + 3
+    c = make(T, D, dt, rt, gate="token")
+    check_forward(c, forward(c, True), True)
+    r1, r2 = roots(c)
+    check_backward(c, backward(c, r1, r2, True, False), r1, r2, True)
+
+
+@pytest.mark.parametrize("dt,rt", TYPES)
+@pytest.mark.parametrize("D", MANY[1:])
+def test_large_calls_are_their_rows(D, dt, rt):
+    """Calls large enough to be read past the caches: the bits of calls over parts of their rows."""
+    T = (1 << 24) // D + 5
+    g = torch.Generator(device="cuda").manual_seed(D)
+    d = {k: torch.randn(T, D, generator=g, device="cuda").to(rt if k in ("h", "dh_out") else dt) for k in ("h", "y", "dn", "dh_out")}
+    w = {k: (1 + 0.1 * torch.randn(D, generator=g, device="cuda")).to(dt) for k in ("w_pre", "w_post", "gate")}
+    r = {k: 0.5 + torch.rand(T, generator=g, device="cuda") for k in ("rstd_pre", "rstd_post")}
+
+    def run(a, b):
+        p = {k: v[a:b] for k, v in d.items()}
+        n8, dh, dy = lm.act8_empty(b - a, D), torch.empty_like(p["h"]), torch.empty_like(p["y"])
+        ho, n = torch.empty_like(p["h"]), torch.empty_like(p["y"])
+        lm.block_norm_fwd(p["h"], p["y"], h_out=ho, n=n, n8=n8, **w)
+        lm.block_norm_bwd(p["dn"], p["dh_out"], p["h"], p["y"], dh=dh, dy=dy, **w, **{k: v[a:b].clone() for k, v in r.items()})
+        return ho, n, *n8, dh, dy
+
+    whole, cuts = run(0, T), [T * k // 5 for k in range(6)]
+    parts = [run(a, b) for a, b in zip(cuts, cuts[1:])]
+    for k, x in enumerate(whole):
+        assert torch.equal(x, torch.cat([p[k] for p in parts])), k
+
+
 @pytest.mark.parametrize("dt,rt,gate", [(BF16, BF16, "channel"), (BF16, F32, "full"), (F32, F32, "token")])
 def test_backward_of_long_rows(dt, rt, gate):
     """Rows that are passed over twice, two of them a workgroup, from whole values and from copies, the stream's
