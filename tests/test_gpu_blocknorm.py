@@ -384,3 +384,30 @@ def test_stream_and_graph():
         torch.cuda.synchronize()
         for k, v in everything.items():
             assert torch.equal(v, got[k]), k
+
+
+@pytest.mark.parametrize("D,kept", [(1032, False), (2048, True), (16384, False)])
+def test_offsets_past_32_bits(D, kept):
+    """More than 2^31 values: the last rows, which repeat the first ones, have their bits."""
+    n = 520  # rows that are repeated
+    k = (1 << 31) // (n * D) + 1
+    T = n * k
+    assert T * D > 1 << 31
+    c = {a: (b if b is None or b.shape[0] != n else b.repeat(k, 1)) for a, b in dev(make(n, D, BF16, BF16)).items()}
+    r = {a: (0.5 + torch.rand(n, device="cuda")).repeat(k) for a in ("rstd_pre", "rstd_post")}
+    w = {a: c[a] for a in ("w_pre", "w_post", "gate")}
+    n8, h8, y8 = (lm.act8_empty(T, D) if kept else None for _ in range(3))
+    ho, nn = torch.empty_like(c["h"]), torch.empty_like(c["y"])
+    lm.block_norm_fwd(c["h"], c["y"], h_out=ho, n=nn, n8=n8, h8=h8, y8=y8, **w)
+    out = [ho, nn]
+    dh, dy = torch.empty_like(c["h"]), torch.empty_like(c["y"])
+    lm.block_norm_bwd(c["dn"], c["dh_out"], h8 if kept else ho, y8 if kept else c["y"], dh=dh, dy=dy, **w, **r)
+    out += [dh, dy]
+    if kept:
+        out += [*n8, *h8, *y8]
+        x8, back = lm.act8_quantize(c["y"], lm.act8_empty(T, D)), torch.empty_like(c["y"])
+        lm.act8_dequantize(x8, back)
+        out += [*x8, back]
+    for i, t in enumerate(out):
+        assert torch.equal(t[-n:], t[:n]), i
+        assert torch.equal(t[(k // 2) * n:(k // 2 + 1) * n], t[:n]), i
