@@ -70,14 +70,14 @@ __device__ __forceinline__ void times(float (&x)[NV][8], const Raw8<E> (&w)[NV],
 // turn and leave their sums of each column in part[0..1][workgroup][D]: of dn hh, and of a yh dh times
 // the gate where that has a value a row; the sums for w2 and for a gate [D] are this one times the
 // column's gate or gain.
-constexpr int bnb_waves(int w) { return w % 3 == 0 ? 12 : w > 8 ? w : 8; }
-constexpr int bnb_rows(int w, bool grads) { return grads ? bnb_waves(w) / w : w == 1 ? 4 : 1; }
-constexpr int bnb_threads(int w, bool grads) { return 64 * w * bnb_rows(w, grads); }
+constexpr int bnb_waves(int w, bool wide) { return w > 12 ? w : w % 3 == 0 || (!wide && w > 1 && w < 8) ? 12 : 8; }
+constexpr int bnb_rows(int w, bool grads, bool wide) { return grads ? bnb_waves(w, wide) / w : w == 1 ? 4 : 1; }
+constexpr int bnb_threads(int w, bool grads, bool wide) { return 64 * w * bnb_rows(w, grads, wide); }
 
 // ONCE: dn and dh' are read past the caches.
 template <class E, class R, int W, int NV, bool GRADS, bool ONCE>
-__global__ __launch_bounds__(bnb_threads(W, GRADS)) void block_norm_bwd_kernel(BlockNormBwd a) {
-  constexpr int RPW = bnb_rows(W, GRADS), NWV = W * RPW;  // rows and waves of a workgroup
+__global__ __launch_bounds__(bnb_threads(W, GRADS, R::VEC == 4)) void block_norm_bwd_kernel(BlockNormBwd a) {
+  constexpr int RPW = bnb_rows(W, GRADS, R::VEC == 4), NWV = W * RPW;  // rows and waves of a workgroup
   __shared__ float red[2][3][NWV];
   const BnCols<W, NV> c{(int)threadIdx.x % (64 * W), a.D};
   const int D = a.D, sub = bn_sub<W>(), wave = threadIdx.x >> 6;
@@ -492,10 +492,10 @@ __global__ __launch_bounds__(256) void block_norm_cols_kernel(BlockNormBwd a, in
 }
 
 // Workgroups that sum over rows: one a CU, one vector a lane where the row allows it, as many waves as the
-// registers of two sums leave room for (4096 x 2048 with an fp32 stream 34.8 us: with 16 waves 39, with
-// two vectors 41, the next row's loads ahead 34.0, but 36.8 in the place of 32.7 for 4096 x 3072 in bf16
-// from 8 bits).  Rows of 6 vectors in 12 waves, two at a time: in 8 waves, one at a time and a quarter of the
-// lanes idle, 42.6 for 32.7.
+// registers of two sums leave room for (8192 x 2048 in bf16 49.2 us in 12 waves, 53.8 in 8; 4096 x 2048 with an fp32
+// stream 34.8 in 8, 36 in 12, 39 in 16, with two vectors 41, the next row's loads ahead 34.0, but 36.8 in the
+// place of 32.7 for 4096 x 3072 in bf16 from 8 bits).  Rows of 6 vectors in 12 waves, two at a time: in 8
+// waves, one at a time and a quarter of the lanes idle, 42.6 for 32.7.
 constexpr int BNB_PARTS = 256;
 static BnShape grads_shape(int64_t D) {
   const int64_t n = (D + 511) / 512;
@@ -510,10 +510,12 @@ static BnShape grads_shape(int64_t D) {
   return {BNL_V, 1};  // (two passes)
 }
 
-int block_norm_parts(int64_t T, int64_t D) {
-  const int rows = bnb_rows(grads_shape(D).w, true);
+static int grads_parts(int64_t T, int64_t D, bool wide) {
+  const int rows = bnb_rows(grads_shape(D).w, true, wide);
   return (int)std::min<int64_t>((T + rows - 1) / rows, BNB_PARTS);
 }
+// (for any types: an fp32 stream has at least as many)
+int block_norm_parts(int64_t T, int64_t D) { return grads_parts(T, D, true); }
 
 template <class E, class R, bool GRADS>
 static hipError_t bwd_long(const BlockNormBwd &a, int grid, hipStream_t st) {
@@ -525,8 +527,9 @@ static hipError_t bwd_long(const BlockNormBwd &a, int grid, hipStream_t st) {
 template <class E, class R>
 static hipError_t bwd_grads(const BlockNormBwd &a, hipStream_t st) {
   const BnShape s = grads_shape(a.D);
-  const int np = block_norm_parts(a.T, a.D);
-#define BWD(W, NV) hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, true, false>), dim3(np), dim3(bnb_threads(W, true)), 0, st, a)
+  constexpr bool wide = R::VEC == 4;
+  const int np = grads_parts(a.T, a.D, wide);
+#define BWD(W, NV) hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, true, false>), dim3(np), dim3(bnb_threads(W, true, wide)), 0, st, a)
   switch (s.w * 8 + s.nv) {
     case 1 * 8 + 1: BWD(1, 1); break;
     case 2 * 8 + 1: BWD(2, 1); break;
@@ -575,9 +578,9 @@ static hipError_t bwd_rows(const BlockNormBwd &a, hipStream_t st) {
 #define BWD(W, NV)                                                                                                     \
   case W * 8 + NV:                                                                                                     \
     if (once)                                                                                                          \
-      hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false, true>), grid, dim3(bnb_threads(W, false)), 0, st, a); \
+      hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false, true>), grid, dim3(bnb_threads(W, false, wide)), 0, st, a); \
     else                                                                                                               \
-      hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false, false>), grid, dim3(bnb_threads(W, false)), 0, st, a); \
+      hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, false, false>), grid, dim3(bnb_threads(W, false, wide)), 0, st, a); \
     break;
   if constexpr (wide) {
     switch (s.w * 8 + s.nv) {
