@@ -280,7 +280,7 @@ __global__ __launch_bounds__(bnb_threads(W, GRADS, R::VEC == 4)) void block_norm
 }
 
 // Rows whose values do not fit a workgroup's registers (over 12288 columns, or 8192 with a stream of fp32 or sums over
-// rows): 16 waves (fp32: 8, which leave the registers for it) take two passes over a row, the first
+// rows): 16 waves (up to 12288 columns 12, fp32 8, which leave the registers for it) take two passes over a row, the first
 // for the three sums, the second for the outputs, a vector of a lane after the other; what the second reads is in
 // the caches.  Sums over rows stand in LDS, each lane's its own.  1024 x 16384 bf16 56 us, with sums 59, fp32
 // 118; with all of a row in registers, some of which go through memory, 116, 263 and 265.
@@ -332,10 +332,9 @@ struct BnbVec {
   }
 };
 
-constexpr int BNL_V = 32;  // vectors of 64 lanes in the longest row
-template <class E, class R, int W, bool GRADS>
+template <class E, class R, int W, int NV, bool GRADS>
 __global__ __launch_bounds__(64 * W) void block_norm_bwd_long_kernel(BlockNormBwd a) {
-  constexpr int NV = BNL_V / W, NT = 64 * W;
+  constexpr int NT = 64 * W;
   __shared__ float red[2][3][W];
   __shared__ f32x4 sums[GRADS ? 2 * NV * 2 : 1][GRADS ? NT : 1];  // [which][vector][half][lane]
   const int D = a.D, t = threadIdx.x, wave = t >> 6, nv = (D + 8 * NT - 1) / (8 * NT);
@@ -507,7 +506,7 @@ static BnShape grads_shape(int64_t D) {
   if (n <= 8) return {8, 1};
   if (n <= 12) return {12, 1};
   if (n <= 16) return {8, 2};
-  return {BNL_V, 1};  // (two passes)
+  return {32, 1};  // (two passes)
 }
 
 static int grads_parts(int64_t T, int64_t D, bool wide) {
@@ -519,8 +518,11 @@ int block_norm_parts(int64_t T, int64_t D) { return grads_parts(T, D, true); }
 
 template <class E, class R, bool GRADS>
 static hipError_t bwd_long(const BlockNormBwd &a, int grid, hipStream_t st) {
-  constexpr int W = E::VEC == 4 ? 8 : 16;
-  hipLaunchKernelGGL((block_norm_bwd_long_kernel<E, R, W, GRADS>), dim3(grid), dim3(64 * W), 0, st, a);
+#define LONG(W, NV) hipLaunchKernelGGL((block_norm_bwd_long_kernel<E, R, W, NV, GRADS>), dim3(grid), dim3(64 * W), 0, st, a)
+  if constexpr (E::VEC == 4) LONG(8, 4);
+  else if (a.D <= 12288) LONG(12, 2);
+  else LONG(16, 2);
+#undef LONG
   return hipPeekAtLastError();
 }
 
