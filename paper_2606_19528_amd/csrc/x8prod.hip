@@ -491,9 +491,10 @@ static int64_t x8_items(int64_t L, int64_t cols, int64_t r) {
 }
 
 // Ranges of tokens: those that take the least time, in units of a step of a workgroup's waves (256
-// tokens).  A workgroup has a CU for itself, and spends about as much as X8_FIXED steps on
-// its first loads, the sums of its waves and the stores, X8_MEET more on a meeting.
-constexpr int X8_FIXED = 4, X8_MEET = 2;
+// tokens, 1.4 us with 16 ranks and 2.6 with 32).  A workgroup has a CU for itself, and spends about as much as
+// X8_FIXED steps on its first loads, the sums of its waves and the stores (3 us), X8_MEET more on a
+// meeting (2.7 us).
+constexpr int X8_FIXED = 2, X8_MEET = 2;
 X8Plan x8_plan(int64_t T, int64_t K, int64_t N, int64_t r) {
   constexpr int64_t STEP = X8P_NW * X8P_ROWS;
   const int64_t items = x8_items(K, ACT8_G, r) + x8_items(N, ACT8_G / 2, r), steps = (T + STEP - 1) / STEP;
