@@ -830,6 +830,7 @@ lora_status_t bwd_x8_impl(const int8_t *xc, const float *xs, const void *W, cons
   ra.V = B; ra.ldv = r; ra.vmode = V_KMAJ_TR; ra.r = (int)r;
   ra.nsplit = ns; ra.seg = L.sp.seg; ra.mb = L.sp.mb;
   ra.out_mult = scale; ra.out = pr.du; ra.out_stride = T * r;
+  ra.streamed = true;
   if (dx) {
     ra.tail = wsb + L.dutail; ra.ldt = L.ldt; ra.tail_mult = scale;
     if (ns > 1) {  // A repeated once per partial of du

@@ -255,6 +255,7 @@ struct RowArgs {
   int mb;  // row tiles of 16 per workgroup: 1 (0), 2 or 4 (bf16, r <= 32)
   unsigned *zero;  // row_skinny only: workgroup (0, 0) also sets zero[0 .. nzero) to 0
   int nzero;
+  bool streamed;  // row_skinny only, bf16, k-major V of 33 to 64 ranks: streamed through LDS too (other sums' order)
 };
 hipError_t launch_row_skinny(const RowArgs &a, Dtype dt, hipStream_t st);
 

@@ -40,10 +40,10 @@ typedef __attribute__((address_space(3))) rp_i16x4 rp_lds_i16x4;
 
 constexpr int ROW_NW = 8;  // waves per workgroup
 
-// Streamed through LDS (see above)?
-template <class E, int JB, int VMODE>
+// Streamed through LDS (see above)?  Up to 32 ranks, and up to 64 where the caller asks for it (U = 4).
+template <class E, int JB, int VMODE, int U>
 constexpr bool row_streamed() {
-  return sizeof(typename E::T) == 2 && JB <= 2 && (VMODE == V_ROW || VMODE == V_KMAJ_TR);
+  return sizeof(typename E::T) == 2 && (JB <= 2 || (JB <= 4 && U == 4)) && (VMODE == V_ROW || VMODE == V_KMAJ_TR);
 }
 constexpr int ROW_KS = 256;  // k per stage of the streamed form
 // Stage bytes and ring depth of the streamed form: 512-byte pieces of the 16 MB
@@ -59,7 +59,7 @@ constexpr int row_lds_bytes() {
   constexpr int CE = 128 / (int)sizeof(typename E::T);
   constexpr int REGION = U * CE * JB * 16 * 2;
   constexpr int RED = NW * 16 * MB * (JB * 16 + 1) * 4;
-  if constexpr (row_streamed<E, JB, VMODE>()) {
+  if constexpr (row_streamed<E, JB, VMODE, U>()) {
     constexpr int RING = row_nbuf<JB, MB>() * row_stage_bytes<JB, MB>();
     return RING > RED ? RING : RED;
   }
@@ -73,7 +73,7 @@ constexpr int row_lds_bytes() {
 template <class E, int JB, int VMODE, int U, int MB, bool COH = false, int NW = ROW_NW>
 __device__ __forceinline__ void row_item(const RowArgs &a, int bx, int by, int gx, int gy, char *smem) {
   constexpr int NT = 64 * NW;
-  static_assert(NW == 8 || (NW == 4 && row_streamed<E, JB, VMODE>()), "eight waves, or four streaming");
+  static_assert(NW == 8 || (NW == 4 && row_streamed<E, JB, VMODE, U>()), "eight waves, or four streaming");
   typedef typename E::T T;
   constexpr int VEC = E::VEC;
   constexpr int CE = 128 / (int)sizeof(T);  // elements per 128-byte chunk
@@ -138,7 +138,7 @@ __device__ __forceinline__ void row_item(const RowArgs &a, int bx, int by, int g
 #pragma unroll
     for (int jb = 0; jb < JB; ++jb) acc[mt][jb] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  if constexpr (row_streamed<E, JB, VMODE>()) {
+  if constexpr (row_streamed<E, JB, VMODE, U>()) {
     // Stage layout: rows 0 .. 16 MB - 1 of the item, then V (row-major: 16 JB
     // rows; k-major: the [256][r] block), 512 bytes per row.  Row-major
     // pieces keep their 16-byte chunk c at c ^ (row & 15), so the fragment
