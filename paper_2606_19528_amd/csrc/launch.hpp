@@ -356,7 +356,7 @@ struct NarrowPlan {
   int64_t flags;
   size_t slot_bytes, da_bytes;
 };
-NarrowPlan narrow_plan(int64_t T, int64_t N, int64_t K, int64_t r);
+NarrowPlan narrow_plan(int64_t T, int64_t N, int64_t K, int64_t r, bool grads = true);
 // Workspace that lora_linear_bwd cannot do without (the tiled kernels').
 size_t bwd_least_workspace(int64_t T, int64_t d_in, int64_t d_out, int64_t r, bool bf16);
 hipError_t launch_narrow(NarrowArgs a, const NarrowPlan &p, bool k_major, hipStream_t st);

@@ -522,17 +522,18 @@ hipError_t launch_narrow_sum(const float *planes, int parts, int n, float *u, hi
 }
 
 // ---- the shape of a call -----------------------------------------------------------
-NarrowPlan narrow_plan(int64_t T, int64_t N, int64_t K, int64_t r) {
+NarrowPlan narrow_plan(int64_t T, int64_t N, int64_t K, int64_t r, bool grads) {
   NarrowPlan p{};
   // Up to 64 tokens (32 above 32 rank columns); up to 128 where W has 2^22
   // weights or more, else the row tiles' meeting over dA costs more than the launch
   // saves; few_rule (api.cpp) says which directions.  fwd + bwd in us against the
   // tiled kernels: 24 tokens of 3072 -> 3072 25 against 160, 64 32 against 93, 128
   // 33 against 59; 50 of 8192 -> 3072 48 against 175; but 128 of 256 -> 256 19
-  // against 18, 128 of 2048 -> 256 with r = 64 43 against 34.  (A part's W rows lie
+  // against 18, 128 of 2048 -> 256 with r = 64 43 against 34.  Without dA and dB (`grads`
+  // false) there is no such meeting, and up to 128 tokens of any W are taken.  (A part's W rows lie
   // within 31-bit offsets.)
   if (T < 1 || T > NARROW_MAX_T || r < 0 || r > 64 || r % 4 || N * K >= (int64_t(1) << 30)) return p;
-  if ((T > 64 && N * K < (int64_t(1) << 22)) || (T > 32 && r > 32)) return p;
+  if ((grads && T > 64 && N * K < (int64_t(1) << 22)) || (T > 32 && r > 32)) return p;
   p.tiles_m = (int)((T + NW_BM - 1) / NW_BM);
   p.tiles_n = (int)((N + NW_BN - 1) / NW_BN);
   // Parts of the reduction: up to 64 tiles leave most CUs idle, and up to four
