@@ -494,13 +494,17 @@ lora_status_t lora_ckpt_backward_x8(const lora_node_t *nodes, int n, int64_t T, 
  * and gains of 1 where w_post or w_pre is NULL (o is then not added).  The gate g is one
  * value a channel [D], a token [T], or each element [T, D].
  * y, n, gains and gate have type dt; h, h' and their gradients res_dt: bf16 with either, or
- * fp32 with fp32.  Each output is rounded once (n from the unrounded h').
+ * fp32 with fp32.  fp32 values (h' of an fp32 stream; n and the roots where dt is fp32) are
+ * formed in 64 bits from the inputs, and from gain_offset, res_scale and eps as they are given,
+ * and rounded once, n from the unrounded h'; bf16 values are formed in 32 bits (h' too, from
+ * which n is) and then rounded.
  *   h_out     h'; may be h itself; NULL: not stored
  *   n         NULL, with n8 and rstd_pre too: no norm before the next block
  *   rstd_*    r2 and r1 [T] fp32 for the backward pass, optional
  *   y8 h8 n8  optional copies in 8 bits of y, h' and n as they are stored (bitwise what
  *             act8_quantize makes of them), written in the same pass
- * y NULL: h' = h, the norm alone.  eps >= 1e-30 (LORA_EINVAL).  D a multiple of 8 up to 16384,
+ * y NULL: h' = h, the norm alone.  eps >= 1e-30, and it, gain_offset and res_scale finite in 32
+ * bits (LORA_EINVAL).  D a multiple of 8 up to 16384,
  * T up to 2^22 (LORA_EUNSUPPORTED). */
 typedef enum {
   BLOCK_GATE_NONE = 0,
@@ -512,7 +516,7 @@ typedef struct {
   int64_t T, D;
   lora_dtype_t dt, res_dt;
   int post_norm, gate_mode;
-  float gain_offset, res_scale;
+  double gain_offset, res_scale;
   const void *w_post, *w_pre, *gate;
 } block_norm_t;
 typedef struct {
@@ -521,7 +525,7 @@ typedef struct {
 } lora_act8_t;
 lora_status_t block_norm_fwd(const block_norm_t *b, const void *h, const void *y, void *h_out, void *n,
                              float *rstd_post, float *rstd_pre, const lora_act8_t *y8,
-                             const lora_act8_t *h8, const lora_act8_t *n8, float eps,
+                             const lora_act8_t *h8, const lora_act8_t *n8, double eps,
                              void *hip_stream);
 /* Its backward, from dn (NULL: n had no use) and dh_out, the gradient of h' through the
  * stream (NULL: 0; one of the two is required), with hh = h' r1, yh = y r2, e = dn (w_pre + o):

@@ -21,6 +21,7 @@ constexpr int64_t kMaxT = int64_t(1) << 22;       // rows of a norm: fewer than 
 constexpr int64_t kMaxGroups = int64_t(1) << 29;  // groups of 128 values
 constexpr int64_t kMaxActT = int64_t(1) << 40;    // rows of an activation (keeps their product with D in 64 bits)
 
+bool finite32(double x) { return std::isfinite((float)x); }  // (bf16 rows and gradients take it in 32 bits)
 bool bad_dtype(lora_dtype_t dt) { return dt != LORA_BF16 && dt != LORA_F32; }
 Dtype dtype(lora_dtype_t dt) { return dt == LORA_BF16 ? DT_BF16 : DT_F32; }
 
@@ -47,7 +48,7 @@ lora_status_t check_block(const block_norm_t *b) {
   if ((b->gate_mode != BLOCK_GATE_NONE) != (b->gate != nullptr)) return fail(LORA_EINVAL, "a gate and its mode go together");
   if (b->post_norm != 0 && b->post_norm != 1) return fail(LORA_EINVAL, "post_norm must be 0 or 1");
   if (b->w_post && !b->post_norm) return fail(LORA_EINVAL, "w_post is the gain of a post norm");
-  if (!std::isfinite(b->res_scale) || !std::isfinite(b->gain_offset)) return fail(LORA_EINVAL, "res_scale and gain_offset must be finite");
+  if (!finite32(b->res_scale) || !finite32(b->gain_offset)) return fail(LORA_EINVAL, "res_scale and gain_offset must be finite");
   return LORA_OK;
 }
 
@@ -116,11 +117,11 @@ lora_status_t act8_dequantize(const int8_t *codes, const float *scale, void *x, 
 }
 
 lora_status_t block_norm_fwd(const block_norm_t *b, const void *h, const void *y, void *h_out, void *n, float *rstd_post,
-                             float *rstd_pre, const lora_act8_t *y8, const lora_act8_t *h8, const lora_act8_t *n8, float eps,
+                             float *rstd_pre, const lora_act8_t *y8, const lora_act8_t *h8, const lora_act8_t *n8, double eps,
                              void *hip_stream) {
   lora_status_t s = check_block(b);
   if (s != LORA_OK) return s;
-  if (!(eps >= 1e-30f) || !std::isfinite(eps)) return fail(LORA_EINVAL, "eps must be finite and at least 1e-30");
+  if (!(eps >= 1e-30) || !finite32(eps)) return fail(LORA_EINVAL, "eps must be finite and at least 1e-30");
   if (!h) return fail(LORA_EINVAL, "h is required");
   if (!whole(y8) || !whole(h8) || !whole(n8)) return fail(LORA_EINVAL, "a copy in 8 bits needs codes and scale");
   if (!y && (b->post_norm || b->gate || y8 || rstd_post)) return fail(LORA_EINVAL, "a post norm, a gate and y8 need y");
@@ -215,7 +216,7 @@ lora_status_t block_norm_bwd(const block_norm_t *b, const void *dn, const void *
   a.want_gate = b->gate_mode == BLOCK_GATE_CHANNEL ? (float *)dgate : nullptr;
   a.part = (float *)ws;
   a.T = b->T; a.D = (int)b->D; a.ng = (int)ng; a.gate_mode = b->gate_mode; a.post = block ? b->post_norm : 0;
-  a.off = b->gain_offset; a.res_scale = b->res_scale;
+  a.off = (float)b->gain_offset; a.res_scale = (float)b->res_scale;
   hipStream_t st = (hipStream_t)hip_stream;
   Timed t(K_BLOCK_NORM_BWD, st);
   const hipError_t err = launch_block_norm_bwd(a, dtype(b->dt), dtype(b->res_dt), st);

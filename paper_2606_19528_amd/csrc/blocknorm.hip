@@ -3,29 +3,29 @@
 //   yn = y r2 (w2 + o)      r2 = 1 / sqrt(mean y^2 + eps)      (yn = y without this norm)
 //   h' = h + a g yn
 //   n  = h' r1 (w1 + o)     r1 = 1 / sqrt(mean h'^2 + eps)
-// One pass over the data (blocknorm.hpp), which the memory path bounds.  Sums are fp32
-// in a fixed order.
+// One pass over the data (blocknorm.hpp), which the memory path bounds, sums in a fixed order.
+// What is stored in fp32 is formed in 64 bits and rounded once: a copy in 8 bits of a value near the middle of
+// two codes shows the last bit of it (a few of a million codes differed from those of the exact values, several 1e-5
+// of the copy's norm, where h' and n came from products in 32 bits).  Rows of bf16 values are formed in 32 bits.
 #include <type_traits>
 
 #include "blocknorm.hpp"
 
 namespace lora {
 
-// 1 / sqrt(mean x^2 + eps) of a row.  WIDE (all values fp32): in 64 bits, so that the root is the nearest
-// 32-bit value but for a few; sums in 32 bits left it off by 5e-8 of itself, which the copies in 8 bits
-// show where a value is near the middle of two codes.  Else in 32 bits, and rows whose squares leave these are
+// 1 / sqrt(mean x^2 + eps) of a row, in 64 bits (F double), or in 32, where rows whose squares leave these are
 // summed again in 64 (the branch is the same in all waves of a row, which are a workgroup where
 // several).
-template <bool WIDE, int NV, class S>
-__device__ __forceinline__ float row_rstd(const float (&x)[NV][8], int D, float eps, S &sum) {
-  if constexpr (!WIDE) {
+template <class F, class X, int NV, class S>
+__device__ __forceinline__ F row_rstd(const X (&x)[NV][8], int D, double eps, S &sum) {
+  if constexpr (std::is_same<F, float>::value) {
     float s = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int e = 0; e < 8; ++e) s = __builtin_fmaf(x[v][e], x[v][e], s);
     s = sum(s);
-    if (__builtin_expect(s < __builtin_inff(), 1)) return 1.0f / __builtin_sqrtf(s / (float)D + eps);
+    if (__builtin_expect(s < __builtin_inff(), 1)) return 1.0f / __builtin_sqrtf(s / (float)D + (float)eps);
   }
   double t = 0.0;
 #pragma unroll
@@ -33,7 +33,7 @@ __device__ __forceinline__ float row_rstd(const float (&x)[NV][8], int D, float 
 #pragma unroll
     for (int e = 0; e < 8; ++e) t = __builtin_fma((double)x[v][e], (double)x[v][e], t);
   t = sum(t);
-  return (float)(1.0 / __builtin_sqrt(t / D + (double)eps));
+  return (F)(1.0 / __builtin_sqrt(t / D + eps));
 }
 
 // A row's 8 values in 8 bits too, where asked for.  (f: as they are stored.)
@@ -51,10 +51,16 @@ __device__ __forceinline__ void round_to(E, float *f) {
   for (int e = 0; e < 8; ++e) f[e] = E::to_float(E::from_float(f[e]));
 }
 
+__device__ __forceinline__ float bn_fma(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
+__device__ __forceinline__ double bn_fma(double a, double b, double c) { return __builtin_fma(a, b, c); }
+
 // ONCE: y and h are read past the caches.
 template <class E, class R, int W, int NV, bool ONCE>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void block_norm_fwd_kernel(BlockNormFwd a) {
   constexpr int RPW = W == 1 ? 4 : 1;  // rows of a workgroup
+  constexpr bool WIDE = std::is_same<R, F32>::value;
+  using H = std::conditional_t<WIDE, double, float>;                         // h' and what goes into it
+  using N = std::conditional_t<std::is_same<E, F32>::value, double, float>;  // n
   __shared__ double red[2 * W];
   RowSum<W, W> sum(red);
   const BnCols<W, NV> c{(int)threadIdx.x % (64 * W), a.D};
@@ -72,76 +78,108 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void block_norm_fwd_kernel(B
   if (a.w_post) bn_load<E>(w2, a.w_post, 0, c);
   if (a.w_pre) bn_load<E>(w1, a.w_pre, 0, c);
   const float gt = a.gate_mode == BN_GATE_TOKEN ? E::to_float(((const typename E::T *)a.gate)[row]) : 1.0f;
-  float x[NV][8];
+  N x[NV][8];  // yn, h', n
   if (a.y) {
-    bn_floats<E>(x, yr, c);
+    float y[NV][8];
+    bn_floats<E>(y, yr, c);
+    // (WIDE: y is made anew from what was loaded for each of its uses, and in 64 bits four values at a time: kept
+    // it takes the room of a sixth of the waves)
+    auto anew = [&](int v) {
+      if constexpr (WIDE) {
+#pragma unroll
+        for (int k = 0; k < Raw8<E>::N; ++k) asm volatile("" : "+v"(yr[v].v[k]));
+        yr[v].get(y[v]);
+      }
+    };
     if (a.y8.codes) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) keep8(E(), a.y8, x[v], row, D, a.ng, c.col(v));
-    }
-    if (a.post) {
-      const float r2 = row_rstd<std::is_same<E, F32>::value>(x, D, a.eps, sum);
-      if (c.t == 0 && a.rstd_post) a.rstd_post[row] = r2;
-#pragma unroll
       for (int v = 0; v < NV; ++v) {
-        float w[8];
-        bn_gain<E, NV>(w, w2[v], a.w_post, a.off);
+        keep8(E(), a.y8, y[v], row, D, a.ng, c.col(v));
+        anew(v);
+      }
+    }
+    H r2 = 1;
+    if (a.post) {
+      r2 = row_rstd<H>(y, D, a.eps, sum);
+      if (c.t == 0 && a.rstd_post) a.rstd_post[row] = (float)r2;
+      if constexpr (!WIDE) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[v][e] *= r2 * w[e];
+        for (int v = 0; v < NV; ++v) {
+          float w[8];
+          bn_gain(w, w2[v], a.w_post, (float)a.off);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[v][e] *= r2 * w[e];
+        }
       }
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      float g[8], h[8];
+      float g[8], h[8], w[8];
+      anew(v);
+      w2[v].get(w);
       gr[v].get(g);
       hr[v].keep_if(c.in(v));
       hr[v].get(h);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[v][e] = __builtin_fmaf(a.res_scale, x[v][e] * (each ? g[e] : gt), h[e]);
+      for (int e = 0; e < 8; ++e) {
+        H yn = (H)y[v][e];
+        if constexpr (WIDE) {
+          if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+          yn *= r2 * (a.post && a.w_post ? (H)w[e] + (H)a.off : (H)1);  // (without a post norm times 1)
+        }
+        x[v][e] = (N)bn_fma((H)a.res_scale, yn * (H)(each ? g[e] : gt), (H)h[e]);
+      }
     }
     if (each) {  // (a gate of the row's last values is not one of the lanes past it)
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[v][e] = c.in(v) ? x[v][e] : 0.0f;
+        for (int e = 0; e < 8; ++e) x[v][e] = c.in(v) ? x[v][e] : (N)0;
     }
   } else {
-    bn_floats<R>(x, hr, c);
-  }
-  // The norm takes the sum as it is, before its rounding to the stream's type.
-  if (a.h_out) {
+    float h[NV][8];
+    bn_floats<R>(h, hr, c);
 #pragma unroll
     for (int v = 0; v < NV; ++v)
-      if (c.in(v)) store8(R(), (typename R::T *)a.h_out + at + c.at(v), x[v]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[v][e] = (N)h[v][e];
+  }
+  // The norm takes the sum before its rounding to a stream of n's type.
+  if (a.h_out) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = (float)x[v][e];
+      if (c.in(v)) store8(R(), (typename R::T *)a.h_out + at + c.at(v), f);
+    }
   }
   if (a.h8.codes) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       float f[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = x[v][e];
+      for (int e = 0; e < 8; ++e) f[e] = (float)x[v][e];
       round_to(R(), f);
       keep8(R(), a.h8, f, row, D, a.ng, c.col(v));
     }
   }
   if (!a.n && !a.n8.codes && !a.rstd_pre) return;
-  const float r1 = row_rstd<std::is_same<E, F32>::value>(x, D, a.eps, sum);
-  if (c.t == 0 && a.rstd_pre) a.rstd_pre[row] = r1;
+  const N r1 = row_rstd<N>(x, D, a.eps, sum);
+  if (c.t == 0 && a.rstd_pre) a.rstd_pre[row] = (float)r1;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    float w[8];
-    bn_gain<E, NV>(w, w1[v], a.w_pre, a.off);
+    N w[8];
+    float f[8];
+    bn_gain(w, w1[v], a.w_pre, (N)a.off);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[v][e] *= r1 * w[e];
-    if (a.n && c.in(v)) store8(E(), (typename E::T *)a.n + at + c.at(v), x[v]);
-  }
-  if (a.n8.codes) {
+    for (int e = 0; e < 8; ++e) f[e] = (float)(x[v][e] * (r1 * w[e]));
+    if (a.n && c.in(v)) store8(E(), (typename E::T *)a.n + at + c.at(v), f);
+    if (a.n8.codes) {
+      round_to(E(), f);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      round_to(E(), x[v]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[v][e] = c.in(v) ? x[v][e] : 0.0f;
-      keep8(E(), a.n8, x[v], row, D, a.ng, c.col(v));
+      for (int e = 0; e < 8; ++e) f[e] = c.in(v) ? f[e] : 0.0f;
+      keep8(E(), a.n8, f, row, D, a.ng, c.col(v));
     }
   }
 }

@@ -2,6 +2,8 @@
 // W waves hold a row, 8 NV values a lane, between the row's sums and its stores.
 #pragma once
 
+#include <type_traits>
+
 #include "act8.hpp"
 #include "launch.hpp"
 
@@ -39,11 +41,12 @@ __device__ __forceinline__ void bn_floats(float (&x)[NV][8], Raw8<E> (&r)[NV], c
   }
 }
 // Gains, loaded where there are any.
-template <class E, int NV>
-__device__ __forceinline__ void bn_gain(float *w, const Raw8<E> &r, bool any, float off) {
-  r.get(w);
+template <class F, class E>
+__device__ __forceinline__ void bn_gain(F *w, const Raw8<E> &r, bool any, F off) {
+  float f[8];
+  r.get(f);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) w[e] = any ? w[e] + off : 1.0f;
+  for (int e = 0; e < 8; ++e) w[e] = any ? (F)f[e] + off : (F)1;
 }
 
 // Sum of a wave, the same bits in each lane: within rows of 16 lanes in turn, then the four rows.
@@ -60,9 +63,22 @@ __device__ __forceinline__ float wave_sum(float x) {
   return (r0 + r1) + (r2 + r3);
 }
 __device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off);
-  return x;
+  auto turned = [](double v, auto ctrl) {  // (a double's halves, moved alike)
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_mov_dpp((int)b, decltype(ctrl)::value, 0xf, 0xf, true);
+    const uint32_t hi = __builtin_amdgcn_mov_dpp((int)(b >> 32), decltype(ctrl)::value, 0xf, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  };
+  x += turned(x, std::integral_constant<int, 0x128>());
+  x += turned(x, std::integral_constant<int, 0x124>());
+  x += turned(x, std::integral_constant<int, 0x122>());
+  x += turned(x, std::integral_constant<int, 0x121>());
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  auto row = [b](int lane) {
+    const uint32_t lo = __builtin_amdgcn_readlane((int)b, lane), hi = __builtin_amdgcn_readlane((int)(b >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  };
+  return (row(0) + row(16)) + (row(32) + row(48));
 }
 
 // Sums over the W waves of a row, NWV waves in the workgroup.

@@ -490,7 +490,7 @@ struct BlockNormFwd {
   Act8Out y8, h8, n8;
   int64_t T;
   int D, ng, gate_mode, post;
-  float eps, off, res_scale;
+  double eps, off, res_scale;  // (fp32 values are formed in 64 bits)
 };
 struct BlockNormBwd {
   const void *dn, *dh_out, *h, *y, *gate, *w_post, *w_pre;

@@ -62,8 +62,8 @@ class _Act8(ctypes.Structure):
 class _BlockNorm(ctypes.Structure):
     """block_norm_t of the C ABI."""
     _fields_ = [("T", ctypes.c_int64), ("D", ctypes.c_int64), ("dt", ctypes.c_int), ("res_dt", ctypes.c_int),
-                ("post_norm", ctypes.c_int), ("gate_mode", ctypes.c_int), ("gain_offset", ctypes.c_float),
-                ("res_scale", ctypes.c_float), ("w_post", ctypes.c_void_p), ("w_pre", ctypes.c_void_p),
+                ("post_norm", ctypes.c_int), ("gate_mode", ctypes.c_int), ("gain_offset", ctypes.c_double),
+                ("res_scale", ctypes.c_double), ("w_post", ctypes.c_void_p), ("w_pre", ctypes.c_void_p),
                 ("gate", ctypes.c_void_p)]
 
 
@@ -171,7 +171,7 @@ def lib() -> ctypes.CDLL:
         getattr(L, name).argtypes = [NP, i32, i64, vp, vp, vp, sz, vp, sz, vp, vp]
         getattr(L, name).restype = i32
     BP, AP = ctypes.POINTER(_BlockNorm), ctypes.POINTER(_Act8)
-    L.block_norm_fwd.argtypes = [BP, vp, vp, vp, vp, vp, vp, AP, AP, AP, f32, vp]
+    L.block_norm_fwd.argtypes = [BP, vp, vp, vp, vp, vp, vp, AP, AP, AP, ctypes.c_double, vp]
     L.block_norm_fwd.restype = i32
     L.block_norm_workspace_bytes.argtypes = [i64, i64]
     L.block_norm_workspace_bytes.restype = sz

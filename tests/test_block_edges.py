@@ -1,0 +1,14 @@
+"""CPU tests of the host logic around the norms between blocks at the edges of its arguments (fake,
+never-dereferenced pointers; refusals before any device work)."""
+import pytest
+
+import paper_2606_19528_amd as lm
+from test_block_api import EINVAL, bwd, fwd
+
+
+@pytest.mark.parametrize("fn,kw", [(fwd, dict(res_scale=1e39)), (fwd, dict(gain_offset=-1e39)), (bwd, dict(res_scale=1e39)),
+                                   (bwd, dict(gain_offset=1e300)), (fwd, dict(eps=1e39)), (fwd, dict(eps=0.99e-30))])
+def test_scalars_outside_32_bits(fn, kw):
+    """They are given in 64 bits; rows of bf16 values and gradients take them in 32."""
+    assert fn(**kw) == EINVAL
+    assert lm.lib().lora_last_error()

@@ -1,0 +1,85 @@
+"""Norms with gate and residual sum at the edges of their values, against their definitions in 64 bits."""
+import pytest
+import torch
+
+import paper_2606_19528_amd as lm
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+TYPES = [(BF16, BF16), (BF16, F32), (F32, F32)]
+EPS = 1e-6
+
+
+def inputs(T, D, dt, rt, post, gate, seed, off=0.0):
+    """Rows of different size with a few large channels, on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def randn(*shape):
+        return torch.randn(*shape, generator=g, device="cuda")
+
+    def activation():
+        x = randn(T, D) * torch.where(torch.rand(D, generator=g, device="cuda") < 0.01, 12.0, 1.0)
+        return x * (0.5 * randn(T, 1)).exp()
+
+    shape = {"none": None, "channel": (D,), "token": (T, 1), "full": (T, D)}[gate]
+    return {"h": activation().to(rt), "y": activation().to(dt), "gate": None if shape is None else randn(*shape).sigmoid().to(dt),
+            "w_pre": (1.0 - off + 0.2 * randn(D)).to(dt), "w_post": (1.0 - off + 0.2 * randn(D)).to(dt) if post else None}
+
+
+def act8(x):
+    """(codes, scale) of fp32 rows by the definition, quotients in 64 bits, on the GPU."""
+    T, D = x.shape
+    n = -(-D // 128)
+    wide = torch.nn.functional.pad(x, (0, n * 128 - D)).view(T, n, 128).double()
+    m = wide.abs().amax(2, keepdim=True)
+    q = torch.floor(wide.abs() * 127.0 / torch.where(m > 0, m, 1.0) + 0.5) * wide.sign()
+    return q.to(torch.int8).view(T, n * 128)[:, :D], (m[..., 0] / 127.0).float()
+
+
+def definition(c, post, off, a, eps):
+    y = c["y"].double()
+    if post:
+        y = y * (1.0 / torch.sqrt(y.square().mean(1, keepdim=True) + eps)) * (c["w_post"].double() + off)
+    h = c["h"].double() + a * y * (1.0 if c["gate"] is None else c["gate"].double())
+    return h, h * (1.0 / torch.sqrt(h.square().mean(1, keepdim=True) + eps)) * (c["w_pre"].double() + off)
+
+
+# rows of every number of waves, short last groups; 13 million values
+COPIES = [(4099, 328, True, "token"), (2053, 1096, True, "channel"), (1021, 2056, False, "full"), (517, 4104, True, "none"),
+          (301, 8200, True, "full"), (131, 12304, True, "channel"), (3, 1000, True, "token")]
+
+
+@pytest.mark.parametrize("dt,rt", TYPES)
+@pytest.mark.parametrize("T,D,post,gate", COPIES)
+def test_copies_of_computed_fp32_values(T, D, post, gate, dt, rt):
+    """fp32 values are computed in 64 bits and rounded once, so that their copies have the codes of the
+    definition's.  Both sides evaluate it in 64 bits: at most 10 roundings of 2^-53, of the parts of h' (|h| + |a y g
+    w r2|) or of n, and D of them in a mean, of which the root takes half.  A stored value is the nearest of the
+    definition's, so off by half a step, and by those roundings: at most
+    2^-24 |v| + 2^-53 ((10 + D) |v| + 10 parts).  (Which of two neighbours is stored where the value is within the
+    latter of their middle is open: with a = 0.7 and products of two bf16 values such middles are met, 7 / 10
+    times a multiple of 10.)  Of the values where the nearest is stored every code is the definition's."""
+    for off, a, eps in ((0.0, 0.7, EPS), (1.0, -1.3, 0.1)):
+        c = inputs(T, D, dt, rt, post, gate, seed=T + D, off=off)
+        h_out, n = torch.empty_like(c["h"]), torch.empty_like(c["y"])
+        y8, h8, n8 = (lm.act8_empty(T, D) for _ in range(3))
+        lm.block_norm_fwd(c["h"], c["y"], h_out=h_out, n=n, w_pre=c["w_pre"], w_post=c["w_post"], gate=c["gate"], y8=y8, h8=h8,
+                          n8=n8, eps=eps, gain_offset=off, res_scale=a)
+        h64, n64 = definition(c, post, off, a, eps)
+        parts = c["h"].double().abs() + (h64 - c["h"].double()).abs()
+        for name, k8, got, want in (("y", y8, c["y"], c["y"]), ("h", h8, h_out, h64), ("n", n8, n, n64)):
+            if name != "y":
+                if got.dtype != F32:
+                    continue  # (a computed bf16 value's copy is that of the value as it is stored)
+                ratio = 1.0 if name == "h" else want.abs() / h64.abs().clamp(min=1e-30)
+                bound = 2.0 ** -24 * want.abs() + 2.0 ** -53 * ((10 + D) * want.abs() + 10 * parts * ratio)
+                wrong = int(((got.double() - want).abs() > bound).sum())
+                assert wrong == 0, f"{name}: {wrong} values are not the nearest"
+            nearest = want.float()
+            codes, scale = act8(nearest)
+            wrong = int(((k8[0] != codes) & (got == nearest)).sum())
+            assert wrong == 0, f"{name}: {wrong} codes of {codes.numel()} are not the definition's"
+            wide = torch.nn.functional.pad(got == nearest, (0, -D % 128), value=True).view(T, -1, 128).all(2)
+            assert bool(((k8[1] == scale) | ~wide).all()), name
+            # (of h' by such products; of n, which has a root in it, one in 10^7 where D is 10^4)
+            assert float((got != nearest).double().mean()) <= (0.01 if name == "h" else 1e-6), name
