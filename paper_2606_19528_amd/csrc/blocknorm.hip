@@ -130,12 +130,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void block_norm_fwd_kernel(B
         x[v][e] = (N)bn_fma((H)a.res_scale, yn * (H)(each ? g[e] : gt), (H)h[e]);
       }
     }
-    if (each) {  // (a gate of the row's last values is not one of the lanes past it)
+    // (lanes past the row hold its last gains and gate, of which an infinity times 0 is no 0)
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[v][e] = c.in(v) ? x[v][e] : (N)0;
-    }
+      for (int e = 0; e < 8; ++e) x[v][e] = c.in(v) ? x[v][e] : (N)0;
   } else {
     float h[NV][8];
     bn_floats<R>(h, hr, c);

@@ -83,3 +83,32 @@ def test_copies_of_computed_fp32_values(T, D, post, gate, dt, rt):
             assert bool(((k8[1] == scale) | ~wide).all()), name
             # (of h' by such products; of n, which has a root in it, one in 10^7 where D is 10^4)
             assert float((got != nearest).double().mean()) <= (0.01 if name == "h" else 1e-6), name
+
+
+@pytest.mark.parametrize("dt,rt", TYPES)
+@pytest.mark.parametrize("D", [264, 1000, 8264])
+def test_infinite_gate_and_gain(D, dt, rt):
+    """Lanes behind a row's end take no part in its sums: a token's gate, or the gain of the last channel, may be
+    infinite, then h' is (there), and 1 / sqrt of its mean square is 0."""
+    T = 5
+    c = inputs(T, D, dt, rt, True, "token", seed=D)
+    c["y"][1].fill_(2.0)
+
+    def run(**kw):
+        o = {"h_out": torch.empty_like(c["h"]), "n": torch.empty_like(c["y"]), "rstd_pre": torch.empty(T, device="cuda")}
+        lm.block_norm_fwd(c["h"], c["y"], **{**{k: c[k] for k in ("w_pre", "w_post", "gate")}, **kw}, **o)
+        return o
+
+    plain = run()
+    gate = c["gate"].clone()
+    gate[1] = torch.inf
+    got = run(gate=gate)
+    assert bool(got["h_out"][1].isinf().all()) and float(got["rstd_pre"][1]) == 0.0 and bool(got["n"][1].isnan().all())
+    rows = [0, 2, 3, 4]
+    assert all(torch.equal(got[k][rows], plain[k][rows]) for k in got)
+    w = c["w_post"].clone()
+    w[D - 1] = torch.inf
+    got = run(w_post=w)
+    assert bool(got["h_out"][:, D - 1].isinf().all()) and torch.equal(got["h_out"][:, :D - 1], plain["h_out"][:, :D - 1])
+    assert bool((got["rstd_pre"] == 0).all())
+    assert bool((got["n"][:, :D - 1] == 0).all()) and bool(got["n"][:, D - 1].isnan().all())
