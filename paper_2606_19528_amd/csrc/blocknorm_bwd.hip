@@ -111,7 +111,7 @@ __global__ __launch_bounds__(bnb_threads(W, GRADS, R::VEC == 4)) void block_norm
     const float gt = a.gate_mode == BN_GATE_TOKEN ? E::to_float(((const typename E::T *)a.gate)[row]) : 1.0f;
     float h[NV][8], p[NV][8], y[NV][8], k[NV][8];  // hh, p and then dh, yh
     float ca = 0.0f, cb = 0.0f, cc = 0.0f;
-    // e = dn (w1 + o), p = dh' + r1 e.  Lanes past the row, and rows past the last, have dn and y
+    // e = dn (w1 + o), p = dh' + r1 e.  Lanes past the row, and rows past the last, have dn, dh' and y
     // zeros, so that they add nothing to a sum.
     if (a.dn) {
       src_floats<R>(h, hr, a.h8, r1);
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(bnb_threads(W, GRADS, R::VEC == 4)) void block_norm
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         float f[8];
-        if constexpr (GRADS) dhr[v].keep_if(live);  // (an infinity there times y's zeros would be a NaN in a sum)
+        dhr[v].keep_if(live && c.in(v));  // (an infinity there times y's zeros would be a NaN in a sum)
         dhr[v].get(f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[v][e] += f[e];
@@ -301,7 +301,7 @@ struct BnbVec {
     if (a.gate_mode & 1) bn_load<E>(g, a.gate, a.gate_mode == BN_GATE_FULL ? at : 0, c);
     if (a.w_post) bn_load<E>(w2, a.w_post, 0, c);
   }
-  // dn, hh, p, yh and k of the vector (dn and yh zeros past the row).
+  // dn, hh, p, yh and k of the vector (dn, dh' and yh zeros past the row).
   template <int W>
   __device__ __forceinline__ void floats(const BlockNormBwd &a, const BnCols<W, 1> &c, float r1, float r2, bool need_y,
                                          float (&d)[1][8], float (&x)[1][8], float (&p)[1][8], float (&z)[1][8],
@@ -322,6 +322,7 @@ struct BnbVec {
       y[0].keep_if(c.in(0));
       src_floats<E>(z, y, a.y8, r2);
     }
+    dho[0].keep_if(c.in(0));  // (an infinity there times y's zeros would be a NaN in a sum)
   }
   // p, which is e, becomes dh' + r1 e.
   __device__ __forceinline__ void add_stream(const BlockNormBwd &a, float r1, float (&p)[1][8]) {

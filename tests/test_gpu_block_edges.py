@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import block_reference as ref
 import paper_2606_19528_amd as lm
 
 pytestmark = pytest.mark.gpu
@@ -112,3 +113,37 @@ def test_infinite_gate_and_gain(D, dt, rt):
     assert bool(got["h_out"][:, D - 1].isinf().all()) and torch.equal(got["h_out"][:, :D - 1], plain["h_out"][:, :D - 1])
     assert bool((got["rstd_pre"] == 0).all())
     assert bool((got["n"][:, :D - 1] == 0).all()) and bool(got["n"][:, D - 1].isnan().all())
+
+
+@pytest.mark.parametrize("dt,rt", TYPES)
+@pytest.mark.parametrize("D", [264, 1000, 3080, 8264, 12296])
+@pytest.mark.parametrize("sums", [False, True])
+def test_an_infinite_stream_gradient_in_the_last_channel(D, dt, rt, sums):
+    """Lanes behind a row's end hold its last values and add nothing to its sums: where dh' is infinite
+    there, dy and a token's dgate are as by the definition, infinite and not NaN; other rows are what they are without it."""
+    T = 6
+    c = inputs(T, D, dt, rt, True, "token", seed=D)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    dn, dho = (torch.randn(T, D, generator=g, device="cuda").to(t) for t in (dt, rt))
+    r1, r2 = (0.5 + torch.rand(T, generator=g, device="cuda") for _ in range(2))
+
+    def run():
+        o = {"dh": torch.empty_like(c["h"]), "dy": torch.empty_like(c["y"]), "dgate": torch.empty(T, 1, device="cuda")}
+        w = torch.empty(D, device="cuda") if sums else None
+        lm.block_norm_bwd(dn, dho, c["h"], c["y"], **{k: c[k] for k in ("w_pre", "w_post", "gate")}, rstd_pre=r1, rstd_post=r2, dw_pre=w,
+                          res_scale=0.75, **o)
+        return o
+
+    plain = run()
+    dho[2, D - 1] = torch.inf
+    got = run()
+    cpu = {k: v.cpu() for k, v in c.items()}
+    want, _ = ref.norm_bwd(dn.cpu(), dho.cpu(), cpu["h"], cpu["y"], True, cpu["w_post"], cpu["gate"], cpu["w_pre"], r2.cpu(), r1.cpu(),
+                           0.0, 0.75)
+    for k, v in got.items():
+        rows = [0, 1, 3, 4, 5]
+        assert torch.equal(v[rows], plain[k][rows]), k
+        x, w = v[2].cpu().double(), want[k].reshape(v.shape)[2]
+        assert torch.equal(x.isnan(), w.isnan()) and torch.equal(x.isinf(), w.isinf()), k
+        inf = w.isinf()
+        assert torch.equal(x[inf], w[inf]), k
