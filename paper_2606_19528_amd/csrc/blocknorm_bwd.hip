@@ -401,7 +401,7 @@ __global__ __launch_bounds__(64 * W) void block_norm_bwd_long_kernel(BlockNormBw
     const float q = r1 * (ca * inv_d);            // dh = p - q hh
     const float fy = __builtin_fmaf(-q, cc, cb);  // sum k dh yh
     if (a.gate_mode == BN_GATE_TOKEN && a.dgate && t == 0) ((float *)a.dgate)[row] = fy;
-    const float kf = gt * r2, c2 = a.post ? kf * (fy * inv_d) : 0.0f;
+    const float kf = gt * r2, c2 = kf * (fy * inv_d);
 #pragma unroll 1
     for (int v = 0; v < nv; ++v) {
       const BnCols<W, 1> c = cols(v);
@@ -437,7 +437,11 @@ __global__ __launch_bounds__(64 * W) void block_norm_bwd_long_kernel(BlockNormBw
       }
       if (!a.dy) continue;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[0][e] = __builtin_fmaf(-c2, y[0][e], k[0][e] * kf * p[0][e]);
+      for (int e = 0; e < 8; ++e) p[0][e] = k[0][e] * kf * p[0][e];
+      if (a.post) {  // (else y, which dgate reads, may be infinite)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[0][e] = __builtin_fmaf(-c2, y[0][e], p[0][e]);
+      }
       if (c.in(0)) store8(E(), (typename E::T *)a.dy + at + c.at(0), p[0]);
     }
   }

@@ -147,3 +147,32 @@ def test_an_infinite_stream_gradient_in_the_last_channel(D, dt, rt, sums):
         assert torch.equal(x.isnan(), w.isnan()) and torch.equal(x.isinf(), w.isinf()), k
         inf = w.isinf()
         assert torch.equal(x[inf], w[inf]), k
+
+
+@pytest.mark.parametrize("dt,rt", TYPES)
+@pytest.mark.parametrize("D", [264, 8264, 12296])
+@pytest.mark.parametrize("gate,sums", [("token", False), ("token", True), ("full", False), ("full", True), ("channel", True)])
+def test_an_infinite_block_output_without_a_post_norm(D, dt, rt, gate, sums):
+    """dy = a g dh does not read y, which dgate does: its infinity comes into dgate alone, in the forms of
+    one pass over a row and of two."""
+    T = 4
+    c = inputs(T, D, dt, rt, False, gate, seed=D)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    dn, dho = (torch.randn(T, D, generator=g, device="cuda").to(t) for t in (dt, rt))
+    r1 = 0.5 + torch.rand(T, generator=g, device="cuda")
+
+    def run():
+        o = {"dh": torch.empty_like(c["h"]), "dy": torch.empty_like(c["y"])}
+        o["dgate"] = torch.empty(c["gate"].shape, dtype=dt if gate == "full" else F32, device="cuda")
+        w = torch.empty(D, device="cuda") if sums else None
+        lm.block_norm_bwd(dn, dho, c["h"], c["y"], w_pre=c["w_pre"], gate=c["gate"], rstd_pre=r1, dw_pre=w, res_scale=0.75, **o)
+        return o
+
+    plain = run()
+    c["y"][1, 9] = torch.inf
+    got = run()
+    assert torch.equal(got["dh"], plain["dh"]) and torch.equal(got["dy"], plain["dy"])
+    at = {"token": (1, 0), "full": (1, 9), "channel": (9,)}[gate]
+    assert bool(got["dgate"][at].isinf())
+    got["dgate"][at] = plain["dgate"][at]
+    assert torch.equal(got["dgate"], plain["dgate"])
