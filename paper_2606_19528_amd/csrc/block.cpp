@@ -17,7 +17,7 @@ static_assert(BN_GATE_CHANNEL == (int)BLOCK_GATE_CHANNEL && BN_GATE_TOKEN == (in
                   BN_GATE_FULL == (int)BLOCK_GATE_FULL && BN_GATE_NONE == (int)BLOCK_GATE_NONE,
               "the header's gate modes are the kernels'");
 
-constexpr int64_t kMaxT = int64_t(1) << 22;       // rows of a norm: fewer than 2^32 threads of up to 768 a row
+constexpr int64_t kMaxT = int64_t(1) << 22;       // rows of a norm
 constexpr int64_t kMaxGroups = int64_t(1) << 29;  // groups of 128 values
 constexpr int64_t kMaxActT = int64_t(1) << 40;    // rows of an activation (keeps their product with D in 64 bits)
 

@@ -64,7 +64,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void block_norm_fwd_kernel(B
   __shared__ double red[2 * W];
   RowSum<W, W> sum(red);
   const BnCols<W, NV> c{(int)threadIdx.x % (64 * W), a.D};
-  const int64_t row = (int64_t)blockIdx.x * RPW + bn_sub<W>();
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * RPW + bn_sub<W>();
   if (row >= a.T) return;  // (a wave's row is its own, or the workgroup's: none waits at a barrier)
   const int D = a.D;
   const int64_t at = row * D;
@@ -186,7 +186,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void block_norm_fwd_kernel(B
 template <class E, class R>
 static hipError_t fwd_shapes(const BlockNormFwd &a, hipStream_t st) {
   const BnShape s = bn_shape(a.T, a.D);
-  const dim3 grid((unsigned)(s.w == 1 ? (a.T + 3) / 4 : a.T)), block(s.w == 1 ? 256 : 64 * s.w);
+  const int64_t groups = s.w == 1 ? (a.T + 3) / 4 : a.T, gy = (groups + BN_GRID_ROWS - 1) / BN_GRID_ROWS;
+  const dim3 grid((unsigned)((groups + gy - 1) / gy), (unsigned)gy), block(s.w == 1 ? 256 : 64 * s.w);
   // Many rows that are written in 8 bits too are read past the caches, which what is written then has:
   // 16384 x 2048 with three copies 72.9 us for 80.6.  (Without copies it gains nothing, 48.2 for 48.2, and loses
   // where the caches hold h and y: 4096 x 2048 14.8 for 12.6.)

@@ -132,6 +132,10 @@ inline BnShape bn_shape(int64_t T, int64_t D) {
   if (n <= 24) return {12, 2};
   return {16, 2};
 }
+// Rows of up to 1024 threads each, one a workgroup, in a grid: a dimension holds fewer than 2^32
+// threads, so more rows go into the second one (or, in a kernel that takes rows in turn, come later).
+constexpr int64_t BN_GRID_ROWS = (int64_t)1 << 21;
+static_assert(BN_GRID_ROWS * 1024 < (int64_t)1 << 32, "a grid's dimension");
 #define BN_SHAPES(s, CASE)             \
   switch ((s).w * 8 + (s).nv) {        \
     case 1 * 8 + 1: CASE(1, 1); break; \

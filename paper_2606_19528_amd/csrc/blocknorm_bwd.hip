@@ -578,7 +578,7 @@ static hipError_t bwd_rows(const BlockNormBwd &a, hipStream_t st) {
   constexpr bool wide = R::VEC == 4;
   if (a.D > (wide ? 8192 : 12288)) return bwd_long<E, R, false>(a, (int)std::min<int64_t>(a.T, 1 << 16), st);
   const BnShape s = rows_shape(a.T, a.D, wide);
-  const dim3 grid((unsigned)(s.w == 1 ? (a.T + 3) / 4 : a.T));
+  const dim3 grid((unsigned)std::min(s.w == 1 ? (a.T + 3) / 4 : a.T, BN_GRID_ROWS));
   // What is large and read once goes past the caches, which what is written then has: 4096 x 3072 from 8 bits 25.2 us
   // for 27.6, 4096 x 2048 22.2 for 22.9.  (With sums over rows it gains nothing, 35.5 for 35.3.)
   const bool once = a.T * (int64_t)a.D >= (int64_t)1 << 23;

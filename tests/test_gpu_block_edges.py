@@ -176,3 +176,31 @@ def test_an_infinite_block_output_without_a_post_norm(D, dt, rt, gate, sums):
     assert bool(got["dgate"][at].isinf())
     got["dgate"][at] = plain["dgate"][at]
     assert torch.equal(got["dgate"], plain["dgate"])
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_the_most_rows(back):
+    """2^22 rows in 16 waves each, forward and backward: 2^32 threads, which no dimension of a grid holds.  The rows
+    repeat 512 of them, whose results they have."""
+    n, T = 512, 1 << 22
+    D = 6152 if back else 12296
+    g = torch.Generator(device="cuda").manual_seed(3)
+    few = torch.randn(n, D, generator=g, device="cuda").to(BF16)
+    many = torch.empty(T, D, dtype=BF16, device="cuda")
+    many.view(T // n, n, D).copy_(few.expand(T // n, n, D))
+
+    def run(x):
+        if back:
+            dy = torch.empty_like(x)
+            lm.block_norm_bwd(None, x, None, dh=x, dy=dy, res_scale=0.75)
+            return dy
+        r = torch.empty(x.shape[0], device="cuda")
+        lm.block_norm_fwd(x, rstd_pre=r)
+        return r
+
+    want = run(few)
+    got = run(many).view(T // n, *want.shape)
+    for a in range(0, T // n, 512):
+        assert bool((got[a:a + 512] == want).all()), a
+    del many, got
+    torch.cuda.empty_cache()
