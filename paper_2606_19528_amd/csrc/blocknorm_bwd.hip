@@ -528,7 +528,7 @@ static hipError_t bwd_long(const BlockNormBwd &a, int grid, hipStream_t st) {
   else if (a.D <= 12288) LONG(12, 2);
   else LONG(16, 2);
 #undef LONG
-  return hipPeekAtLastError();
+  return hipGetLastError();
 }
 
 template <class E, class R>
@@ -536,6 +536,7 @@ static hipError_t bwd_grads(const BlockNormBwd &a, hipStream_t st) {
   const BnShape s = grads_shape(a.D);
   constexpr bool wide = R::VEC == 4;
   const int np = grads_parts(a.T, a.D, wide);
+  hipError_t e = hipSuccess;
 #define BWD(W, NV) hipLaunchKernelGGL((block_norm_bwd_kernel<E, R, W, NV, true, false>), dim3(np), dim3(bnb_threads(W, true, wide)), 0, st, a)
   switch (s.w * 8 + s.nv) {
     case 1 * 8 + 1: BWD(1, 1); break;
@@ -546,11 +547,10 @@ static hipError_t bwd_grads(const BlockNormBwd &a, hipStream_t st) {
     case 8 * 8 + 1: BWD(8, 1); break;
     case 12 * 8 + 1: BWD(12, 1); break;
     case 8 * 8 + 2: BWD(8, 2); break;
-    default: (void)bwd_long<E, R, true>(a, np, st); break;
+    default: e = bwd_long<E, R, true>(a, np, st); break;
   }
 #undef BWD
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || (e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL((block_norm_cols_kernel<E>), dim3((a.D + 63) / 64, 2), dim3(256), 0, st, a, np);
   return hipGetLastError();
 }
