@@ -974,9 +974,9 @@ def block_norm_bwd(dn, dh_out, h, y=None, dh=None, dy=None, w_pre=None, w_post=N
     shape, rt = dh.shape, dh.dtype
     torch, _, f32, _, _, _ = _torch_names()
     (T, D), dev = shape, torch.cuda.current_device()
-    dt = next((t for t in (dn, dy, w_pre, gate) if t is not None), dh).dtype
-    b = _block(T, D, dt, rt, post_norm, w_post, w_pre, gate, gain_offset, res_scale, dev)
     whole_h, whole_y = not isinstance(h, (tuple, list)), not isinstance(y, (tuple, list))
+    dt = next((t for t in (dn, dy, w_pre, gate, w_post, y if whole_y else None) if t is not None), dh).dtype
+    b = _block(T, D, dt, rt, post_norm, w_post, w_pre, gate, gain_offset, res_scale, dev)
     wp, wn = None, 0
     if ws is not None or dw_pre is not None or dw_post is not None or (dgate is not None and b.gate_mode == BLOCK_GATE_CHANNEL):
         wp, wn, ws = _ws_for(ws, lambda: block_norm_workspace_bytes(T, D), dh, stream)

@@ -204,3 +204,19 @@ def test_the_most_rows(back):
         assert bool((got[a:a + 512] == want).all()), a
     del many, got
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("kept", [False, True])
+def test_the_gradient_of_a_post_gain_alone(kept):
+    """bf16 y and gain behind an fp32 stream, through which alone a gradient comes."""
+    T, D = 70, 264
+    c = inputs(T, D, BF16, F32, True, "none", seed=4)
+    dho = torch.randn(T, D, generator=torch.Generator(device="cuda").manual_seed(5), device="cuda")
+    r2 = 0.5 + torch.rand(T, device="cuda")
+    y8 = lm.act8_quantize(c["y"], lm.act8_empty(T, D))
+    y = ref.act8_values(*(t.cpu() for t in y8)) if kept else c["y"].cpu()
+    dh, w = torch.empty_like(dho), torch.empty(D, device="cuda")
+    lm.block_norm_bwd(None, dho, None, y8 if kept else c["y"], dh=dh, w_post=c["w_post"], rstd_post=r2, dw_post=w, res_scale=0.75)
+    want, err = ref.norm_bwd(None, dho.cpu(), None, y, True, c["w_post"].cpu(), None, None, r2.cpu(), None, 0.0, 0.75)
+    assert torch.equal(dh, dho)
+    ref.check(w, want["dw_post"], err["dw_post"], "dw_post")
