@@ -582,6 +582,19 @@ typedef struct {
 lora_status_t lora_few_token_plan(int64_t T, int64_t d_in, int64_t d_out, int64_t r, lora_dtype_t dt,
                                   lora_few_token_plan_t *plan);
 
+/* How lora_linear_bwd_x8 (quantized = 0) or lora_linear_bwd_q_x8 (1) runs these sizes, with dx
+ * wanted (1) or not (0): whether dx comes from the few-token kernel, and over how many parts
+ * of its reduction; else whether du's rows are producers in dx's launch; else over how many partial
+ * sums du is computed; those of a recomputed u; and the ranges of tokens that dA and dB run
+ * over (more than one meet in the launch).  All 0 for r = 0, where lora_linear_bwd's kernels
+ * run.  Host logic only; errors as for lora_linear_plan, LORA_EINVAL for flags other than 0 and 1,
+ * LORA_EUNSUPPORTED for r > 64 with a quantized base. */
+typedef struct {
+  int few_tokens, few_parts, fused, du_parts, u_parts, token_ranges;
+} lora_x8_plan_t;
+lora_status_t lora_linear_x8_plan(int64_t T, int64_t d_in, int64_t d_out, int64_t r, int quantized,
+                                  int want_dx, lora_x8_plan_t *plan);
+
 /* A fused launch hands the rank-r rows from its producer workgroups to its
  * tiles through counters in the workspace; a wait for them gives up after a
  * bounded time (0.2 s) instead of hanging, and a launch whose wait gave up

@@ -12,7 +12,7 @@ from .lora import (LORA_BF16, LORA_F32, LORA_OP_BWD, LORA_OP_FROZEN_DX, LORA_OP_
                    embed_bwd_workspace_bytes, embed_fwd, GradList, grad_clip, grad_list, grad_norm, policy_loss,
                    preference_loss, token_logp, token_loss_workspace_bytes,
                    ACT8_GROUP, act8_dequantize, act8_empty, act8_quantize, lora_linear_bwd_q_x8, lora_linear_bwd_x8,
-                   lora_linear_x8_workspace_bytes, lora_ckpt_backward_x8, lora_ckpt_forward_x8, lora_ckpt_sizes_x8,
+                   lora_linear_x8_plan, lora_linear_x8_workspace_bytes, lora_ckpt_backward_x8, lora_ckpt_forward_x8, lora_ckpt_sizes_x8,
                    BLOCK_GATE_CHANNEL, BLOCK_GATE_FULL, BLOCK_GATE_NONE, BLOCK_GATE_TOKEN, block_norm_bwd, block_norm_fwd,
                    block_norm_workspace_bytes,
                    topk_table_build, lora_linear_plan, lora_few_token_plan, handover_giveups, debug_set_handover)

@@ -1329,6 +1329,27 @@ lora_status_t lora_few_token_plan(int64_t T, int64_t d_in, int64_t d_out, int64_
   return LORA_OK;
 }
 
+lora_status_t lora_linear_x8_plan(int64_t T, int64_t d_in, int64_t d_out, int64_t r, int quantized, int want_dx,
+                                  lora_x8_plan_t *plan) {
+  if (!plan) return fail(LORA_EINVAL, "plan is NULL");
+  if ((quantized != 0 && quantized != 1) || (want_dx != 0 && want_dx != 1)) return fail(LORA_EINVAL, "quantized and want_dx are 0 or 1");
+  lora_status_t s = check_shapes(T, d_in, d_out, r, LORA_BF16);
+  if (s != LORA_OK) return s;
+  if (quantized && r > 64) return fail(LORA_EUNSUPPORTED, "rank r must be at most 64 with a quantized weight");
+  lora_x8_plan_t p{};
+  if (r > 0) {
+    const X8Layout L = x8_layout(T, d_in, d_out, r, quantized != 0, want_dx != 0);
+    p.few_tokens = L.few;
+    p.few_parts = L.few ? L.p.parts : 0;
+    p.fused = L.fused;
+    p.du_parts = L.few || L.fused ? 0 : L.sp.nsplit;
+    p.u_parts = L.u_parts;
+    p.token_ranges = x8_plan(T, d_in, d_out, r).parts;
+  }
+  *plan = p;
+  return LORA_OK;
+}
+
 lora_status_t lora_handover_giveups(uint64_t *count, int reset) {
   if (!count) return fail(LORA_EINVAL, "count is NULL");
   unsigned c = 0;

@@ -42,6 +42,11 @@ class _FewTokenPlan(ctypes.Structure):
     _fields_ += [(n, ctypes.c_size_t) for n in ("fwd_bytes", "bwd_bytes", "fwd_tiled_bytes", "bwd_tiled_bytes")]
 
 
+class _X8Plan(ctypes.Structure):
+    """lora_x8_plan_t of the C ABI."""
+    _fields_ = [(n, ctypes.c_int) for n in ("few_tokens", "few_parts", "fused", "du_parts", "u_parts", "token_ranges")]
+
+
 class _Grad(ctypes.Structure):
     """lora_grad_t of the C ABI."""
     _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64),
@@ -195,6 +200,8 @@ def lib() -> ctypes.CDLL:
     L.lora_linear_plan.restype = i32
     L.lora_few_token_plan.argtypes = [i64, i64, i64, i64, i32, ctypes.POINTER(_FewTokenPlan)]
     L.lora_few_token_plan.restype = i32
+    L.lora_linear_x8_plan.argtypes = [i64, i64, i64, i64, i32, i32, ctypes.POINTER(_X8Plan)]
+    L.lora_linear_x8_plan.restype = i32
     L.lora_debug_host_mapped.argtypes = [vp, sz]
     L.lora_debug_host_mapped.restype = i32
     L.lora_handover_giveups.argtypes = [ctypes.POINTER(ctypes.c_uint64), i32]
@@ -1034,6 +1041,14 @@ def lora_few_token_plan(T: int, d_in: int, d_out: int, r: int, dt: int = LORA_BF
     p = _FewTokenPlan()
     _check(lib().lora_few_token_plan(T, d_in, d_out, r, dt, ctypes.byref(p)), "lora_few_token_plan")
     return {n: getattr(p, n) for n, _ in _FewTokenPlan._fields_}
+
+
+def lora_linear_x8_plan(T: int, d_in: int, d_out: int, r: int, quantized: bool = False, want_dx: bool = True) -> dict:
+    """How lora_linear_bwd_x8 (lora_linear_bwd_q_x8 where `quantized`) runs these sizes: the kernel that dx comes from,
+    partial sums of du and u, ranges of tokens of dA and dB."""
+    p = _X8Plan()
+    _check(lib().lora_linear_x8_plan(T, d_in, d_out, r, int(quantized), int(want_dx), ctypes.byref(p)), "lora_linear_x8_plan")
+    return {n: getattr(p, n) for n, _ in _X8Plan._fields_}
 
 
 def handover_giveups(reset: bool = False) -> int:
