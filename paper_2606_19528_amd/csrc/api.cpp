@@ -740,11 +740,17 @@ struct X8Layout {
 X8Layout x8_layout(int64_t T, int64_t K, int64_t N, int64_t r, bool quant, bool dx) {
   X8Layout L{};
   if (r == 0) return L;
-  // (dx alone, and up to 256 tiles: 128 tokens of 512 -> 4096 15.3 us for 25.9, 256 -> 2048 14.5 for 16.8, 1024 ->
-  // 1024 with r = 32 14.5 for 13.9)
+  // dx alone up to 128 tokens where it has up to 256 tiles: 128 tokens of 256 -> 256 with r = 16 9.6 us for 10.8 with producers,
+  // 1024 -> 1024 12.2 for 12.8, 512 -> 4096 15.3 for 25.7; with r = 20, which has no producers, 1024 -> 1024 13.8 for
+  // 25.2.  Producers where they are and the ranks are more than 16, but for short and long reductions: with r = 32 256 ->
+  // 256 11.8 for 11.8, 1024 -> 640 12.9 for 12.7, 2048 -> 768 13.6 for 12.5, 1024 -> 1024 14.1 for 13.6, 1024 -> 1536 15.8 for
+  // 15.8, 2048 -> 2040 17.4 for 18.0, 512 -> 4096 17.3 for 26.4.
+  const bool producers = fuse_ok(T, K, N, r, LORA_BF16, true);
   L.p = narrow_plan(T, K, N, r, false);
-  L.few = dx && !quant && (few_rule(T, K, N, r, LORA_BF16).bwd || (L.p.ok && L.p.tiles_m * L.p.tiles_n <= 256));
-  L.fused = dx && !quant && !L.few && fuse_ok(T, K, N, r, LORA_BF16, true);
+  L.few = dx && !quant &&
+          (few_rule(T, K, N, r, LORA_BF16).bwd ||
+           (L.p.ok && L.p.tiles_m * L.p.tiles_n <= 256 && !(producers && r > 16 && N > 512 && N < 1536)));
+  L.fused = dx && !quant && !L.few && producers;
   L.u_parts = x8_down_parts(T, K);
   L.sp = L.few || L.fused ? whole_rows(N, DT_BF16) : row_split(T, N, (int)r, DT_BF16);
   L.ldt = tail_ld(L.sp.nsplit * (int)r, DT_BF16);

@@ -57,3 +57,13 @@ def test_the_sizes_reach_every_way(name, sizes):
 
 def test_two_blocks_of_ranks_in_the_few_token_kernel():
     assert ("few tokens", "up to 64", "33 ranks and more") in ways([(*s, 16) for s in SIZES])
+
+
+def test_few_tokens_or_producers():
+    """65 to 128 tokens over a W of fewer than 2^22 weights: the few-token kernel, but producers where they are and measured
+    faster, at more than 16 ranks and reductions of middle length."""
+    for K, N, r, few in ((256, 256, 8, 1), (1024, 1024, 16, 1), (1024, 1024, 20, 1), (1024, 1024, 32, 0), (2048, 768, 24, 0),
+                         (256, 640, 32, 0), (1024, 512, 32, 1), (1024, 1536, 32, 1), (512, 4096, 32, 1)):
+        for T in (72, 128):
+            p = lm.lora_linear_x8_plan(T, K, N, r)
+            assert p["few_tokens"] == few and p["fused"] == 1 - few, (T, K, N, r, p)
