@@ -438,7 +438,8 @@ lora_status_t grad_clip(const lora_grad_list_t *list, float max_norm, float *nor
  * row may be shorter), with m the largest magnitude in the group:
  *   scale[t][g] = m / 127
  *   code        = sign(x) floor(127 |x| / m + 1/2)    in [-127, 127], 0 where m = 0
- *   value       = scale code,   |value - x| <= m / 254
+ *   value       = scale code,   |value - x| <= m / 254 (and the rounding of scale and product; scale
+ *                               is subnormal, and so coarser, for m below 2^-119)
  * codes [T, D] int8, scale [T, ceil(D / 128)] fp32.  Codes are exactly these; a value
  * that is not finite makes its group's scale NaN (and its codes 0), so that all of the
  * group is restored as NaN.  D a multiple of 8 up to 2^20, T ceil(D / 128) up to 2^29
@@ -453,8 +454,10 @@ lora_status_t act8_dequantize(const int8_t *codes, const float *scale, void *x, 
  * its values: dx and du as there,
  *   dA = du^T xq,  dB = s dy^T u,  u = u_saved, or xq A^T where that is NULL.
  * Neither xq nor a bf16 copy of it is formed in memory.  Unlike there, du and u are not
- * rounded to bf16 in dA and dB (dx's LoRA term takes du in bf16).  A u recomputed differs
- * from the forward's by what x lost in 8 bits.  r = 0: x's codes are not read and may be
+ * rounded to bf16 in dA and dB (dx's LoRA term takes du in bf16, and its product a quantized
+ * W = s q + b rounded to bf16, as lora_linear_bwd_q does).  Where dy, du or u is not finite, or
+ * above the largest bf16, the sums that it enters are not finite: NaN also where the formula has
+ * an infinity.  A u recomputed differs from the forward's by what x lost in 8 bits.  r = 0: x's codes are not read and may be
  * NULL.  Errors and limits as there; workspace lora_linear_x8_workspace_bytes ((size_t)-1
  * for rejected sizes). */
 size_t lora_linear_x8_workspace_bytes(int64_t T, int64_t d_in, int64_t d_out, int64_t r);
@@ -535,8 +538,9 @@ lora_status_t block_norm_fwd(const block_norm_t *b, const void *h, const void *y
  *   dw_pre = sum_t dn hh,  dw_post = sum_t g z yh     [D] fp32, optional
  *   dgate = z yn, summed over what the gate is broadcast along, optional: fp32 for a gate a channel
  *           or a token, type dt for a full one
- * h is the forward's h_out, y its y, whole or as h8, y8; rstd_* the forward's.  Outputs are
- * overwritten.  Sums over rows are fp32 in a fixed order; they need a workspace of
+ * h is the forward's h_out, y its y, whole or as h8, y8; rstd_* the forward's.  Where a gain or a
+ * gate is infinite, dh (w_pre) or dy and a token's dgate of its rows are not finite, NaN also
+ * where the formulas have an infinity.  Outputs are overwritten.  Sums over rows are fp32 in a fixed order; they need a workspace of
  * block_norm_workspace_bytes ((size_t)-1 for rejected sizes), the other outputs none. */
 size_t block_norm_workspace_bytes(int64_t T, int64_t D);
 lora_status_t block_norm_bwd(const block_norm_t *b, const void *dn, const void *dh_out, const void *h,
