@@ -111,7 +111,7 @@ struct RowSum {
 // (16384 x 2048 forward with its 8-bit copies, read through the caches, 79.7 us, one vector 81.5, four 88; 4096 x 3072
 // backward 28.7, one 38, three 30.7).  Few rows: a lane's chain of loads and sums is the time,
 // so more waves share a row (one row of 2048 forward 2.2 us, with two waves 3.1).  The longest rows: 1024 x
-// 16384 forward 37.6 us, in 8 waves 38.6, with an fp32 stream 50 and 52.
+// 16384 forward 37.6 us, in 8 waves 38.6, with an fp32 stream (in 32 bits) 50 and 52, 51 in 64 bits.
 struct BnShape {
   int w, nv;
 };

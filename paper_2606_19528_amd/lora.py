@@ -932,7 +932,6 @@ def _gate_mode(gate, T: int, D: int) -> int:
 def _block(T, D, dtype, res_dtype, post_norm, w_post, w_pre, gate, gain_offset, res_scale, dev):
     if post_norm is None:
         post_norm = w_post is not None
-    # (an element of D = 1 or T = 1 makes two of a gate's shapes alike: either names the same values)
     mode = _gate_mode(gate, T, D)
     return _BlockNorm(T, D, _code(dtype), _code(res_dtype), 1 if post_norm else 0, mode, gain_offset, res_scale,
                       _dev_opt(w_post, "w_post", dtype, (D,), dev), _dev_opt(w_pre, "w_pre", dtype, (D,), dev),
